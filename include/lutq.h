@@ -385,6 +385,83 @@ lutq_status lutq_dequant(const void* packed, const void* scales, const void* lut
                          int bits, int group_size, int64_t N, int64_t K, lutq_dtype dtype,
                          void* W_out, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * Microscaled 4-bit floating point: both factors of the product at 4 bits, for any number of rows.
+ *
+ * A row of K values is cut into blocks of 32 consecutive ones.  A block holds one exponent byte e, which stands
+ * for 2^(e - 127) (255: not a number, the whole block is), and 32 codes of 4 bits: sign, two bits of exponent, one of
+ * mantissa, with the magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 in the order of the codes.  The value is code times power of two.
+ * (This is the E2M1 / E8M0 pair of the Open Compute microscaling formats, whose products the matrix
+ * instruction takes as they are.)
+ *
+ * Two forms hold it.  ROWS, for activations and for interchange: codes [M, K / 2] bytes, two codes a byte, the even column
+ * in the low four bits, and exponents [M, K / 32] bytes, both row-major.  PACKED, for weights (normative): N is cut into
+ * row blocks of 16 rows, K into tiles of 128 columns, four tiles to a quad, the last of which may be short.  A row block is a record of
+ * (K / 128) * 1024 + ceil(K / 512) * 256 bytes, first its tiles in order of K, then its exponents.  In a tile, lane l = 16 * o + i
+ * (i = 0..15, o = 0..3) owns the 16 bytes at offset 16 * l: the codes of row i, columns 32 * o .. 32 * o + 31 of the tile,
+ * what v_mfma_scale_f32_16x16x128_f8f6f4 takes from that lane.  In the exponents of a quad, byte t of the 4 bytes at offset
+ * 4 * l is the exponent of that lane's block in tile t (zero where the quad has no such tile).
+ *
+ * Domain: N a multiple of 16, K of 128, both up to 2^24; rows 0 <= M < 2^30 with M * K / 128 < 2^30 (no rows: nothing is
+ * done and no pointer is looked at); device pointers 16-byte aligned (rows and offsets: 4).
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of the packed form of an [N, K] matrix; 0 if the arguments are unsupported.  The experts of a grouped product are
+ * such records one behind the other. */
+size_t lutq_mx4_packed_bytes(int64_t N, int64_t K);
+
+/* From the row form to the packed one and back, host to host (a checkpoint that holds the format already; on the device
+ * lutq_mx4_quantize_packed packs what it quantises).  Errors: NULL, SHAPE. */
+lutq_status lutq_mx4_pack(const void* codes, const void* exponents, int64_t N, int64_t K, void* packed_out);
+lutq_status lutq_mx4_unpack(const void* packed, int64_t N, int64_t K, void* codes_out, void* exponents_out);
+
+/* Quantiser.  For each block, with a = max |x|: e = max(0, 125 + floor(log2 a)), 0 where a = 0; each code is x / 2^(e - 127)
+ * rounded to the nearest magnitude, ties to the even code, to 6 beyond it.  A block that holds an infinity or a NaN gets
+ * e = 255 and codes 0.
+ *   X       device, [source_rows, K] row-major; fp32 if x_is_f32 != 0, else `dtype`
+ *   rows    device, M row numbers (int32), or NULL: output row m is row rows[m] of X, a row of zeros where rows[m] is not
+ *           in 0 .. source_rows - 1.  NULL: row m (source_rows is then M)
+ *   codes_out, exponents_out   device, the row form, fully overwritten
+ * lutq_mx4_quantize_packed writes the packed form of W [N, K] instead.
+ * Asynchronous on `stream`.  Errors: NULL, SHAPE, DTYPE, ALIGN, DEVICE. */
+lutq_status lutq_mx4_quantize(const void* X, int x_is_f32, lutq_dtype dtype, int64_t source_rows, const int32_t* rows,
+                              int64_t M, int64_t K, void* codes_out, void* exponents_out, void* stream);
+lutq_status lutq_mx4_quantize_packed(const void* W, int w_is_f32, lutq_dtype dtype, int64_t N, int64_t K,
+                                     void* packed_out, void* stream);
+
+/* The values back, rounded once to the 16-bit `dtype` (exact in bf16 but beyond its largest number): [M, K] from the row
+ * form, [N, K] from the packed one.  Asynchronous on `stream`.  Errors: NULL, SHAPE, DTYPE, ALIGN, DEVICE. */
+lutq_status lutq_mx4_dequant(const void* codes, const void* exponents, int64_t M, int64_t K, lutq_dtype dtype,
+                             void* X_out, void* stream);
+lutq_status lutq_mx4_dequant_packed(const void* packed, int64_t N, int64_t K, lutq_dtype dtype, void* W_out, void* stream);
+
+/* Bytes of device scratch of the products below for up to M rows; experts = 1 for lutq_mx4_matmul.  0 if unsupported. */
+size_t lutq_mx4_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t experts);
+
+/* Y[m, n] = sum_k X[m, k] * W[n, k] over the 4-bit values of both, accumulated in fp32, rounded once to `dtype`.
+ *   X, x_exponents   device: the row form of the activations; or, x_exponents NULL, activations [M, K] of `dtype`, which
+ *                    are quantised on the way in, to what lutq_mx4_quantize would make of them
+ *   packed           device, the packed form of W [N, K]
+ *   Y                device, [M, N] row-major, dtype; fully overwritten
+ *   workspace        device, >= lutq_mx4_workspace_bytes(M, N, K, 1), zero-filled once before its first use, and then as for
+ *                    lutq_matmul: its first 64 KiB are left zero, calls that may run concurrently need one each
+ * Asynchronous on `stream`.  Errors: NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, DEVICE; Y untouched on error. */
+lutq_status lutq_mx4_matmul(const void* X, const void* x_exponents, const void* packed, int64_t M, int64_t N, int64_t K,
+                            lutq_dtype dtype, void* Y, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same by expert: rows offsets[g] .. offsets[g + 1] - 1 of X times the weights of expert g.
+ *   packed    device, `experts` packed forms of [N, K] one behind the other
+ *   offsets   device, experts + 1 row numbers (int32), not decreasing, within 0 .. M: read on the device, so the sizes may
+ *             come from a kernel before it on the stream, and a captured call follows them.  (Values outside are taken as the
+ *             nearest inside, an expert whose end is before its start has no rows, and rows that several experts claim
+ *             hold either's result.)
+ *   Y         [M, N]; rows before offsets[0] and from offsets[experts] on stay as they were
+ *   workspace >= lutq_mx4_workspace_bytes(M, N, K, experts)
+ * 1 <= experts <= 65536.  Everything else as for lutq_mx4_matmul. */
+lutq_status lutq_mx4_matmul_grouped(const void* X, const void* x_exponents, const void* packed, const int32_t* offsets,
+                                    int64_t experts, int64_t M, int64_t N, int64_t K, lutq_dtype dtype, void* Y,
+                                    void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

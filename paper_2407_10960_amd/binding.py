@@ -16,6 +16,8 @@ EXPORTED_SYMBOLS = (
     "lutq_status_string", "lutq_packed_bytes", "lutq_pack", "lutq_unpack", "lutq_workspace_bytes",
     "lutq_plan_default", "lutq_plan_default_for", "lutq_plan_check", "lutq_pack_layout", "lutq_plan_table_set", "lutq_plan_table_lookup", "lutq_matmul", "lutq_matmul_plan", "lutq_matmul_static", "lutq_matmul_channel", "lutq_matmul_pairs", "lutq_matmul_quads", "lutq_tune", "lutq_tune_candidates", "lutq_quantize", "lutq_dequant",
     "lutq_calib_stream_read", "lutq_calib_copy", "lutq_calib_matmul_trace", "lutq_calib_route", "lutq_calib_plan",
+    "lutq_mx4_packed_bytes", "lutq_mx4_pack", "lutq_mx4_unpack", "lutq_mx4_quantize", "lutq_mx4_quantize_packed", "lutq_mx4_dequant",
+    "lutq_mx4_dequant_packed", "lutq_mx4_workspace_bytes", "lutq_mx4_matmul", "lutq_mx4_matmul_grouped",
 )
 
 LUTQ_F16, LUTQ_BF16 = 0, 1
@@ -137,13 +139,25 @@ def load_library():
     lib.lutq_calib_route.argtypes = [ci, ci, i64, i64, i64, ci, ci, sz, ctypes.POINTER(ctypes.c_int)]
     lib.lutq_calib_plan.restype = ci
     lib.lutq_calib_plan.argtypes = [ci, ci, i64, i64, i64, ci, ci, sz, ctypes.POINTER(_CPlan), ci, ctypes.POINTER(_CPlan)]
+    lib.lutq_mx4_packed_bytes.restype = sz
+    lib.lutq_mx4_packed_bytes.argtypes = [i64, i64]
+    lib.lutq_mx4_workspace_bytes.restype = sz
+    lib.lutq_mx4_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    for name, args in (("pack", [vp, vp, i64, i64, vp]), ("unpack", [vp, i64, i64, vp, vp]),
+                       ("quantize", [vp, ci, ci, i64, vp, i64, i64, vp, vp, vp]),
+                       ("quantize_packed", [vp, ci, ci, i64, i64, vp, vp]),
+                       ("dequant", [vp, vp, i64, i64, ci, vp, vp]), ("dequant_packed", [vp, i64, i64, ci, vp, vp]),
+                       ("matmul", [vp, vp, vp, i64, i64, i64, ci, vp, vp, sz, vp]),
+                       ("matmul_grouped", [vp, vp, vp, vp, i64, i64, i64, i64, ci, vp, vp, sz, vp])):
+        f = getattr(lib, "lutq_mx4_" + name)
+        f.restype, f.argtypes = ci, args
     _LIB = lib
     return lib
 
 
 class _NoNative:
     """In place of the native part where it cannot be loaded: takes no call."""
-    mm = quantize = dequant = staticmethod(lambda *args: -1)
+    mm = quantize = dequant = mx4_quantize = mx4_dequant = mx4_mm = staticmethod(lambda *args: -1)
 
 
 def _native():
@@ -160,7 +174,9 @@ def _native():
             raise ImportError(f"built for torch {native.built_for}, this is {torch.__version__}")
         native.bind(*(ctypes.cast(getattr(lib, f), ctypes.c_void_p).value for f in
                       ("lutq_packed_bytes", "lutq_matmul", "lutq_matmul_static", "lutq_matmul_channel", "lutq_matmul_pairs",
-                       "lutq_matmul_quads", "lutq_quantize", "lutq_dequant")))
+                       "lutq_matmul_quads", "lutq_quantize", "lutq_dequant", "lutq_mx4_packed_bytes", "lutq_mx4_quantize",
+                       "lutq_mx4_quantize_packed", "lutq_mx4_dequant", "lutq_mx4_dequant_packed", "lutq_mx4_matmul",
+                       "lutq_mx4_matmul_grouped")))
     except ImportError as e:
         warnings.warn(f"calls take about 6 us more host time each: the binding's native part is not loaded ({e}); "
                       "`python -m paper_2407_10960_amd.build` builds it", RuntimeWarning, stacklevel=3)
@@ -510,6 +526,200 @@ def lutq_dequant(packed, scales, lut, bits: int, group_size: int, W_out, stream=
     _check(lib.lutq_dequant(packed.data_ptr(), scales.data_ptr(), lut.data_ptr(), bits, group_size, N, K, code,
                             W_out.data_ptr(), _stream_ptr(stream)), "lutq_dequant")
     return W_out
+
+
+# ------------------------------------------------------------------ microscaled 4-bit floating point
+def lutq_mx4_packed_bytes(N: int, K: int) -> int:
+    return int(load_library().lutq_mx4_packed_bytes(N, K))
+
+
+def lutq_mx4_pack(codes, exponents) -> np.ndarray:
+    """Row form on the host (codes [N, K / 2], exponents [N, K / 32], uint8) -> packed bytes (numpy uint8, 1-D)."""
+    lib = load_library()
+    c, e = (np.ascontiguousarray(np.asarray(a, dtype=np.uint8)) for a in (codes, exponents))
+    if c.ndim != 2 or e.ndim != 2 or c.shape[0] != e.shape[0] or c.shape[1] != 16 * e.shape[1]:
+        raise ValueError("codes must be [N, K / 2] and exponents [N, K / 32]")
+    N, K = c.shape[0], 2 * c.shape[1]
+    out = np.empty(max(int(lib.lutq_mx4_packed_bytes(N, K)), 1), dtype=np.uint8)
+    _check(lib.lutq_mx4_pack(c.ctypes.data, e.ctypes.data, N, K, out.ctypes.data), "lutq_mx4_pack")
+    return out
+
+
+def lutq_mx4_unpack(packed, N: int, K: int) -> tuple:
+    """Packed bytes on the host -> (codes [N, K / 2], exponents [N, K / 32])."""
+    lib = load_library()
+    buf = np.ascontiguousarray(np.asarray(packed, dtype=np.uint8)).reshape(-1)
+    if buf.size == 0 or buf.size != lib.lutq_mx4_packed_bytes(N, K):
+        raise ValueError("packed buffer has the wrong size for (N, K)")
+    c, e = np.empty((N, K // 2), dtype=np.uint8), np.empty((N, K // 32), dtype=np.uint8)
+    _check(lib.lutq_mx4_unpack(buf.ctypes.data, N, K, c.ctypes.data, e.ctypes.data), "lutq_mx4_unpack")
+    return c, e
+
+
+def lutq_mx4_workspace_bytes(M: int, N: int, K: int, experts: int = 1) -> int:
+    return int(load_library().lutq_mx4_workspace_bytes(M, N, K, experts))
+
+
+def new_mx4_workspace(M: int, N: int, K: int, experts: int = 1, device="cuda"):
+    """A zero-filled device workspace for the products of up to M rows (reusable across calls on one stream)."""
+    torch = _torch()
+    n = lutq_mx4_workspace_bytes(M, N, K, experts)
+    if n == 0:
+        raise ValueError("unsupported problem")
+    return torch.zeros(n, dtype=torch.uint8, device=device)
+
+
+def _mx4_tensors(name, stream, *tensors):
+    """Checks that the tensors are contiguous and on one device; that device's index and the stream to launch on."""
+    torch = _torch()
+    given = [t for t in tensors if t is not None]
+    for t in given:
+        if not (t.is_cuda and t.is_contiguous()):
+            raise ValueError(f"{name} needs contiguous CUDA (HIP) tensors")
+        if t.device != given[0].device:
+            raise ValueError(f"{name} needs its tensors on one device")
+    device = given[0].device
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    elif getattr(stream, "device", device) != device:
+        raise ValueError(f"{name} needs a stream of the tensors' device")
+    return device, int(stream.cuda_stream)
+
+
+def _mx4_bytes(name, *tensors):
+    torch = _torch()
+    for t in tensors:
+        if t is not None and t.dtype != torch.uint8:
+            raise TypeError(f"{name}: codes, exponents, packed and workspace must be uint8")
+
+
+def _mx4_source(x, name) -> tuple:
+    """(whether it is fp32, dtype code) of dense values."""
+    torch = _torch()
+    if x.dtype == torch.float32:
+        return 1, LUTQ_F16
+    if x.dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"{name}: dense values must be float32, float16 or bfloat16")
+    return 0, _dtype_code(x)
+
+
+def lutq_mx4_quantize(X, codes_out, exponents_out, rows=None, stream=None):
+    """Quantises X [., K] (float32, float16, bfloat16) to codes [M, K / 2] and exponent bytes [M, K / 32] (uint8).  With rows
+    (int32, [M], on the device) output row m is row rows[m] of X, zeros where that is no row of X."""
+    if stream is None and _done(_native().mx4_quantize(X, codes_out, exponents_out, rows), "lutq_mx4_quantize"):
+        return codes_out, exponents_out
+    torch = _torch()
+    device, on = _mx4_tensors("lutq_mx4_quantize", stream, X, codes_out, exponents_out, rows)
+    _mx4_bytes("lutq_mx4_quantize", codes_out, exponents_out)
+    f32, code = _mx4_source(X, "lutq_mx4_quantize")
+    if rows is not None and (rows.dtype != torch.int32 or rows.dim() != 1):
+        raise TypeError("lutq_mx4_quantize: rows must be int32, [M]")
+    if X.dim() != 2:
+        raise ValueError("inconsistent shapes")
+    M, K = (X.shape[0] if rows is None else rows.shape[0]), X.shape[1]
+    if K % 32 != 0 or tuple(codes_out.shape) != (M, K // 2) or tuple(exponents_out.shape) != (M, K // 32):
+        raise ValueError("inconsistent shapes")
+    with torch.cuda.device(device):
+        _check(load_library().lutq_mx4_quantize(X.data_ptr(), f32, code, X.shape[0], rows.data_ptr() if rows is not None else None,
+                                                M, K, codes_out.data_ptr(), exponents_out.data_ptr(), on), "lutq_mx4_quantize")
+    return codes_out, exponents_out
+
+
+def lutq_mx4_quantize_packed(W, packed_out, stream=None):
+    """Quantises W [N, K] (float32, float16, bfloat16) to the packed form that the products read."""
+    if stream is None and _done(_native().mx4_quantize(W, packed_out, None, None), "lutq_mx4_quantize_packed"):
+        return packed_out
+    torch = _torch()
+    device, on = _mx4_tensors("lutq_mx4_quantize_packed", stream, W, packed_out)
+    _mx4_bytes("lutq_mx4_quantize_packed", packed_out)
+    f32, code = _mx4_source(W, "lutq_mx4_quantize_packed")
+    N, K = W.shape
+    if packed_out.numel() == 0 or packed_out.numel() != lutq_mx4_packed_bytes(N, K):
+        raise ValueError("packed buffer has the wrong size for (N, K)")
+    with torch.cuda.device(device):
+        _check(load_library().lutq_mx4_quantize_packed(W.data_ptr(), f32, code, N, K, packed_out.data_ptr(), on),
+               "lutq_mx4_quantize_packed")
+    return packed_out
+
+
+def lutq_mx4_dequant(codes, exponents, X_out, stream=None):
+    """X_out [M, K] (float16 or bfloat16) = the values that codes and exponents stand for."""
+    if stream is None and _done(_native().mx4_dequant(codes, exponents, X_out), "lutq_mx4_dequant"):
+        return X_out
+    torch = _torch()
+    device, on = _mx4_tensors("lutq_mx4_dequant", stream, codes, exponents, X_out)
+    _mx4_bytes("lutq_mx4_dequant", codes, exponents)
+    code = _dtype_code(X_out)
+    M, K = X_out.shape
+    if K % 32 != 0 or tuple(codes.shape) != (M, K // 2) or tuple(exponents.shape) != (M, K // 32):
+        raise ValueError("inconsistent shapes")
+    with torch.cuda.device(device):
+        _check(load_library().lutq_mx4_dequant(codes.data_ptr(), exponents.data_ptr(), M, K, code, X_out.data_ptr(), on),
+               "lutq_mx4_dequant")
+    return X_out
+
+
+def lutq_mx4_dequant_packed(packed, W_out, stream=None):
+    """W_out [N, K] (float16 or bfloat16) = the values that the packed form stands for."""
+    if stream is None and _done(_native().mx4_dequant(packed, None, W_out), "lutq_mx4_dequant_packed"):
+        return W_out
+    torch = _torch()
+    device, on = _mx4_tensors("lutq_mx4_dequant_packed", stream, packed, W_out)
+    _mx4_bytes("lutq_mx4_dequant_packed", packed)
+    code = _dtype_code(W_out)
+    N, K = W_out.shape
+    if packed.numel() == 0 or packed.numel() != lutq_mx4_packed_bytes(N, K):
+        raise ValueError("packed buffer has the wrong size for (N, K)")
+    with torch.cuda.device(device):
+        _check(load_library().lutq_mx4_dequant_packed(packed.data_ptr(), N, K, code, W_out.data_ptr(), on),
+               "lutq_mx4_dequant_packed")
+    return W_out
+
+
+def _mx4_product(name, X, packed, offsets, Y, workspace, x_scales, stream):
+    if stream is None and _done(_native().mx4_mm(X, x_scales, packed, offsets, Y, workspace), name):
+        return Y
+    torch = _torch()
+    device, on = _mx4_tensors(name, stream, X, x_scales, packed, offsets, Y, workspace)
+    _mx4_bytes(name, x_scales, packed, workspace)
+    code = _dtype_code(Y)
+    if X.dtype != (Y.dtype if x_scales is None else torch.uint8):
+        raise TypeError(f"{name}: X must be uint8 codes with x_scales, or share the dtype of Y without")
+    if X.dim() != 2 or Y.dim() != 2 or X.shape[0] != Y.shape[0]:
+        raise ValueError("inconsistent shapes")
+    M, N = Y.shape
+    K = X.shape[1] * (1 if x_scales is None else 2)
+    experts = 1
+    if offsets is not None:
+        if offsets.dtype != torch.int32 or offsets.dim() != 1:
+            raise TypeError(f"{name}: offsets must be int32, [experts + 1]")
+        experts = offsets.shape[0] - 1
+    if x_scales is not None and (K % 32 != 0 or tuple(x_scales.shape) != (M, K // 32)):
+        raise ValueError("inconsistent shapes")
+    if experts < 1 or packed.numel() == 0 or packed.numel() != experts * lutq_mx4_packed_bytes(N, K):
+        raise ValueError("packed buffer has the wrong size for (N, K)" + ("" if offsets is None else " and the number of experts"))
+    head = [X.data_ptr(), x_scales.data_ptr() if x_scales is not None else None, packed.data_ptr()]
+    tail = [M, N, K, code, Y.data_ptr(), workspace.data_ptr(), workspace.numel(), on]
+    with torch.cuda.device(device):
+        if offsets is None:
+            _check(load_library().lutq_mx4_matmul(*head, *tail), name)
+        else:
+            _check(load_library().lutq_mx4_matmul_grouped(*head, offsets.data_ptr(), experts, *tail), name)
+    return Y
+
+
+def lutq_mx4_matmul(X, packed, Y, workspace, x_scales=None, stream=None):
+    """Y [M, N] = X W^T with both factors at 4 bits.  X: codes [M, K / 2] (uint8) with x_scales [M, K / 32], or values
+    [M, K] of Y's dtype, which are quantised on the way in.  packed: W from lutq_mx4_quantize_packed."""
+    return _mx4_product("lutq_mx4_matmul", X, packed, None, Y, workspace, x_scales, stream)
+
+
+def lutq_mx4_matmul_grouped(X, packed, offsets, Y, workspace, x_scales=None, stream=None):
+    """The same by expert: rows offsets[g] .. offsets[g + 1] (int32, on the device) of X times the weights of expert g, of
+    which packed holds offsets.numel() - 1 one behind the other.  Rows outside stay as they were."""
+    if offsets is None:
+        raise TypeError("lutq_mx4_matmul_grouped: offsets must be int32, [experts + 1]")
+    return _mx4_product("lutq_mx4_matmul_grouped", X, packed, offsets, Y, workspace, x_scales, stream)
 
 
 # ------------------------------------------------------------------ measurement helpers

@@ -25,6 +25,23 @@ inline int64_t tile_index(int64_t rb, int64_t kt, int64_t KT, int SB) { return (
 
 }  // namespace layout
 
+// The packed form of the microscaled 4-bit weights (include/lutq.h): a record per row block of 16 rows, K tiles of 128
+// columns and 1 KiB, then 256 bytes of exponents per four tiles.  The record's length is an odd number of 256-byte pieces
+// more than a power of two for the usual K, so that row blocks streamed side by side do not start in the same memory channel.
+namespace mx4 {
+
+inline int64_t k_tiles(int64_t K) { return K / 128; }
+inline int64_t k_quads(int64_t K) { return (K + 511) / 512; }
+inline int64_t record_bytes(int64_t K) { return k_tiles(K) * 1024 + k_quads(K) * 256; }
+inline bool shape_ok(int64_t N, int64_t K) {
+    return N > 0 && K > 0 && N <= (1 << 24) && K <= (1 << 24) && N % 16 == 0 && K % 128 == 0;
+}
+inline bool rows_ok(int64_t M, int64_t K) {
+    return M >= 0 && K > 0 && K <= (1 << 24) && K % 128 == 0 && M < (int64_t(1) << 30) && M * (K / 128) < (int64_t(1) << 30);
+}
+
+}  // namespace mx4
+
 // Compute units of the current device, 0 if it cannot be asked (lutq_api.hip).
 int compute_units();
 

@@ -133,3 +133,47 @@ extern "C" lutq_status lutq_unpack(const void* packed, int64_t N, int64_t K, int
     }
     return LUTQ_OK;
 }
+
+extern "C" size_t lutq_mx4_packed_bytes(int64_t N, int64_t K) {
+    return lutq::mx4::shape_ok(N, K) ? (size_t)(N / 16) * (size_t)lutq::mx4::record_bytes(K) : 0;
+}
+
+namespace {
+
+// Visits the blocks of 32 values: f(row, block of the row, byte of its codes in the packed form, byte of its exponent there)
+template <typename F> void each_mx4_block(int64_t N, int64_t K, F f) {
+    const int64_t rec = lutq::mx4::record_bytes(K), KT = lutq::mx4::k_tiles(K);
+#pragma omp parallel for
+    for (int64_t rb = 0; rb < N / 16; ++rb)
+        for (int64_t kt = 0; kt < KT; ++kt)
+            for (int l = 0; l < 64; ++l)
+                f(16 * rb + (l & 15), 4 * kt + (l >> 4), rb * rec + kt * 1024 + 16 * l,
+                  rb * rec + KT * 1024 + (kt >> 2) * 256 + 4 * l + (kt & 3));
+}
+
+}  // namespace
+
+extern "C" lutq_status lutq_mx4_pack(const void* codes, const void* exponents, int64_t N, int64_t K, void* packed_out) {
+    if (!codes || !exponents || !packed_out) return LUTQ_ERR_NULL;
+    if (!lutq::mx4::shape_ok(N, K)) return LUTQ_ERR_SHAPE;
+    const uint8_t *c = static_cast<const uint8_t*>(codes), *e = static_cast<const uint8_t*>(exponents);
+    uint8_t* p = static_cast<uint8_t*>(packed_out);
+    std::memset(p, 0, lutq_mx4_packed_bytes(N, K));
+    each_mx4_block(N, K, [=](int64_t n, int64_t b, int64_t at, int64_t eat) {
+        std::memcpy(p + at, c + n * (K / 2) + b * 16, 16);
+        p[eat] = e[n * (K / 32) + b];
+    });
+    return LUTQ_OK;
+}
+
+extern "C" lutq_status lutq_mx4_unpack(const void* packed, int64_t N, int64_t K, void* codes_out, void* exponents_out) {
+    if (!packed || !codes_out || !exponents_out) return LUTQ_ERR_NULL;
+    if (!lutq::mx4::shape_ok(N, K)) return LUTQ_ERR_SHAPE;
+    const uint8_t* p = static_cast<const uint8_t*>(packed);
+    uint8_t *c = static_cast<uint8_t*>(codes_out), *e = static_cast<uint8_t*>(exponents_out);
+    each_mx4_block(N, K, [=](int64_t n, int64_t b, int64_t at, int64_t eat) {
+        std::memcpy(c + n * (K / 2) + b * 16, p + at, 16);
+        e[n * (K / 32) + b] = p[eat];
+    });
+    return LUTQ_OK;
+}

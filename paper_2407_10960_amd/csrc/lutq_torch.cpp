@@ -25,12 +25,19 @@ decltype(&lutq_matmul_pairs) matmul_pairs = nullptr;
 decltype(&lutq_matmul_quads) matmul_quads = nullptr;
 decltype(&lutq_quantize) quantize = nullptr;
 decltype(&lutq_dequant) dequant = nullptr;
+decltype(&lutq_mx4_packed_bytes) mx4_packed_bytes = nullptr;
+decltype(&lutq_mx4_quantize) mx4_quantize = nullptr;
+decltype(&lutq_mx4_quantize_packed) mx4_quantize_packed = nullptr;
+decltype(&lutq_mx4_dequant) mx4_dequant = nullptr;
+decltype(&lutq_mx4_dequant_packed) mx4_dequant_packed = nullptr;
+decltype(&lutq_mx4_matmul) mx4_matmul = nullptr;
+decltype(&lutq_mx4_matmul_grouped) mx4_matmul_grouped = nullptr;
 
 // the functions of liblutq.so by address, in the order of the declarations above
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    void* p[8];
-    if (n != 8) { PyErr_SetString(PyExc_TypeError, "eight addresses"); return nullptr; }
-    for (int i = 0; i < 8; ++i) {
+    void* p[15];
+    if (n != 15) { PyErr_SetString(PyExc_TypeError, "fifteen addresses"); return nullptr; }
+    for (int i = 0; i < 15; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (!p[i]) { if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address"); return nullptr; }
     }
@@ -42,6 +49,13 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     matmul_quads = reinterpret_cast<decltype(matmul_quads)>(p[5]);
     quantize = reinterpret_cast<decltype(quantize)>(p[6]);
     dequant = reinterpret_cast<decltype(dequant)>(p[7]);
+    mx4_packed_bytes = reinterpret_cast<decltype(mx4_packed_bytes)>(p[8]);
+    mx4_quantize = reinterpret_cast<decltype(mx4_quantize)>(p[9]);
+    mx4_quantize_packed = reinterpret_cast<decltype(mx4_quantize_packed)>(p[10]);
+    mx4_dequant = reinterpret_cast<decltype(mx4_dequant)>(p[11]);
+    mx4_dequant_packed = reinterpret_cast<decltype(mx4_dequant_packed)>(p[12]);
+    mx4_matmul = reinterpret_cast<decltype(mx4_matmul)>(p[13]);
+    mx4_matmul_grouped = reinterpret_cast<decltype(mx4_matmul_grouped)>(p[14]);
     Py_RETURN_NONE;
 }
 
@@ -166,11 +180,105 @@ PyObject* dequantise(PyObject*, PyObject* const* args, Py_ssize_t n) { return an
     return PyLong_FromLong((long)st);
 }); }
 
+// Whether `o` is None (then *t stays null) or a plain tensor.
+bool plain_or_none(PyObject* o, const at::Tensor** t) {
+    if (o == Py_None) return true;
+    *t = plain(o);
+    return *t != nullptr;
+}
+
+// Tensors (null ones aside) on the current device.  (The older calls leave the device to the caller.)
+template <typename... T> bool on_current_device(const T*... t) {
+    const auto here = c10::hip::current_device();
+    return ((!t || t->get_device() == here) && ...);
+}
+
+bool is_bytes(const at::Tensor* t) { return !t || t->scalar_type() == at::kByte; }
+bool is_numbers(const at::Tensor* t) { return !t || (t->scalar_type() == at::kInt && t->dim() == 1); }
+
+// (X, codes, exponents or None for the packed form, rows or None) -> status, or -1
+PyObject* mx4_quant(PyObject*, PyObject* const* args, Py_ssize_t n) { return answer([&]() -> PyObject* {
+    if (!mx4_quantize || n != 4) return PyLong_FromLong(-1);
+    const at::Tensor *X = plain(args[0]), *codes = plain(args[1]), *exponents = nullptr, *rows = nullptr;
+    if (!X || !codes || !plain_or_none(args[2], &exponents) || !plain_or_none(args[3], &rows) || X->dim() != 2 ||
+        !on_current_device(X, codes, exponents, rows) || !is_bytes(codes) || !is_bytes(exponents) || !is_numbers(rows))
+        return PyLong_FromLong(-1);
+    const bool f32 = X->scalar_type() == at::kFloat;
+    const int code = f32 ? LUTQ_F16 : dtype_code(*X);
+    const int64_t from = X->size(0), K = X->size(1), M = rows ? rows->size(0) : from;
+    if (code < 0) return PyLong_FromLong(-1);
+    if (exponents ? K % 32 != 0 || !shape_is(*codes, M, K / 2) || !shape_is(*exponents, M, K / 32)
+                  : rows || codes->numel() == 0 || codes->numel() != (int64_t)mx4_packed_bytes(M, K))
+        return PyLong_FromLong(-1);
+    const void *x = X->data_ptr(), *r = rows ? rows->data_ptr() : nullptr;
+    void *c = codes->data_ptr(), *e = exponents ? exponents->data_ptr() : nullptr, *stream = current_stream();
+    const lutq_dtype dt = (lutq_dtype)code;
+    lutq_status st;
+    {
+        WithoutGil released;
+        st = e || exponents ? mx4_quantize(x, f32, dt, from, static_cast<const int32_t*>(r), M, K, c, e, stream)
+                            : mx4_quantize_packed(x, f32, dt, M, K, c, stream);
+    }
+    return PyLong_FromLong((long)st);
+}); }
+
+// (codes, exponents or None for the packed form, out) -> status, or -1
+PyObject* mx4_dequantise(PyObject*, PyObject* const* args, Py_ssize_t n) { return answer([&]() -> PyObject* {
+    if (!mx4_dequant || n != 3) return PyLong_FromLong(-1);
+    const at::Tensor *codes = plain(args[0]), *exponents = nullptr, *out = plain(args[2]);
+    if (!codes || !plain_or_none(args[1], &exponents) || !out || out->dim() != 2 || !on_current_device(codes, exponents, out) ||
+        !is_bytes(codes) || !is_bytes(exponents))
+        return PyLong_FromLong(-1);
+    const int code = dtype_code(*out);
+    const int64_t M = out->size(0), K = out->size(1);
+    if (code < 0) return PyLong_FromLong(-1);
+    if (exponents ? K % 32 != 0 || !shape_is(*codes, M, K / 2) || !shape_is(*exponents, M, K / 32)
+                  : codes->numel() == 0 || codes->numel() != (int64_t)mx4_packed_bytes(M, K))
+        return PyLong_FromLong(-1);
+    const void *c = codes->data_ptr(), *e = exponents ? exponents->data_ptr() : nullptr;
+    void *w = out->data_ptr(), *stream = current_stream();
+    lutq_status st;
+    {
+        WithoutGil released;
+        st = exponents ? mx4_dequant(c, e, M, K, (lutq_dtype)code, w, stream) : mx4_dequant_packed(c, M, K, (lutq_dtype)code, w, stream);
+    }
+    return PyLong_FromLong((long)st);
+}); }
+
+// (X, exponents or None, packed, offsets or None, Y, workspace) -> status, or -1
+PyObject* mx4_mm(PyObject*, PyObject* const* args, Py_ssize_t n) { return answer([&]() -> PyObject* {
+    if (!mx4_matmul || n != 6) return PyLong_FromLong(-1);
+    const at::Tensor *X = plain(args[0]), *xe = nullptr, *packed = plain(args[2]), *offsets = nullptr, *Y = plain(args[4]), *ws = plain(args[5]);
+    if (!X || !plain_or_none(args[1], &xe) || !packed || !plain_or_none(args[3], &offsets) || !Y || !ws || X->dim() != 2 || Y->dim() != 2 ||
+        !on_current_device(X, xe, packed, offsets, Y, ws) || !is_bytes(xe) || !is_bytes(packed) || !is_bytes(ws) || !is_numbers(offsets))
+        return PyLong_FromLong(-1);
+    const int code = dtype_code(*Y);
+    const int64_t M = Y->size(0), N = Y->size(1), K = X->size(1) * (xe ? 2 : 1), experts = offsets ? offsets->size(0) - 1 : 1;
+    if (code < 0 || X->size(0) != M || (xe ? X->scalar_type() != at::kByte || K % 32 != 0 || !shape_is(*xe, M, K / 32)
+                                           : X->scalar_type() != Y->scalar_type()))
+        return PyLong_FromLong(-1);
+    if (experts < 1 || packed->numel() == 0 || packed->numel() != experts * (int64_t)mx4_packed_bytes(N, K)) return PyLong_FromLong(-1);
+    const void *x = X->data_ptr(), *e = xe ? xe->data_ptr() : nullptr, *w = packed->data_ptr(), *at = offsets ? offsets->data_ptr() : nullptr;
+    void *y = Y->data_ptr(), *scratch = ws->data_ptr(), *stream = current_stream();
+    const size_t bytes = (size_t)ws->numel();
+    const lutq_dtype dt = (lutq_dtype)code;
+    lutq_status st;
+    {
+        WithoutGil released;
+        st = offsets ? mx4_matmul_grouped(x, e, w, static_cast<const int32_t*>(at), experts, M, N, K, dt, y, scratch, bytes, stream)
+                     : mx4_matmul(x, e, w, M, N, K, dt, y, scratch, bytes, stream);
+    }
+    return PyLong_FromLong((long)st);
+}); }
+
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
     {"mm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mm)), METH_FASTCALL, nullptr},
     {"quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quant)), METH_FASTCALL, nullptr},
     {"dequant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(dequantise)), METH_FASTCALL, nullptr},
+    {"mx4_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx4_quant)), METH_FASTCALL, nullptr},
+    {"mx4_dequant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx4_dequantise)), METH_FASTCALL, nullptr},
+    {"mx4_mm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx4_mm)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lutq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
