@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "lutq.h"
 #include "lutq_layout.hpp"
@@ -16,6 +17,14 @@ namespace mx4 {
 lutq_status quantize_rows_on(const void* X, int source, int64_t source_rows, const int32_t* rows, int64_t M, int64_t K,
                              void* codes, void* exponents, hipStream_t stream);
 
+// Sixteen bytes per lane from memory to LDS, where lane l's go to `to` + 16 l.
+__device__ __forceinline__ void copy16(__amdgpu_buffer_rsrc_t from, uint32_t lane_at, int at, char* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_at, at, 0, 0);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t unbounded(const char* base) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (uint32_t)-1, 0x00020000);
+}
+
 struct ProductParams {
     const char* x;             // row form: codes; or 16-bit values
     const char* xe;            // row form: exponents
@@ -25,7 +34,7 @@ struct ProductParams {
     int64_t record, expert;    // bytes of a row block's record, of an expert's weights
     int M, N, K, KT, KQ, NB;   // K tiles, quads, row blocks
     int experts;
-    int slot0;                 // first piece of rows of this launch
+    int slot0, slots;          // first piece of rows of this launch, and how many
     int bf16;                  // type of Y
 };
 
@@ -148,6 +157,197 @@ __global__ __launch_bounds__(512) void stream_kernel(const ProductParams p) {
     }
 }
 
+// Waits until at most N of this wavefront's global loads are under way and all its LDS reads are done, then for the workgroup.
+template <int N> __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
+
+// Many rows: a workgroup of GN x GM wavefronts owns 16 WN GN rows of weights times 16 WM GM rows of X, each wavefront WN x WM blocks of
+// sixteen by sixteen.  K goes by in steps of two tiles (256 columns), which are copied from memory into LDS without passing through
+// registers; two steps fit, so one is under way while the other is multiplied.  The operands of one tile are read from LDS while the matrix
+// instructions of the tile before run.  The exponents come the same way, a quad (two steps) at a time.  K >= 512.
+//
+// In LDS the weights lie as in memory, in operand order.  Of X a piece is sixteen rows of 128 bytes, whole cache lines as they are
+// read (a line asked for in halves, a step apart, was fetched twice); block b of row i lies at 16 (b ^ (i >> 1)), so that the
+// sixteen lanes that are served together hit all banks.
+template <int WN, int WM, int GN, int GM, bool GROUPED>
+__global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductParams p) {
+    constexpr int kWaves = GN * GM, kRB = WN * GN, kMB = WM * GM;              // pieces of sixteen rows of either factor
+    constexpr int kWLoads = kRB / kWaves, kXLoads = 2 * kMB / kWaves;          // per wavefront: pieces of weights, halves of pieces of X
+    constexpr int kLoads = 2 * kWLoads + kXLoads;
+    constexpr int kExpPieces = (kRB + kMB) / 4, kExpLoads = (kExpPieces + kWaves - 1) / kWaves;
+    static_assert(kRB % kWaves == 0 && 2 * kMB % kWaves == 0 && kRB % 4 == 0 && kMB % 4 == 0, "whole loads per wavefront");
+    constexpr int kStep = (kRB + kMB) * 2048, kExps = (kRB + kMB) * 256;
+    __shared__ __align__(1024) char lds[2 * kStep + kExps];
+    using std::integral_constant;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int i = lane & 15, o = lane >> 4;
+
+    // Workgroups go to the eight dies in turn: each die gets a run of consecutive tiles of Y, ordered in bands of kBand pieces of rows
+    // of X, so that what its cache holds of either factor is used several times.
+    constexpr int kBand = 4;
+    const int nx = (p.NB + kRB - 1) / kRB, per = (int)(gridDim.x >> 3);
+    int id = (int)blockIdx.x;
+    if (id < per * 8) id = (id & 7) * per + (id >> 3);
+    const int band = id / (kBand * nx), inside = id - band * kBand * nx;
+    const int high = min(kBand, p.slots - band * kBand);
+    const int nt = inside / high, slot = p.slot0 + band * kBand + (inside - nt * high);
+    int expert = 0, m0 = slot * 16 * kMB, m1 = min(p.M, m0 + 16 * kMB);
+    if (GROUPED && !find_piece<16 * kMB>(p.offsets, p.experts, p.M, slot, expert, m0, m1)) return;
+    const int rb0 = nt * kRB, rows = m1 - m0;
+
+    // Byte offsets of this lane in what the wavefront copies.  Rows and row blocks past the end repeat the last.
+    const int last_rb = p.NB - 1 - rb0, half = p.K / 2, ebytes = p.K / 32;
+    const auto wsrc = unbounded(p.w + expert * p.expert + rb0 * p.record);
+    const auto xsrc = unbounded(p.x + (int64_t)m0 * half);
+    const auto esrc = unbounded(p.xe + (int64_t)m0 * ebytes);
+    const int block = (lane & 7) ^ (lane >> 4);        // of the row that this lane copies (i >> 1 of row i = 8 g + lane / 8 is 4 g + lane / 16)
+    uint32_t wfrom[kWLoads], xfrom[kXLoads], efrom[kExpLoads];
+#pragma unroll
+    for (int j = 0; j < kWLoads; ++j) wfrom[j] = (uint32_t)min(wave + kWaves * j, last_rb) * (uint32_t)p.record + lane * 16;
+#pragma unroll
+    for (int j = 0; j < kXLoads; ++j) {
+        const int c = wave + kWaves * j;               // eight rows
+        xfrom[j] = (uint32_t)min(8 * c + (lane >> 3), rows - 1) * (uint32_t)half + (block ^ (4 * (c & 1))) * 16;
+    }
+#pragma unroll
+    for (int j = 0; j < kExpLoads; ++j) {
+        const int c = min(wave + kWaves * j, kExpPieces - 1);                  // (the last may be copied twice)
+        efrom[j] = c < kRB / 4 ? (uint32_t)min(4 * c + o, last_rb) * (uint32_t)p.record + (uint32_t)p.KT * 1024 + i * 16
+                               : (uint32_t)min(64 * (c - kRB / 4) + lane, rows - 1) * (uint32_t)ebytes;
+    }
+    // Copy `j` of this wavefront's kLoads of a step.
+    auto load_part = [&](int step, int buffer, int j) {
+        char* to = lds + buffer * kStep;
+        // An odd last step has one tile: the second is the first again, so that nothing behind the rows is touched, and
+        // has exponents of zero on both sides, 2^-254 for their products, which adds nothing to an fp32 sum.
+        const bool whole = 2 * step + 1 < p.KT;
+        if (j < 2 * kWLoads) {
+            const int c = wave + kWaves * (j >> 1), second = j & 1;
+            copy16(wsrc, wfrom[j >> 1], step * 2048 + (second && whole ? 1024 : 0), to + c * 2048 + second * 1024);
+        } else {
+            const int c = wave + kWaves * (j - 2 * kWLoads);
+            const uint32_t at = xfrom[j - 2 * kWLoads], from = whole ? at : at - ((block ^ (4 * (c & 1))) & 4) * 16;
+            copy16(xsrc, from, step * 128, to + kRB * 2048 + c * 1024);
+        }
+    };
+    auto load_step = [&](int step, int buffer) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) load_part(step, buffer, j);
+    };
+    // Exponents of a quad: of a row block of weights its 256 bytes, of a row of X its sixteen.  The row's last quad may be short: the
+    // sixteen bytes that end with the row are taken then, so that no byte behind X is touched.
+    auto load_exps = [&](int q) {
+        char* to = lds + 2 * kStep;
+#pragma unroll
+        for (int j = 0; j < kExpLoads; ++j) {
+            const int c = min(wave + kWaves * j, kExpPieces - 1);
+            if (c < kRB / 4) copy16(wsrc, efrom[j], q * 256, to + c * 1024);
+            else copy16(esrc, efrom[j], min(q * 16, ebytes - 16), to + c * 1024);
+        }
+    };
+
+    const int wn = wave % GN, wm = wave / GN;
+    u32x4 w[WN], x[2][WM];
+    uint32_t we[WN], xe[WM];
+    f32x4 acc[WN][WM] = {};
+    const char* const wplace = lds + lane * 16 + wn * WN * 2048;
+    const char* const xplace = lds + kRB * 2048 + i * 128 + wm * WM * 2048;
+    const int xblock[2] = {(o ^ (i >> 1)) * 16, ((4 + o) ^ (i >> 1)) * 16};
+    auto read_w = [&](int buffer, int h, int r) { w[r] = *reinterpret_cast<const u32x4*>(wplace + buffer * kStep + h * 1024 + r * 2048); };
+    auto read_x = [&](int buffer, int h) {
+#pragma unroll
+        for (int b = 0; b < WM; ++b) x[h][b] = *reinterpret_cast<const u32x4*>(xplace + xblock[h] + buffer * kStep + b * 2048);
+    };
+    // A lane's word of exponents has the quad's tiles in its four bytes.  That is how the weights' lie; of X, word t of a row holds the
+    // four blocks of tile t, of which this lane needs block o.
+    auto read_exps = [&](int q) {
+        const char* at = lds + 2 * kStep;
+        const uint32_t pick = (uint32_t)o * 0x0101u + 0x0400u;
+        const int missing = 4 * (q + 1) > p.KT ? 4 * (q + 1) - p.KT : 0;
+#pragma unroll
+        for (int r = 0; r < WN; ++r) we[r] = *reinterpret_cast<const uint32_t*>(at + (wn * WN + r) * 256 + lane * 4);
+#pragma unroll
+        for (int b = 0; b < WM; ++b) {
+            const u32x4 e = *reinterpret_cast<const u32x4*>(at + kRB * 256 + (16 * (wm * WM + b) + i) * 16);
+            const uint32_t low = __builtin_amdgcn_perm(e[1], e[0], pick), high = __builtin_amdgcn_perm(e[3], e[2], pick);
+            xe[b] = __builtin_amdgcn_perm(high, low, 0x05040100u) >> (8 * missing);
+        }
+    };
+    // The tile in the registers, half H of its step; the next one (half 1 - H, in `buffer`) is read meanwhile: of X into registers of
+    // their own, of a row block of weights when its last product has been started.  Copies of a later step are asked for one at a
+    // time between the products: together, they would keep the wavefronts from issuing anything else for a thousand cycles.
+    auto multiply = [&](auto half_of_step, int buffer, auto part) {
+        constexpr int H = decltype(half_of_step)::value;
+        read_x(buffer, 1 - H);
+#pragma unroll
+        for (int r = 0; r < WN; ++r) {
+#pragma unroll
+            for (int b = 0; b < WM; ++b) acc[r][b] = product<H, H>(w[r], x[H][b], acc[r][b], we[r], xe[b]);
+            // (without this the compiler moves products behind the branches and barriers that follow)
+#pragma unroll
+            for (int b = 0; b < WM; ++b) asm volatile("" : "+v"(acc[r][b]));
+            __builtin_amdgcn_sched_barrier(0);
+            read_w(buffer, 1 - H, r);
+            part(r);
+        }
+    };
+    // Step s; its first tile is in the registers.  LOAD: there is a step s + 2.
+    auto one_step = [&](int s, auto load) {
+        constexpr bool LOAD = decltype(load)::value;
+        const int here = s & 1;
+        multiply(integral_constant<int, 0>(), here, [](int) {});
+        arrive<0>();                                   // the next step is there, and nobody needs this one's place any more
+        __builtin_amdgcn_sched_barrier(0);
+        if (LOAD && here == 0) load_exps(s / 2 + 1);
+        multiply(integral_constant<int, 1>(), 1 - here, [&](int r) {
+            if constexpr (LOAD) {
+#pragma unroll
+                for (int j = r * kLoads / WN; j < (r + 1) * kLoads / WN; ++j) load_part(s + 2, here, j);
+            }
+        });
+        if (here == 0) {
+#pragma unroll
+            for (int r = 0; r < WN; ++r) we[r] >>= 16;
+#pragma unroll
+            for (int b = 0; b < WM; ++b) xe[b] >>= 16;
+        } else {
+            read_exps(s / 2 + 1);
+        }
+    };
+    const int steps = (p.KT + 1) / 2;
+    load_exps(0);
+    load_step(0, 0);
+    load_step(1, 1);
+    arrive<2 * kWLoads + kXLoads>();
+    read_exps(0);
+    read_x(0, 0);
+#pragma unroll
+    for (int r = 0; r < WN; ++r) read_w(0, 0, r);
+    int s = 0;
+    for (; s < steps - 2; ++s) one_step(s, std::true_type());
+    for (; s < steps; ++s) one_step(s, std::false_type());
+
+    // The lanes of a row of X hold four neighbouring sums each, of either row block of a pair.  The two blocks' words are exchanged
+    // between neighbouring rows of lanes, so that every lane stores sixteen bytes: those of even o of the first block, of odd o of the second.
+    static_assert(WN % 2 == 0, "row blocks in pairs");
+#pragma unroll
+    for (int b = 0; b < WM; ++b) {
+        const int m = m0 + 16 * (wm * WM + b) + i;
+        char* y = p.y + ((int64_t)m * p.N + 16 * (rb0 + wn * WN + (o & 1)) + 8 * (o >> 1)) * 2;
+#pragma unroll
+        for (int r = 0; r < WN; r += 2) {
+            u32x4 out;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const auto two = __builtin_amdgcn_permlane16_swap(round_pair(acc[r][b][2 * h], acc[r][b][2 * h + 1], p.bf16),
+                                                                  round_pair(acc[r + 1][b][2 * h], acc[r + 1][b][2 * h + 1], p.bf16), false, false);
+                out[h] = two[0];
+                out[2 + h] = two[1];
+            }
+            if (m < m1 && rb0 + wn * WN + r + (o & 1) < p.NB) *reinterpret_cast<u32x4*>(y + r * 32) = out;
+        }
+    }
+}
+
 namespace {
 
 constexpr size_t kCounterBytes = 64 * 1024;
@@ -174,6 +374,18 @@ void launch_stream(ProductParams p, int waves, hipStream_t s) {
         const dim3 grid(nx, (unsigned)(pieces - at < most ? pieces - at : most));
         if (p.offsets) stream_kernel<SRC, R, MB, true><<<grid, waves * 64, lds, s>>>(p);
         else stream_kernel<SRC, R, MB, false><<<grid, waves * 64, lds, s>>>(p);
+    }
+}
+
+template <int WN, int WM, int GN, int GM>
+void launch_tiles(ProductParams p, hipStream_t s) {
+    const int64_t nx = (p.NB + WN * GN - 1) / (WN * GN), pieces = most_pieces(p, 16 * WM * GM);
+    const int64_t most = (int64_t(1) << 31) / (nx * GN * GM * 64);             // (a launch has fewer than 2^32 threads)
+    for (int64_t at = 0; at < pieces; at += most) {
+        p.slot0 = (int)at;
+        p.slots = (int)(pieces - at < most ? pieces - at : most);
+        if (p.offsets) tile_kernel<WN, WM, GN, GM, true><<<nx * p.slots, GN * GM * 64, 0, s>>>(p);
+        else tile_kernel<WN, WM, GN, GM, false><<<nx * p.slots, GN * GM * 64, 0, s>>>(p);
     }
 }
 
@@ -208,7 +420,8 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     if (src == kF16) launch_stream<kF16, 2, 1>(p, waves, s);
     else if (src == kBF16) launch_stream<kBF16, 2, 1>(p, waves, s);
     else if (mb == 1) launch_stream<kF32, 2, 1>(p, waves, s);
-    else launch_stream<kF32, 4, 4>(p, waves < 4 ? waves : 4, s);
+    else if (K < 512 || rows <= 128) launch_stream<kF32, 4, 4>(p, waves < 4 ? waves : 4, s);
+    else launch_tiles<8, 4, 2, 4>(p, s);
     return hipGetLastError() == hipSuccess ? LUTQ_OK : LUTQ_ERR_DEVICE;
 }
 
