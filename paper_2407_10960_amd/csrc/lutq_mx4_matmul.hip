@@ -25,52 +25,85 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t unbounded(const char* base) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (uint32_t)-1, 0x00020000);
 }
 
+// Sixteen bytes per lane that workgroups on other dies read, or wrote, in the same launch: past the caches that are a die's own.
+constexpr int kSc1 = 16;
+__device__ __forceinline__ void store16_shared(__amdgpu_buffer_rsrc_t to, uint32_t lane_at, int at, f32x4 v) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, lane_at, at, kSc1);
+}
+__device__ __forceinline__ f32x4 load16_shared(__amdgpu_buffer_rsrc_t from, uint32_t lane_at, int at) {
+    return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane_at, at, kSc1));
+}
+
 struct ProductParams {
     const char* x;             // row form: codes; or 16-bit values
     const char* xe;            // row form: exponents
     const char* w;             // records
     char* y;
     const int32_t* offsets;    // by expert: experts + 1; else null
+    uint32_t* counters;        // K in slices: how many of a tile's are done, and
+    char* partial;             // their sums
     int64_t record, expert;    // bytes of a row block's record, of an expert's weights
     int M, N, K, KT, KQ, NB;   // K tiles, quads, row blocks
     int experts;
     int slot0, slots;          // first piece of rows of this launch, and how many
+    int slices;                // of K
     int bf16;                  // type of Y
 };
 
-// Rows [first, end) of X and the expert of the `slot`-th piece of ROWS rows: pieces do not straddle experts and are numbered in order of
-// the experts.  False where there are fewer pieces.  Every lane of a wavefront looks at one expert at a time; the whole
-// wavefront gets the answer.
-template <int ROWS>
-__device__ __forceinline__ bool find_piece(const int32_t* offsets, int experts, int M, int slot, int& expert, int& first, int& end) {
-    const int lane = threadIdx.x & 63;
-    int before = 0;                                    // pieces of the experts looked at so far
-    for (int base = 0; base < experts; base += 64) {
-        const int g = base + lane;
-        int a = 0, b = 0;
+// The rows of X in pieces of at most ROWS that do not straddle experts, numbered in order of the experts.  Every lane of a wavefront looks
+// at one expert at a time; the whole wavefront gets the answers.
+template <int ROWS> struct Pieces {
+    const int32_t* offsets;
+    int experts, M;
+    int a, b, sum;             // of the lane's expert among the 64 last looked at: its rows, its pieces and those of the ones before it
+
+    __device__ __forceinline__ void look(int base) {
+        const int lane = threadIdx.x & 63, g = base + lane;
+        a = b = 0;
         if (g < experts) {
             a = min(max(offsets[g], 0), M);
             b = min(max(offsets[g + 1], 0), M);
         }
-        const int mine = b > a ? (b - a + ROWS - 1) / ROWS : 0;
-        int sum = mine;                                // inclusive prefix sum over the wavefront
+        sum = mine();
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int up = __shfl_up(sum, d);
             if (lane >= d) sum += up;
         }
-        const uint64_t past = __ballot(before + sum > slot);
-        if (past) {
-            const int at = __builtin_ctzll(past);
-            const int begin = __shfl(before + sum - mine, at);
-            expert = __builtin_amdgcn_readfirstlane(base + at);
-            first = __builtin_amdgcn_readfirstlane(__shfl(a, at) + (slot - begin) * ROWS);
-            end = __builtin_amdgcn_readfirstlane(min(__shfl(b, at), first + ROWS));
-            return true;
-        }
-        before += __builtin_amdgcn_readfirstlane(__shfl(sum, 63));
     }
-    return false;
+    __device__ __forceinline__ int mine() const { return b > a ? (b - a + ROWS - 1) / ROWS : 0; }
+    __device__ __forceinline__ int all() const { return __builtin_amdgcn_readlane(sum, 63); }
+
+    __device__ __forceinline__ int count() {
+        int n = 0;
+        for (int base = 0; base < experts; base += 64) { look(base); n += all(); }
+        return n;
+    }
+    // The expert and the rows [first, end) of piece `slot`, which has to exist.  (Up to 64 experts, count() has looked already.)
+    __device__ __forceinline__ void find(int slot, int& expert, int& first, int& end) {
+        int before = 0;
+        for (int base = 0; base < experts; base += 64) {
+            if (experts > 64) look(base);
+            if (before + all() > slot) {
+                const int at = __builtin_ctzll(__ballot(before + sum > slot));
+                const int begin = before + __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine(), at);
+                expert = base + at;
+                first = __builtin_amdgcn_readlane(a, at) + (slot - begin) * ROWS;
+                end = min(__builtin_amdgcn_readlane(b, at), first + ROWS);
+                return;
+            }
+            before += all();
+        }
+    }
+};
+
+// Quotients of scalars, which the compiler computes in vector registers and would leave there.
+__device__ __forceinline__ int quotient(int a, int b) { return __builtin_amdgcn_readfirstlane((int)((uint32_t)a / (uint32_t)b)); }
+
+// Workgroups go to the eight dies in turn: the place of workgroup `id` of `n` such that each die gets a run of consecutive places.
+__device__ __forceinline__ int by_die(int id, int n) {
+    const int per = n >> 3;
+    return id < per * 8 ? (id & 7) * per + (id >> 3) : id;
 }
 
 // Few rows: a workgroup owns R row blocks of weights and MB blocks of sixteen rows of X over all of K; its wavefronts take the
@@ -83,7 +116,11 @@ __global__ __launch_bounds__(512) void stream_kernel(const ProductParams p) {
     const int waves = blockDim.x >> 6, i = lane & 15, o = lane >> 4;
     const int slot = p.slot0 + (int)blockIdx.y;
     int expert = 0, m0 = slot * 16 * MB, m1 = min(p.M, m0 + 16 * MB);
-    if (GROUPED && !find_piece<16 * MB>(p.offsets, p.experts, p.M, slot, expert, m0, m1)) return;
+    if constexpr (GROUPED) {
+        Pieces<16 * MB> pieces{p.offsets, p.experts, p.M};
+        if (slot >= pieces.count()) return;
+        pieces.find(slot, expert, m0, m1);
+    }
     const int rb0 = (int)blockIdx.x * R;
     const char* w[R];
 #pragma unroll
@@ -160,63 +197,106 @@ __global__ __launch_bounds__(512) void stream_kernel(const ProductParams p) {
 // Waits until at most N of this wavefront's global loads are under way and all its LDS reads are done, then for the workgroup.
 template <int N> __device__ __forceinline__ void arrive() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory"); }
 
-// Many rows: a workgroup of GN x GM wavefronts owns 16 WN GN rows of weights times 16 WM GM rows of X, each wavefront WN x WM blocks of
-// sixteen by sixteen.  K goes by in steps of two tiles (256 columns), which are copied from memory into LDS without passing through
-// registers; two steps fit, so one is under way while the other is multiplied.  The operands of one tile are read from LDS while the matrix
-// instructions of the tile before run.  The exponents come the same way, a quad (two steps) at a time.  K >= 512.
+// Many rows: a workgroup of GN x GM wavefronts makes tiles of Y, 16 WN GN rows of weights times 16 WM GM rows of X, each wavefront WN x WM
+// blocks of sixteen by sixteen.  K goes by in steps of two tiles (256 columns), which are copied from memory into LDS without passing
+// through registers; there is room for DEPTH steps, so DEPTH - 1 are under way while one is multiplied.  The operands of one tile are read
+// from LDS while the matrix instructions of the tile before run.  The exponents come the same way, a quad (two steps) at a time.  K >= 512.
+//
+// There are at most as many workgroups as run at once, and each takes one tile of Y after the other.  The copies run ahead across the
+// tiles' borders: while one is finished and stored, the first steps of the next are under way.
 //
 // In LDS the weights lie as in memory, in operand order.  Of X a piece is sixteen rows of 128 bytes, whole cache lines as they are
 // read (a line asked for in halves, a step apart, was fetched twice); block b of row i lies at 16 (b ^ (i >> 1)), so that the
 // sixteen lanes that are served together hit all banks.
-template <int WN, int WM, int GN, int GM, bool GROUPED>
+//
+// Where Y has too few tiles for the device, K is cut into slices of whole quads as well.  Each slice leaves its sums in the
+// workspace, and the last workgroup of a tile to finish adds them in the order of the slices.  No workgroup waits for another: the sums are
+// stored past the caches that the dies do not share (sc1), complete before the workgroup counts itself, and read the same way.
+template <int WN, int WM, int GN, int GM, int DEPTH> struct TileShape {
+    static constexpr int kWaves = GN * GM, kThreads = 64 * kWaves;
+    static constexpr int kRB = WN * GN, kMB = WM * GM;                         // pieces of sixteen rows of either factor
+    static constexpr int kStep = (kRB + kMB) * 2048, kExps = (kRB + kMB) * 256;
+    static constexpr int kExpPlaces = DEPTH;           // (a quad may be a single step: the last of a tile of Y)
+    static constexpr int kLds = DEPTH * kStep + kExpPlaces * kExps + 16;
+    static constexpr int kSums = kWaves * WN * WM * 1024;                      // bytes of a tile's sums
+};
+
+template <int WN, int WM, int GN, int GM, int DEPTH, bool GROUPED>
 __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductParams p) {
-    constexpr int kWaves = GN * GM, kRB = WN * GN, kMB = WM * GM;              // pieces of sixteen rows of either factor
+    using std::integral_constant;
+    using Shape = TileShape<WN, WM, GN, GM, DEPTH>;
+    constexpr int kWaves = Shape::kWaves, kRB = Shape::kRB, kMB = Shape::kMB, kStep = Shape::kStep, kExps = Shape::kExps;
     constexpr int kWLoads = kRB / kWaves, kXLoads = 2 * kMB / kWaves;          // per wavefront: pieces of weights, halves of pieces of X
     constexpr int kLoads = 2 * kWLoads + kXLoads;
     constexpr int kExpPieces = (kRB + kMB) / 4, kExpLoads = (kExpPieces + kWaves - 1) / kWaves;
     static_assert(kRB % kWaves == 0 && 2 * kMB % kWaves == 0 && kRB % 4 == 0 && kMB % 4 == 0, "whole loads per wavefront");
-    constexpr int kStep = (kRB + kMB) * 2048, kExps = (kRB + kMB) * 256;
-    __shared__ __align__(1024) char lds[2 * kStep + kExps];
-    using std::integral_constant;
+    static_assert(DEPTH == 2 || DEPTH == 4, "of any DEPTH - 2 steps half at least begin a quad");
+    extern __shared__ __align__(1024) char lds[];      // DEPTH steps, then the exponents of quads, then a word
+    char* const exp_places = lds + DEPTH * kStep;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int i = lane & 15, o = lane >> 4;
 
-    // Workgroups go to the eight dies in turn: each die gets a run of consecutive tiles of Y, ordered in bands of kBand pieces of rows
-    // of X, so that what its cache holds of either factor is used several times.
-    constexpr int kBand = 4;
-    const int nx = (p.NB + kRB - 1) / kRB, per = (int)(gridDim.x >> 3);
-    int id = (int)blockIdx.x;
-    if (id < per * 8) id = (id & 7) * per + (id >> 3);
-    const int band = id / (kBand * nx), inside = id - band * kBand * nx;
-    const int high = min(kBand, p.slots - band * kBand);
-    const int nt = inside / high, slot = p.slot0 + band * kBand + (inside - nt * high);
-    int expert = 0, m0 = slot * 16 * kMB, m1 = min(p.M, m0 + 16 * kMB);
-    if (GROUPED && !find_piece<16 * kMB>(p.offsets, p.experts, p.M, slot, expert, m0, m1)) return;
-    const int rb0 = nt * kRB, rows = m1 - m0;
+    const int nx = (p.NB + kRB - 1) / kRB;
+    Pieces<16 * kMB> pieces{p.offsets, p.experts, p.M};
+    int slots = p.slots;
+    if constexpr (GROUPED) slots = min(slots, pieces.count() - p.slot0);
+    const int total = slots * nx * p.slices;           // tiles of Y, each `slices` times
 
-    // Byte offsets of this lane in what the wavefront copies.  Rows and row blocks past the end repeat the last.
-    const int last_rb = p.NB - 1 - rb0, half = p.K / 2, ebytes = p.K / 32;
-    const auto wsrc = unbounded(p.w + expert * p.expert + rb0 * p.record);
-    const auto xsrc = unbounded(p.x + (int64_t)m0 * half);
-    const auto esrc = unbounded(p.xe + (int64_t)m0 * ebytes);
+    struct Item { int expert, m0, m1, rb0, tile, slice, step, steps; };        // step .. steps - 1 of the whole of K
+    // Tiles of Y are ordered in bands of kBand pieces of rows of X, so that what a die's cache holds of either factor is used several times.
+    auto item = [&](int number) {
+        constexpr int kBand = 4;
+        Item it;
+        const int id = by_die(number, total);
+        it.tile = p.slices == 1 ? id : quotient(id, p.slices);
+        it.slice = id - it.tile * p.slices;
+        const int band = quotient(it.tile, kBand * nx), inside = it.tile - band * kBand * nx, high = min(kBand, slots - band * kBand);
+        const int nt = quotient(inside, high), slot = p.slot0 + band * kBand + (inside - nt * high);
+        it.expert = 0;
+        it.m0 = slot * 16 * kMB;
+        it.m1 = min(p.M, it.m0 + 16 * kMB);
+        if constexpr (GROUPED) pieces.find(slot, it.expert, it.m0, it.m1);
+        it.rb0 = nt * kRB;
+        it.step = 0;
+        it.steps = (p.KT + 1) / 2;
+        if (p.slices > 1) {                            // (up to 2^15 quads, and slices that the workspace holds: the product fits)
+            it.step = 2 * quotient(it.slice * p.KQ, p.slices);
+            it.steps = min(it.steps, 2 * quotient((it.slice + 1) * p.KQ, p.slices));
+        }
+        return it;
+    };
+
+    // Where the copies are: an item, its next step, the places they go to, and this lane's byte offsets in what the wavefront copies.  Rows
+    // and row blocks past the end repeat the last.
+    const int half = p.K / 2, ebytes = p.K / 32;
     const int block = (lane & 7) ^ (lane >> 4);        // of the row that this lane copies (i >> 1 of row i = 8 g + lane / 8 is 4 g + lane / 16)
+    int number = (int)blockIdx.x, step = 0, steps = 0, place = 0, exp_place = 0;
+    __amdgpu_buffer_rsrc_t wsrc, xsrc, esrc;
     uint32_t wfrom[kWLoads], xfrom[kXLoads], efrom[kExpLoads];
+    auto aim = [&](const Item& it) {
+        step = it.step;
+        steps = it.steps;
+        const int last_rb = p.NB - 1 - it.rb0, rows = it.m1 - it.m0;
+        wsrc = unbounded(p.w + it.expert * p.expert + it.rb0 * p.record);
+        xsrc = unbounded(p.x + (int64_t)it.m0 * half);
+        esrc = unbounded(p.xe + (int64_t)it.m0 * ebytes);
 #pragma unroll
-    for (int j = 0; j < kWLoads; ++j) wfrom[j] = (uint32_t)min(wave + kWaves * j, last_rb) * (uint32_t)p.record + lane * 16;
+        for (int j = 0; j < kWLoads; ++j) wfrom[j] = (uint32_t)min(wave + kWaves * j, last_rb) * (uint32_t)p.record + lane * 16;
 #pragma unroll
-    for (int j = 0; j < kXLoads; ++j) {
-        const int c = wave + kWaves * j;               // eight rows
-        xfrom[j] = (uint32_t)min(8 * c + (lane >> 3), rows - 1) * (uint32_t)half + (block ^ (4 * (c & 1))) * 16;
-    }
+        for (int j = 0; j < kXLoads; ++j) {
+            const int c = wave + kWaves * j;           // eight rows
+            xfrom[j] = (uint32_t)min(8 * c + (lane >> 3), rows - 1) * (uint32_t)half + (block ^ (4 * (c & 1))) * 16;
+        }
 #pragma unroll
-    for (int j = 0; j < kExpLoads; ++j) {
-        const int c = min(wave + kWaves * j, kExpPieces - 1);                  // (the last may be copied twice)
-        efrom[j] = c < kRB / 4 ? (uint32_t)min(4 * c + o, last_rb) * (uint32_t)p.record + (uint32_t)p.KT * 1024 + i * 16
-                               : (uint32_t)min(64 * (c - kRB / 4) + lane, rows - 1) * (uint32_t)ebytes;
-    }
+        for (int j = 0; j < kExpLoads; ++j) {
+            const int c = min(wave + kWaves * j, kExpPieces - 1);              // (the last may be copied twice)
+            efrom[j] = c < kRB / 4 ? (uint32_t)min(4 * c + o, last_rb) * (uint32_t)p.record + (uint32_t)p.KT * 1024 + i * 16
+                                   : (uint32_t)min(64 * (c - kRB / 4) + lane, rows - 1) * (uint32_t)ebytes;
+        }
+    };
     // Copy `j` of this wavefront's kLoads of a step.
-    auto load_part = [&](int step, int buffer, int j) {
-        char* to = lds + buffer * kStep;
+    auto load_part = [&](int j) {
+        char* to = lds + place * kStep;
         // An odd last step has one tile: the second is the first again, so that nothing behind the rows is touched, and
         // has exponents of zero on both sides, 2^-254 for their products, which adds nothing to an fp32 sum.
         const bool whole = 2 * step + 1 < p.KT;
@@ -229,38 +309,46 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             copy16(xsrc, from, step * 128, to + kRB * 2048 + c * 1024);
         }
     };
-    auto load_step = [&](int step, int buffer) {
-#pragma unroll
-        for (int j = 0; j < kLoads; ++j) load_part(step, buffer, j);
-    };
-    // Exponents of a quad: of a row block of weights its 256 bytes, of a row of X its sixteen.  The row's last quad may be short: the
-    // sixteen bytes that end with the row are taken then, so that no byte behind X is touched.
-    auto load_exps = [&](int q) {
-        char* to = lds + 2 * kStep;
+    // Exponents of the quad that begins with this step: of a row block of weights its 256 bytes, of a row of X its sixteen.  The row's last
+    // quad may be short: the sixteen bytes that end with the row are taken then, so that no byte behind X is touched.
+    auto load_exps = [&]() {
+        if (step & 1) return;
+        char* to = exp_places + exp_place * kExps;
+        exp_place = exp_place == Shape::kExpPlaces - 1 ? 0 : exp_place + 1;
 #pragma unroll
         for (int j = 0; j < kExpLoads; ++j) {
             const int c = min(wave + kWaves * j, kExpPieces - 1);
-            if (c < kRB / 4) copy16(wsrc, efrom[j], q * 256, to + c * 1024);
-            else copy16(esrc, efrom[j], min(q * 16, ebytes - 16), to + c * 1024);
+            if (c < kRB / 4) copy16(wsrc, efrom[j], step * 128, to + c * 1024);
+            else copy16(esrc, efrom[j], min(step * 8, ebytes - 16), to + c * 1024);
         }
+    };
+    bool more = number < total;                        // there is something left to copy
+    auto next = [&]() {
+        place = (place + 1) % DEPTH;
+        if (++step < steps) return;
+        number += (int)gridDim.x;
+        more = number < total;
+        if (more) aim(item(number));
     };
 
     const int wn = wave % GN, wm = wave / GN;
     u32x4 w[WN], x[2][WM];
     uint32_t we[WN], xe[WM];
-    f32x4 acc[WN][WM] = {};
+    f32x4 acc[WN][WM];
+    int here = 0, exps_here = 0;                       // the places of the step and of the quad being multiplied
     const char* const wplace = lds + lane * 16 + wn * WN * 2048;
     const char* const xplace = lds + kRB * 2048 + i * 128 + wm * WM * 2048;
     const int xblock[2] = {(o ^ (i >> 1)) * 16, ((4 + o) ^ (i >> 1)) * 16};
-    auto read_w = [&](int buffer, int h, int r) { w[r] = *reinterpret_cast<const u32x4*>(wplace + buffer * kStep + h * 1024 + r * 2048); };
-    auto read_x = [&](int buffer, int h) {
+    auto read_w = [&](int from, int h, int r) { w[r] = *reinterpret_cast<const u32x4*>(wplace + from * kStep + h * 1024 + r * 2048); };
+    auto read_x = [&](int from, int h) {
 #pragma unroll
-        for (int b = 0; b < WM; ++b) x[h][b] = *reinterpret_cast<const u32x4*>(xplace + xblock[h] + buffer * kStep + b * 2048);
+        for (int b = 0; b < WM; ++b) x[h][b] = *reinterpret_cast<const u32x4*>(xplace + xblock[h] + from * kStep + b * 2048);
     };
     // A lane's word of exponents has the quad's tiles in its four bytes.  That is how the weights' lie; of X, word t of a row holds the
     // four blocks of tile t, of which this lane needs block o.
     auto read_exps = [&](int q) {
-        const char* at = lds + 2 * kStep;
+        const char* at = exp_places + exps_here * kExps;
+        exps_here = exps_here == Shape::kExpPlaces - 1 ? 0 : exps_here + 1;
         const uint32_t pick = (uint32_t)o * 0x0101u + 0x0400u;
         const int missing = 4 * (q + 1) > p.KT ? 4 * (q + 1) - p.KT : 0;
 #pragma unroll
@@ -272,85 +360,151 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             xe[b] = __builtin_amdgcn_perm(high, low, 0x05040100u) >> (8 * missing);
         }
     };
-    // The tile in the registers, half H of its step; the next one (half 1 - H, in `buffer`) is read meanwhile: of X into registers of
+    // The tile in the registers, half H of its step; the next one (half 1 - H, at `from`) is read meanwhile: of X into registers of
     // their own, of a row block of weights when its last product has been started.  Copies of a later step are asked for one at a
     // time between the products: together, they would keep the wavefronts from issuing anything else for a thousand cycles.
-    auto multiply = [&](auto half_of_step, int buffer, auto part) {
+    auto multiply = [&](auto half_of_step, int from, auto before_reads, auto part) {
         constexpr int H = decltype(half_of_step)::value;
-        read_x(buffer, 1 - H);
 #pragma unroll
         for (int r = 0; r < WN; ++r) {
 #pragma unroll
             for (int b = 0; b < WM; ++b) acc[r][b] = product<H, H>(w[r], x[H][b], acc[r][b], we[r], xe[b]);
-            // (without this the compiler moves products behind the branches and barriers that follow)
-#pragma unroll
-            for (int b = 0; b < WM; ++b) asm volatile("" : "+v"(acc[r][b]));
             __builtin_amdgcn_sched_barrier(0);
-            read_w(buffer, 1 - H, r);
+            if (r == 0) {
+                before_reads();
+                read_x(from, 1 - H);
+            }
+            read_w(from, 1 - H, r);
             part(r);
         }
+        // (without this the compiler moves products behind the branches and barriers that follow)
+#pragma unroll
+        for (int r = 0; r < WN; ++r)
+#pragma unroll
+            for (int b = 0; b < WM; ++b) asm volatile("" : "+v"(acc[r][b]));
     };
-    // Step s; its first tile is in the registers.  LOAD: there is a step s + 2.
-    auto one_step = [&](int s, auto load) {
+    // Step s of `it`; its first tile is in the registers.  LOAD: there is something left to copy.
+    auto one_step = [&](int s, const Item& it, int first_quad, auto load) {
         constexpr bool LOAD = decltype(load)::value;
-        const int here = s & 1;
-        multiply(integral_constant<int, 0>(), here, [](int) {});
-        arrive<0>();                                   // the next step is there, and nobody needs this one's place any more
-        __builtin_amdgcn_sched_barrier(0);
-        if (LOAD && here == 0) load_exps(s / 2 + 1);
-        multiply(integral_constant<int, 1>(), 1 - here, [&](int r) {
+        multiply(integral_constant<int, 0>(), here, []() {}, [](int) {});
+        here = (here + 1) % DEPTH;
+        multiply(integral_constant<int, 1>(), here, [&]() {
+            // The next step is there, and nobody needs this one's place any more.  (Here and not before the first products, when the
+            // operands read last may still be on their way.)
+            if constexpr (LOAD) arrive<(DEPTH - 2) * kLoads + (DEPTH - 2) / 2 * kExpLoads>();
+            else if (DEPTH > 2 && s + 3 == it.steps) arrive<kLoads>();
+            else if (DEPTH > 2 && s + 3 < it.steps) arrive<2 * kLoads>();
+            else arrive<0>();
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (LOAD) load_exps();
+        }, [&](int r) {
             if constexpr (LOAD) {
 #pragma unroll
-                for (int j = r * kLoads / WN; j < (r + 1) * kLoads / WN; ++j) load_part(s + 2, here, j);
+                for (int j = r * kLoads / WN; j < (r + 1) * kLoads / WN; ++j) load_part(j);
             }
         });
-        if (here == 0) {
+        if constexpr (LOAD) next();
+        if (s + 1 == it.steps || (s & 1)) {
+            read_exps(s + 1 == it.steps ? first_quad : s / 2 + 1);
+        } else {
 #pragma unroll
             for (int r = 0; r < WN; ++r) we[r] >>= 16;
 #pragma unroll
             for (int b = 0; b < WM; ++b) xe[b] >>= 16;
-        } else {
-            read_exps(s / 2 + 1);
         }
     };
-    const int steps = (p.KT + 1) / 2;
-    load_exps(0);
-    load_step(0, 0);
-    load_step(1, 1);
-    arrive<2 * kWLoads + kXLoads>();
-    read_exps(0);
+
+    if (!more) return;
+    Item it = item(number);
+    aim(it);
+#pragma unroll
+    for (int t = 0; t < DEPTH; ++t) {
+        if (!more) break;
+        load_exps();
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) load_part(j);
+        next();
+    }
+    if (it.step + DEPTH <= it.steps) arrive<(DEPTH - 1) * kLoads + (DEPTH / 2 - 1) * kExpLoads>();
+    else arrive<0>();
+    read_exps(it.step / 2);
     read_x(0, 0);
 #pragma unroll
     for (int r = 0; r < WN; ++r) read_w(0, 0, r);
-    int s = 0;
-    for (; s < steps - 2; ++s) one_step(s, std::true_type());
-    for (; s < steps; ++s) one_step(s, std::false_type());
 
-    // The lanes of a row of X hold four neighbouring sums each, of either row block of a pair.  The two blocks' words are exchanged
-    // between neighbouring rows of lanes, so that every lane stores sixteen bytes: those of even o of the first block, of odd o of the second.
-    static_assert(WN % 2 == 0, "row blocks in pairs");
+    for (int mine = (int)blockIdx.x;;) {
 #pragma unroll
-    for (int b = 0; b < WM; ++b) {
-        const int m = m0 + 16 * (wm * WM + b) + i;
-        char* y = p.y + ((int64_t)m * p.N + 16 * (rb0 + wn * WN + (o & 1)) + 8 * (o >> 1)) * 2;
+        for (int r = 0; r < WN; ++r)
 #pragma unroll
-        for (int r = 0; r < WN; r += 2) {
-            u32x4 out;
+            for (int b = 0; b < WM; ++b) acc[r][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        mine += (int)gridDim.x;
+        const Item after = mine < total ? item(mine) : it;
+        int s = it.step;
+        for (; s < it.steps && more; ++s) one_step(s, it, after.step / 2, std::true_type());
+        for (; s < it.steps; ++s) one_step(s, it, after.step / 2, std::false_type());
+
+        bool finished = true;
+        if (p.slices > 1) {                            // the other slices of this tile
+            const auto sums = unbounded(p.partial + ((int64_t)it.tile * p.slices) * Shape::kSums);
+            const uint32_t at = wave * (WN * WM * 1024) + lane * 16;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const auto two = __builtin_amdgcn_permlane16_swap(round_pair(acc[r][b][2 * h], acc[r][b][2 * h + 1], p.bf16),
-                                                                  round_pair(acc[r + 1][b][2 * h], acc[r + 1][b][2 * h + 1], p.bf16), false, false);
-                out[h] = two[0];
-                out[2 + h] = two[1];
+            for (int r = 0; r < WN; ++r)
+#pragma unroll
+                for (int b = 0; b < WM; ++b) store16_shared(sums, at + (r * WM + b) * 1024, it.slice * Shape::kSums, acc[r][b]);
+            arrive<0>();
+            uint32_t* last = reinterpret_cast<uint32_t*>(lds + Shape::kLds - 16);
+            if (threadIdx.x == 0) {
+                uint32_t* count = p.counters + it.tile;
+                const uint32_t n = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                *last = n + 1 == (uint32_t)p.slices;
+                if (*last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             }
-            if (m < m1 && rb0 + wn * WN + r + (o & 1) < p.NB) *reinterpret_cast<u32x4*>(y + r * 32) = out;
+            __syncthreads();
+            finished = __builtin_amdgcn_readfirstlane(*last);
+            __syncthreads();                           // (the word is free for the next item)
+            if (finished) {
+#pragma unroll
+                for (int r = 0; r < WN; ++r)
+#pragma unroll
+                    for (int b = 0; b < WM; ++b) {
+                        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+                        for (int z = 0; z < p.slices; ++z) sum += load16_shared(sums, at + (r * WM + b) * 1024, z * Shape::kSums);
+                        acc[r][b] = sum;
+                    }
+            }
         }
+        // The lanes of a row of X hold four neighbouring sums each, of either row block of a pair.  The two blocks' words are exchanged between
+        // neighbouring rows of lanes, so that every lane stores sixteen bytes: those of even o of the first block, of odd o of the second.
+        static_assert(WN % 2 == 0, "row blocks in pairs");
+        if (finished) {
+#pragma unroll
+            for (int b = 0; b < WM; ++b) {
+                const int m = it.m0 + 16 * (wm * WM + b) + i;
+                char* y = p.y + ((int64_t)m * p.N + 16 * (it.rb0 + wn * WN + (o & 1)) + 8 * (o >> 1)) * 2;
+#pragma unroll
+                for (int r = 0; r < WN; r += 2) {
+                    u32x4 out;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const auto two = __builtin_amdgcn_permlane16_swap(round_pair(acc[r][b][2 * h], acc[r][b][2 * h + 1], p.bf16),
+                                                                          round_pair(acc[r + 1][b][2 * h], acc[r + 1][b][2 * h + 1], p.bf16), false, false);
+                        out[h] = two[0];
+                        out[2 + h] = two[1];
+                    }
+                    if (m < it.m1 && it.rb0 + wn * WN + r + (o & 1) < p.NB) *reinterpret_cast<u32x4*>(y + r * 32) = out;
+                }
+            }
+        }
+        if (mine >= total) break;
+        it = after;
     }
 }
 
 namespace {
 
 constexpr size_t kCounterBytes = 64 * 1024;
+constexpr int64_t kCounters = kCounterBytes / 4;
+constexpr size_t kPartialBytes = 32 * 1024 * 1024;
 
 bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -377,16 +531,72 @@ void launch_stream(ProductParams p, int waves, hipStream_t s) {
     }
 }
 
-template <int WN, int WM, int GN, int GM>
-void launch_tiles(ProductParams p, hipStream_t s) {
-    const int64_t nx = (p.NB + WN * GN - 1) / (WN * GN), pieces = most_pieces(p, 16 * WM * GM);
-    const int64_t most = (int64_t(1) << 31) / (nx * GN * GM * 64);             // (a launch has fewer than 2^32 threads)
-    for (int64_t at = 0; at < pieces; at += most) {
+// The kernel with `lds` bytes of LDS, which may be more than a launch gets unasked.
+template <typename K> hipError_t launch(K kernel, dim3 grid, int threads, int lds, const ProductParams& p, hipStream_t s) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    kernel<<<grid, threads, lds, s>>>(p);
+    return hipGetLastError();
+}
+
+template <int WN, int WM, int GN, int GM, int DEPTH>
+hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
+    using Shape = TileShape<WN, WM, GN, GM, DEPTH>;
+    constexpr int kAtOnce = 160 * 1024 / Shape::kLds < 8 / Shape::kWaves ? 160 * 1024 / Shape::kLds : 8 / Shape::kWaves;   // per compute unit
+    const int64_t nx = (p.NB + Shape::kRB - 1) / Shape::kRB, pieces = most_pieces(p, 16 * Shape::kMB);
+    // slices that the workspace has room for, of a quad at least
+    slices = slices < p.KQ ? slices : p.KQ;
+    while (slices > 1 && (nx * pieces > kCounters || nx * pieces * slices * Shape::kSums > (int64_t)kPartialBytes)) --slices;
+    p.slices = slices;
+    const int64_t most = (int64_t(1) << 30) / (nx * slices);                   // pieces of rows per launch: tiles are counted in 32 bits
+    hipError_t e = hipSuccess;
+    for (int64_t at = 0; at < pieces && e == hipSuccess; at += most) {
         p.slot0 = (int)at;
         p.slots = (int)(pieces - at < most ? pieces - at : most);
-        if (p.offsets) tile_kernel<WN, WM, GN, GM, true><<<nx * p.slots, GN * GM * 64, 0, s>>>(p);
-        else tile_kernel<WN, WM, GN, GM, false><<<nx * p.slots, GN * GM * 64, 0, s>>>(p);
+        const int64_t items = nx * p.slots * slices, grid = items < (int64_t)cus * kAtOnce ? items : (int64_t)cus * kAtOnce;
+        e = p.offsets ? launch(tile_kernel<WN, WM, GN, GM, DEPTH, true>, dim3((unsigned)grid), Shape::kThreads, Shape::kLds, p, s)
+                      : launch(tile_kernel<WN, WM, GN, GM, DEPTH, false>, dim3((unsigned)grid), Shape::kThreads, Shape::kLds, p, s);
     }
+    return e;
+}
+
+// Which tile shape, and for the smallest how many slices of K: the least of times estimated from the number of tiles on the busiest
+// compute unit (n) and of steps (S).  Microseconds, fitted to 90 products of 17 to 4096 rows on 1024 x 4096 to 28672 x 4096:
+//   256 x 256       3.0 + n (1.75 S + 5)                  one workgroup per compute unit; the 5 are its stores, all at once
+//   128 x 128       1.5 + 1.25 S per two, 0.95 S for one  two workgroups per unit, two steps of room each
+//   128 x 128 deep  3.2 + n (0.70 S + 1)                  one, four steps of room
+//   128 x 64 deep   3.0 + n (0.505 S + 0.4)
+//   64 x 64 deep    2.5 + 0.62 S per two, 0.39 S for one; in z slices 0.5 + 1.8 z more
+// Examples (us, shapes in this order): 512 rows, 4096 x 4096 28.7, 14.7, 14.9, 11.5, 11.6; 8192 rows, 8192 x 8192 258, 318, 390, 543, 569;
+// 200 rows, 28672 x 4096 35, 26.2, 28.9, 38, 33.6; 64 rows, 4096 x 14336 85, 53, 41, 32.6, 24.6, in four slices 16.0.
+// By expert the number of tiles is not known here: every expert is taken to have the mean number of rows and half a tile that is not full.
+struct TileChoice { int shape, slices; };
+
+TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int cus) {
+    const double S = (double)((KT + 1) / 2);
+    const int64_t KQ = (KT + 3) / 4;
+    TileChoice best{0, 1};
+    double least = 1e300;
+    auto tiles = [&](int64_t rb, int64_t rows) {
+        const int64_t nx = (NB + rb - 1) / rb;
+        if (!experts) return (double)nx * (double)((M + rows - 1) / rows);
+        const double some = (double)(M < experts ? M : experts), filled = (double)M / (double)rows + 0.5 * some;
+        return (double)nx * (filled > some ? filled : some);
+    };
+    auto consider = [&](int shape, int slices, double us) {
+        if (us < least) { least = us; best = {shape, slices}; }
+    };
+    auto rounds = [&](double t) { return (double)(int64_t)((t + cus - 1) / cus); };
+    auto pairs = [&](double n, double one, double two) { return two * (double)(int64_t)(n / 2) + ((int64_t)n % 2 ? one : 0.0); };
+    const double t0 = tiles(16, 256), t1 = tiles(8, 128), t3 = tiles(8, 64), t4 = tiles(4, 64);
+    const double n0 = rounds(t0), n1 = rounds(t1), n3 = rounds(t3);
+    consider(0, 1, 3.0 + n0 * (1.75 * S + 5.0 * (t0 < cus ? t0 / cus : 1.0)));
+    consider(1, 1, 1.5 + pairs(n1, 0.95, 1.25) * S + 1.3 * n1);
+    consider(2, 1, 3.2 + n1 * (0.70 * S + 1.0));
+    consider(3, 1, 3.0 + n3 * (0.505 * S + 0.4));
+    for (int z = 1; z <= 8 && (z == 1 || (!experts && z <= KQ && t4 * z <= 2.0 * cus)); ++z)
+        consider(4, z, 2.5 + pairs(rounds(t4 * z), 0.39, 0.62) * (double)((int64_t)(S + z - 1) / z) + (z > 1 ? 0.5 + 1.8 * z : 0.0));
+    return best;
 }
 
 lutq_status product_on(const void* X, const void* xe, const void* packed, const int32_t* offsets, int64_t experts, int64_t M,
@@ -406,10 +616,12 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     p.record = record_bytes(K); p.expert = N / 16 * p.record;
     p.M = (int)M; p.N = (int)N; p.K = (int)K; p.KT = (int)k_tiles(K); p.KQ = (int)k_quads(K); p.NB = (int)(N / 16);
     p.bf16 = dtype == LUTQ_BF16;
+    p.counters = static_cast<uint32_t*>(workspace);
+    p.partial = static_cast<char*>(workspace) + kCounterBytes;
     int src = xe ? kF32 : dtype == LUTQ_F16 ? kF16 : kBF16;
     const int64_t rows = M / experts;                  // rows an expert has on average
     if (src != kF32 && rows > 16) {
-        char *codes = static_cast<char*>(workspace) + kCounterBytes, *exponents = codes + up256((size_t)M * (K / 2));
+        char *codes = p.partial + kPartialBytes, *exponents = codes + up256((size_t)M * (K / 2));
         const lutq_status st = quantize_rows_on(X, src, M, nullptr, M, K, codes, exponents, s);
         if (st != LUTQ_OK) return st;
         p.x = codes; p.xe = exponents;
@@ -420,8 +632,18 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     if (src == kF16) launch_stream<kF16, 2, 1>(p, waves, s);
     else if (src == kBF16) launch_stream<kBF16, 2, 1>(p, waves, s);
     else if (mb == 1) launch_stream<kF32, 2, 1>(p, waves, s);
-    else if (K < 512 || rows <= 128) launch_stream<kF32, 4, 4>(p, waves < 4 ? waves : 4, s);
-    else launch_tiles<8, 4, 2, 4>(p, s);
+    else if (K < 512) launch_stream<kF32, 4, 4>(p, waves < 4 ? waves : 4, s);
+    else {
+        const int cus = compute_units();
+        if (cus < 1) return LUTQ_ERR_DEVICE;
+        const TileChoice c = choose_tiles(M, p.NB, p.KT, offsets ? experts : 0, cus);
+        const hipError_t e = c.shape == 0   ? launch_tiles<8, 4, 2, 4, 2>(p, 1, cus, s)
+                             : c.shape == 1 ? launch_tiles<4, 4, 2, 2, 2>(p, 1, cus, s)
+                             : c.shape == 2 ? launch_tiles<4, 4, 2, 2, 4>(p, 1, cus, s)
+                             : c.shape == 3 ? launch_tiles<4, 2, 2, 2, 4>(p, 1, cus, s)
+                                            : launch_tiles<2, 2, 2, 2, 4>(p, c.slices, cus, s);
+        return e == hipSuccess ? LUTQ_OK : LUTQ_ERR_DEVICE;
+    }
     return hipGetLastError() == hipSuccess ? LUTQ_OK : LUTQ_ERR_DEVICE;
 }
 
@@ -434,7 +656,7 @@ using namespace lutq::mx4;
 
 extern "C" size_t lutq_mx4_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t experts) {
     if (!shape_ok(N, K) || !rows_ok(M, K) || experts < 1 || experts > 65536) return 0;
-    return kCounterBytes + up256((size_t)M * (size_t)(K / 2)) + up256((size_t)M * (size_t)(K / 32));
+    return kCounterBytes + kPartialBytes + up256((size_t)M * (size_t)(K / 2)) + up256((size_t)M * (size_t)(K / 32));
 }
 
 extern "C" lutq_status lutq_mx4_matmul(const void* X, const void* x_exponents, const void* packed, int64_t M, int64_t N, int64_t K,
