@@ -228,6 +228,9 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
     constexpr int kWaves = Shape::kWaves, kRB = Shape::kRB, kMB = Shape::kMB, kStep = Shape::kStep, kExps = Shape::kExps;
     constexpr int kWLoads = kRB / kWaves, kXLoads = 2 * kMB / kWaves;          // per wavefront: pieces of weights, halves of pieces of X
     constexpr int kLoads = 2 * kWLoads + kXLoads;
+    // Of a step's copies, those that are asked for in the second half of a step; the others follow in the first half of the next, where
+    // the steps are long or many enough for them to arrive in time.
+    constexpr int kEarly = DEPTH > 2 || kWaves > 4 ? (2 * kLoads + 2) / 3 : kLoads;
     constexpr int kExpPieces = (kRB + kMB) / 4, kExpLoads = (kExpPieces + kWaves - 1) / kWaves;
     static_assert(kRB % kWaves == 0 && 2 * kMB % kWaves == 0 && kRB % 4 == 0 && kMB % 4 == 0, "whole loads per wavefront");
     static_assert(DEPTH == 2 || DEPTH == 4, "of any DEPTH - 2 steps half at least begin a quad");
@@ -322,13 +325,15 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             else copy16(esrc, efrom[j], min(step * 8, ebytes - 16), to + c * 1024);
         }
     };
-    bool more = number < total;                        // there is something left to copy
     auto next = [&]() {
         place = (place + 1) % DEPTH;
         if (++step < steps) return;
-        number += (int)gridDim.x;
-        more = number < total;
-        if (more) aim(item(number));
+        // (After the last item its last step is copied again and again, to places that nobody reads any more: as many copies are under way
+        // at every step.)
+        if (number + (int)gridDim.x < total) {
+            number += (int)gridDim.x;
+            aim(item(number));
+        } else --step;
     };
 
     const int wn = wave % GN, wm = wave / GN;
@@ -383,27 +388,27 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
 #pragma unroll
             for (int b = 0; b < WM; ++b) asm volatile("" : "+v"(acc[r][b]));
     };
-    // Step s of `it`; its first tile is in the registers.  LOAD: there is something left to copy.
-    auto one_step = [&](int s, const Item& it, int first_quad, auto load) {
-        constexpr bool LOAD = decltype(load)::value;
-        multiply(integral_constant<int, 0>(), here, []() {}, [](int) {});
+    // Step s of `it`; its first tile is in the registers.
+    auto one_step = [&](int s, const Item& it, int first_quad) {
+        constexpr int kLate = WN / 2;
+        multiply(integral_constant<int, 0>(), here, []() {}, [&](int r) {
+            if (r < kLate) {
+#pragma unroll
+                for (int j = kEarly + r * (kLoads - kEarly) / kLate; j < kEarly + (r + 1) * (kLoads - kEarly) / kLate; ++j) load_part(j);
+            }
+        });
+        next();
         here = (here + 1) % DEPTH;
         multiply(integral_constant<int, 1>(), here, [&]() {
             // The next step is there, and nobody needs this one's place any more.  (Here and not before the first products, when the
             // operands read last may still be on their way.)
-            if constexpr (LOAD) arrive<(DEPTH - 2) * kLoads + (DEPTH - 2) / 2 * kExpLoads>();
-            else if (DEPTH > 2 && s + 3 == it.steps) arrive<kLoads>();
-            else if (DEPTH > 2 && s + 3 < it.steps) arrive<2 * kLoads>();
-            else arrive<0>();
+            arrive<(DEPTH - 2) * kLoads>();
             __builtin_amdgcn_sched_barrier(0);
-            if constexpr (LOAD) load_exps();
+            load_exps();
         }, [&](int r) {
-            if constexpr (LOAD) {
 #pragma unroll
-                for (int j = r * kLoads / WN; j < (r + 1) * kLoads / WN; ++j) load_part(j);
-            }
+            for (int j = r * kEarly / WN; j < (r + 1) * kEarly / WN; ++j) load_part(j);
         });
-        if constexpr (LOAD) next();
         if (s + 1 == it.steps || (s & 1)) {
             read_exps(s + 1 == it.steps ? first_quad : s / 2 + 1);
         } else {
@@ -414,19 +419,20 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         }
     };
 
-    if (!more) return;
+    // Two wavefronts share a SIMD, and the older one is served first by itself: with the younger ones preferred they drift apart, and one
+    // multiplies while the other waits for its copies to be taken (4096 rows, 28672 x 4096: 262 -> 246 us).
+    if (kWaves == 8 && wave >= 4) __builtin_amdgcn_s_setprio(1);
+    if (number >= total) return;
     Item it = item(number);
     aim(it);
 #pragma unroll
     for (int t = 0; t < DEPTH; ++t) {
-        if (!more) break;
         load_exps();
 #pragma unroll
-        for (int j = 0; j < kLoads; ++j) load_part(j);
-        next();
+        for (int j = 0; j < (t < DEPTH - 1 ? kLoads : kEarly); ++j) load_part(j);
+        if (t < DEPTH - 1) next();
     }
-    if (it.step + DEPTH <= it.steps) arrive<(DEPTH - 1) * kLoads + (DEPTH / 2 - 1) * kExpLoads>();
-    else arrive<0>();
+    arrive<(DEPTH - 2) * kLoads + kEarly>();
     read_exps(it.step / 2);
     read_x(0, 0);
 #pragma unroll
@@ -440,8 +446,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         mine += (int)gridDim.x;
         const Item after = mine < total ? item(mine) : it;
         int s = it.step;
-        for (; s < it.steps && more; ++s) one_step(s, it, after.step / 2, std::true_type());
-        for (; s < it.steps; ++s) one_step(s, it, after.step / 2, std::false_type());
+        for (; s < it.steps; ++s) one_step(s, it, after.step / 2);
 
         bool finished = true;
         if (p.slices > 1) {                            // the other slices of this tile
@@ -498,6 +503,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         if (mine >= total) break;
         it = after;
     }
+    arrive<0>();                                       // (no copy into this workgroup's LDS outlives it)
 }
 
 namespace {
