@@ -106,31 +106,41 @@ __device__ __forceinline__ int by_die(int id, int n) {
     return id < per * 8 ? (id & 7) * per + (id >> 3) : id;
 }
 
-// Few rows: a workgroup owns R row blocks of weights and MB blocks of sixteen rows of X over all of K; its wavefronts take the
-// quads in turn, and their sums are added in LDS in the order of the wavefronts.  Both factors go from memory into
-// the operand registers: the weights as they lie, X by rows (SRC 0), or 16-bit values whose blocks of 32, one per lane, are quantised there.
-template <int SRC, int R, int MB, bool GROUPED>
-__global__ __launch_bounds__(512) void stream_kernel(const ProductParams p) {
+// Few rows: a workgroup owns R row blocks of weights and sixteen rows of X over all of K; its wavefronts take the quads in turn, and
+// their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the weights, which go from memory into the operand
+// registers as they lie, all of a quad asked for before X is looked at: 28672 x 4096, 62 MB, 1 row 12.7 us (4.9 TB/s), and 13 rows 14.1; smaller
+// ones by the time that one load after another takes to arrive (2048 x 256, 1 row: 2.4 us).
+// X is read as its cache lines lie and passes through a place of the wavefront's own in LDS into the order of the operands.  (A lane per row
+// would make 64 requests of every load: 4096 x 14336, 13 rows of codes 14.5 us, so 9.5; of bf16, 6144 x 4096, 8 rows, 7.5 and 6.9.)
+// 16-bit values (SRC 1, 2) are quantised on the way.  ROWS 1 or 4: that many rows at a time, by the four lanes that hold a block, and the
+// codes lie in LDS; 16: the values lie there, and each lane reads its block, which is half the instructions for sixteen rows, and more for
+// four (4096 x 14336, 4 rows: 10.4 us and 11.1).  ROWS says what is likely; any number of rows is right.
+// R = 4 is for K of one quad: a wavefront has sixteen rows of its own there, and the weights are shared in the first cache.
+constexpr int kPlane = 256 + 16;                       // codes of one block of sixteen rows; the rest keeps the planes in different banks
+constexpr int kStreamPlace = 16 * kPlane + 256;        // a quad's blocks, and their exponents
+
+template <int SRC, int R, int ROWS, bool GROUPED>
+__global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const ProductParams p) {
     extern __shared__ __align__(16) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int waves = blockDim.x >> 6, i = lane & 15, o = lane >> 4;
-    const int slot = p.slot0 + (int)blockIdx.y;
-    int expert = 0, m0 = slot * 16 * MB, m1 = min(p.M, m0 + 16 * MB);
+    constexpr bool solo = R == 4;                      // every wavefront has sixteen rows of its own, and K is a quad
+    const int slot = p.slot0 + (solo ? (int)blockIdx.y * waves + wave : (int)blockIdx.y);
+    if (solo && !GROUPED && slot * 16 >= p.M) return;
+    int expert = 0, m0 = slot * 16, m1 = min(p.M, m0 + 16);
     if constexpr (GROUPED) {
-        Pieces<16 * MB> pieces{p.offsets, p.experts, p.M};
+        Pieces<16> pieces{p.offsets, p.experts, p.M};
         if (slot >= pieces.count()) return;
         pieces.find(slot, expert, m0, m1);
     }
-    const int rb0 = (int)blockIdx.x * R;
+    const int rb0 = (int)blockIdx.x * R, rows = m1 - m0;
     const char* w[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) w[r] = p.w + expert * p.expert + min(rb0 + r, p.NB - 1) * p.record;
-    int64_t row[MB];                                   // (rows past the end repeat the last: their sums are not stored)
-#pragma unroll
-    for (int b = 0; b < MB; ++b) row[b] = min(m0 + 16 * b + i, m1 - 1);
+    char *const place = smem + wave * kStreamPlace, *const exps = place + 16 * kPlane;
 
-    f32x4 acc[R][MB] = {};
-    for (int q = wave; q < p.KQ; q += waves) {
+    f32x4 acc[R] = {};
+    for (int q = solo ? 0 : wave; q < p.KQ; q += waves) {
         const int tiles = min(4, p.KT - 4 * q);
         uint32_t we[R];
         u32x4 wv[R][4];
@@ -141,56 +151,106 @@ __global__ __launch_bounds__(512) void stream_kernel(const ProductParams p) {
             for (int t = 0; t < 4; ++t)
                 wv[r][t] = *reinterpret_cast<const u32x4*>(w[r] + (int64_t)(4 * q + min(t, tiles - 1)) * 1024 + lane * 16);
         }
+        auto multiply = [&](int t, u32x4 xv, uint32_t xe) {                    // `t` is a constant where this is called
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                if (t == 0) acc[r] = product<0, 0>(wv[r][0], xv, acc[r], we[r], xe);
+                if (t == 1) acc[r] = product<1, 1>(wv[r][1], xv, acc[r], we[r], xe);
+                if (t == 2) acc[r] = product<2, 2>(wv[r][2], xv, acc[r], we[r], xe);
+                if (t == 3) acc[r] = product<3, 3>(wv[r][3], xv, acc[r], we[r], xe);
+            }
+        };
+        if constexpr (SRC != kF32 && ROWS == 16) {
+            // (rows that do not exist: the last row's values, or what lies in their places, whose sums are not stored)
+            u32x4 v[4][4];
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    if (4 * g < rows)
+                        v[t][g] = *reinterpret_cast<const u32x4*>(p.x + ((int64_t)min(m0 + 4 * g + o, m1 - 1) * p.K + q * 512 + min(t, tiles - 1) * 128 + i * 8) * 2);
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                if (t >= tiles) break;
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    if (4 * g < rows) *reinterpret_cast<u32x4*>(place + (4 * g + o) * kPlane + i * 16) = v[t][g];
+                Eight<SRC> block[4];
+                uint32_t a = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) block[j].v[0] = *reinterpret_cast<const u32x4*>(place + i * kPlane + o * 64 + j * 16);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) max_bits<SRC>(block[j / 4].v[0][j % 4], a);
+                const uint32_t e = exponent_byte<SRC>(a);                      // (255 makes the products NaN whatever the codes)
+                u32x4 xv;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xv[j] = to_codes<SRC>(block[j], power_of(e));
+                multiply(t, xv, e << (8 * t));
+            }
+            continue;
+        }
+        // Rows that do not exist stay unread, and what lies in their places is multiplied: their sums are not stored.
+        if constexpr (SRC == kF32) {                   // (sixteen lanes take a row's sixteen blocks, four lanes its four words of exponents)
+            const char* from = p.x + (int64_t)(m0 + (lane >> 4)) * (p.K / 2) + q * 256 + (lane & 15) * 16;
+            u32x4 c[4];
+            uint32_t e = 0;
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (4 * g + (lane >> 4) < rows && (lane & 15) < 4 * tiles) c[g] = *reinterpret_cast<const u32x4*>(from + (int64_t)g * 2 * p.K);
+            const bool word = (lane >> 2) < rows && (lane & 3) < tiles;
+            if (word) e = *reinterpret_cast<const uint32_t*>(p.xe + (int64_t)(m0 + (lane >> 2)) * (p.K / 32) + q * 16 + (lane & 3) * 4);
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (4 * g + (lane >> 4) < rows && (lane & 15) < 4 * tiles)
+                    *reinterpret_cast<u32x4*>(place + (lane & 15) * kPlane + (4 * g + (lane >> 4)) * 16) = c[g];
+            if (word)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) exps[k * 64 + lane] = (char)(e >> (8 * k));
+        } else {                                       // lane 16 tile + 4 block + piece
+            const bool there = o < tiles;
+            for (int first = 0; first < rows; first += ROWS) {
+                const char* from = p.x + ((int64_t)(m0 + first) * p.K + q * 512 + lane * 8) * 2;
+                Eight<SRC> v[ROWS];
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k)
+                    if (first + k < rows && there) v[k].v[0] = *reinterpret_cast<const u32x4*>(from + (int64_t)k * p.K * 2);
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    if (first + k >= rows || !there) continue;
+                    uint32_t e;
+                    const uint32_t c = quantize_eight<SRC>(v[k], e);
+                    *reinterpret_cast<uint32_t*>(place + (lane >> 2) * kPlane + (first + k) * 16 + (lane & 3) * 4) = c;
+                    if ((lane & 3) == 0) exps[((lane >> 2) & 3) * 64 + (first + k) * 4 + o] = (char)e;
+                }
+            }
+        }
+        const uint32_t xe = *reinterpret_cast<const uint32_t*>(exps + lane * 4);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             if (t >= tiles) break;
-            const int64_t block = (int64_t)(4 * q + t) * 4 + o;
-            u32x4 xv[MB];
-            uint32_t xe[MB];
-#pragma unroll
-            for (int b = 0; b < MB; ++b) {
-                if constexpr (SRC == kF32) {           // (the row form)
-                    xv[b] = *reinterpret_cast<const u32x4*>(p.x + row[b] * (p.K / 2) + block * 16);
-                    xe[b] = *reinterpret_cast<const uint8_t*>(p.xe + row[b] * (p.K / 32) + block);
-                } else {
-                    const u32x4* from = reinterpret_cast<const u32x4*>(p.x + (row[b] * p.K + block * 32) * 2);
-                    Eight<SRC> v[4];
-                    uint32_t a = 0;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j].v[0] = from[j];
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) max_bits<SRC>(v[j / 4].v[0][j % 4], a);
-                    xe[b] = exponent_byte<SRC>(a);     // (255 makes the products NaN whatever the codes)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) xv[b][j] = to_codes<SRC>(v[j], power_of(xe[b]));
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int b = 0; b < MB; ++b) {
-                    if (t == 0) acc[r][b] = product<0, 0>(wv[r][0], xv[b], acc[r][b], we[r], xe[b]);
-                    if (t == 1) acc[r][b] = product<1, 0>(wv[r][1], xv[b], acc[r][b], we[r], xe[b]);
-                    if (t == 2) acc[r][b] = product<2, 0>(wv[r][2], xv[b], acc[r][b], we[r], xe[b]);
-                    if (t == 3) acc[r][b] = product<3, 0>(wv[r][3], xv[b], acc[r][b], we[r], xe[b]);
-                }
+            multiply(t, *reinterpret_cast<const u32x4*>(place + (4 * t + o) * kPlane + i * 16), xe);
         }
     }
 
-    f32x4* sums = reinterpret_cast<f32x4*>(smem);      // [wave][row block, block of X][lane]
+    auto store = [&](int r, const f32x4& sum) {
+        if (i >= rows || rb0 + r >= p.NB) return;
+        const u32x2 out = {round_pair(sum[0], sum[1], p.bf16), round_pair(sum[2], sum[3], p.bf16)};
+        *reinterpret_cast<u32x2*>(p.y + ((int64_t)(m0 + i) * p.N + 16 * (rb0 + r) + 4 * o) * 2) = out;
+    };
+    if constexpr (solo) {
 #pragma unroll
-    for (int r = 0; r < R; ++r)
-#pragma unroll
-        for (int b = 0; b < MB; ++b) sums[(wave * R * MB + r * MB + b) * 64 + lane] = acc[r][b];
+        for (int r = 0; r < R; ++r) store(r, acc[r]);
+        return;
+    }
     __syncthreads();
-    for (int d = wave; d < R * MB; d += waves) {
-        f32x4 s = sums[d * 64 + lane];
-        for (int v = 1; v < waves; ++v) s += sums[(v * R * MB + d) * 64 + lane];
-        const int m = m0 + 16 * (d % MB) + i, rb = rb0 + d / MB;
-        if (m < m1 && rb < p.NB) {
-            const u32x2 out = {round_pair(s[0], s[1], p.bf16), round_pair(s[2], s[3], p.bf16)};
-            *reinterpret_cast<u32x2*>(p.y + ((int64_t)m * p.N + 16 * rb + 4 * o) * 2) = out;
-        }
+    f32x4* sums = reinterpret_cast<f32x4*>(smem);      // [wave][row block][lane]
+#pragma unroll
+    for (int r = 0; r < R; ++r) sums[(wave * R + r) * 64 + lane] = acc[r];
+    __syncthreads();
+    for (int r = wave; r < R; r += waves) {
+        f32x4 sum = sums[r * 64 + lane];
+        for (int v = 1; v < waves; ++v) sum += sums[(v * R + r) * 64 + lane];
+        store(r, sum);
     }
 }
 
@@ -521,19 +581,19 @@ int64_t most_pieces(const ProductParams& p, int rows) {
     return p.offsets ? p.M / rows + (p.M < p.experts ? p.M : p.experts) : (p.M + rows - 1) / rows;
 }
 
-template <int SRC, int R, int MB>
+template <int SRC, int R, int ROWS>
 void launch_stream(ProductParams p, int waves, hipStream_t s) {
     const int nx = (p.NB + R - 1) / R;
-    const size_t lds = (size_t)waves * R * MB * 1024;
+    const size_t lds = (size_t)waves * kStreamPlace;
     // (a launch has fewer than 2^16 workgroups along y and 2^32 threads)
     int64_t most = (int64_t(1) << 31) / (int64_t(nx) * waves * 64);
     most = most > 65535 ? 65535 : most;
-    const int64_t pieces = most_pieces(p, 16 * MB);
-    for (int64_t at = 0; at < pieces; at += most) {
-        p.slot0 = (int)at;
-        const dim3 grid(nx, (unsigned)(pieces - at < most ? pieces - at : most));
-        if (p.offsets) stream_kernel<SRC, R, MB, true><<<grid, waves * 64, lds, s>>>(p);
-        else stream_kernel<SRC, R, MB, false><<<grid, waves * 64, lds, s>>>(p);
+    const int64_t each = R == 4 ? waves : 1, pieces = most_pieces(p, 16), slots = (pieces + each - 1) / each;
+    for (int64_t at = 0; at < slots; at += most) {
+        p.slot0 = (int)(at * each);
+        const dim3 grid(nx, (unsigned)(slots - at < most ? slots - at : most));
+        if (p.offsets) stream_kernel<SRC, R, ROWS, true><<<grid, waves * 64, lds, s>>>(p);
+        else stream_kernel<SRC, R, ROWS, false><<<grid, waves * 64, lds, s>>>(p);
     }
 }
 
@@ -566,29 +626,33 @@ hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
     return e;
 }
 
-// Which tile shape, and for the smallest how many slices of K: the least of times estimated from the number of tiles on the busiest
-// compute unit (n) and of steps (S).  Microseconds, fitted to 90 products of 17 to 4096 rows on 1024 x 4096 to 28672 x 4096:
+// Whether the weights are streamed past sixteen rows at a time, or which tile shape, and for the smallest how many slices of K: the least
+// of times estimated from the bytes of weights over the pieces of rows (B), or from the number of tiles on the busiest compute unit (n) and of
+// steps (S).  Microseconds, fitted to 120 products of 1 to 4096 rows on 1024 x 4096 to 28672 x 4096:
+//   streamed        2.3 + B / 6.6 TB/s
 //   256 x 256       3.0 + n (1.75 S + 5)                  one workgroup per compute unit; the 5 are its stores, all at once
 //   128 x 128       1.5 + 1.25 S per two, 0.95 S for one  two workgroups per unit, two steps of room each
 //   128 x 128 deep  3.2 + n (0.70 S + 1)                  one, four steps of room
 //   128 x 64 deep   3.0 + n (0.505 S + 0.4)
 //   64 x 64 deep    2.5 + 0.62 S per two, 0.39 S for one; in z slices 0.5 + 1.8 z more
-// Examples (us, shapes in this order): 512 rows, 4096 x 4096 28.7, 14.7, 14.9, 11.5, 11.6; 8192 rows, 8192 x 8192 258, 318, 390, 543, 569;
-// 200 rows, 28672 x 4096 35, 26.2, 28.9, 38, 33.6; 64 rows, 4096 x 14336 85, 53, 41, 32.6, 24.6, in four slices 16.0.
-// By expert the number of tiles is not known here: every expert is taken to have the mean number of rows and half a tile that is not full.
-struct TileChoice { int shape, slices; };
+// Examples (us, shapes in this order): 17 rows, 6144 x 4096 6.2, and tiles at best 9.3; 28672 x 4096 21.8, and 15.5; 512 rows,
+// 4096 x 4096 -, 28.7, 14.7, 14.9, 11.5, 11.6; 8192 rows, 8192 x 8192 -, 250, 318, 378, 543, 569; 200 rows, 28672 x 4096 -, 35, 26.2, 28.9,
+// 38, 33.6; 64 rows, 4096 x 14336 -, 85, 53, 41, 32.6, 24.6, in four slices 16.0.
+// By expert the number of pieces is not known here: every expert is taken to have the mean number of rows and half a piece that is not full.
+struct TileChoice { int shape, slices; };             // shape -1: streamed
 
-TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int cus) {
+TileChoice choose_kernel(int64_t M, int64_t NB, int64_t KT, int64_t experts, int64_t record, int cus) {
     const double S = (double)((KT + 1) / 2);
     const int64_t KQ = (KT + 3) / 4;
-    TileChoice best{0, 1};
-    double least = 1e300;
+    TileChoice best{-1, 1};
     auto tiles = [&](int64_t rb, int64_t rows) {
         const int64_t nx = (NB + rb - 1) / rb;
         if (!experts) return (double)nx * (double)((M + rows - 1) / rows);
         const double some = (double)(M < experts ? M : experts), filled = (double)M / (double)rows + 0.5 * some;
         return (double)nx * (filled > some ? filled : some);
     };
+    if (M <= 16 * (experts ? experts : 1) || KT < 4) return best;              // (tiles begin with a whole quad)
+    double least = 2.3 + tiles(1, 16) * (double)record / 6.6e6;
     auto consider = [&](int shape, int slices, double us) {
         if (us < least) { least = us; best = {shape, slices}; }
     };
@@ -625,24 +689,46 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     p.counters = static_cast<uint32_t*>(workspace);
     p.partial = static_cast<char*>(workspace) + kCounterBytes;
     int src = xe ? kF32 : dtype == LUTQ_F16 ? kF16 : kBF16;
-    const int64_t rows = M / experts;                  // rows an expert has on average
-    if (src != kF32 && rows > 16) {
+    const int cus = compute_units();
+    if (cus < 1) return LUTQ_ERR_DEVICE;
+    const TileChoice c = choose_kernel(M, p.NB, p.KT, offsets ? experts : 0, p.record, cus);
+    // Where the streaming workgroups quantise X on the way in, every one of them does it for all its rows.  Beyond some hundred rows and quads
+    // per compute unit that takes longer than a launch which does it once (us, so and with that launch: 4096 x 14336, 1 row (28) 8.9 and
+    // 10.5, 4 rows (112) 10.1 and 10.7, 8 rows (224) 14.4 and 11.1; 6144 x 4096, 13 rows (104) 7.4 and 7.9; 1024 x 8192, 8 rows (128) 7.4 and 6.3).
+    // Two row blocks per workgroup halve it, and leave fewer wavefronts to hide the reads (28672 x 4096, 1 row 13.4 and 13.6, 2 rows 14.7 and
+    // 13.9 with one; 128 experts of 1536 x 4096, 64 rows, 34.4 and 35.3).  Codes alone gain by two where workgroups are many and share their
+    // weights (64 experts, 250 rows: 36.8 and 38.1; 500 rows 37.4 and 39.4) and lose with a row each (34.1 and 33.2).  A single quad of K
+    // leaves nothing to hide: 8192 rows, 8192 x 384, 71 us with four row blocks, 97 with one.
+    const int64_t pieces = offsets ? (M < experts ? M : experts) : (M + 15) / 16, groups = p.NB * pieces, mean = (M + pieces - 1) / pieces;
+    int wide = src != kF32 && (groups > 1024 || mean > 4) ? 2 : 1;             // row blocks per streaming workgroup
+    const int64_t own = (groups / wide + cus - 1) / cus * p.KQ * mean;         // quads of rows that a compute unit would quantise
+    if (src != kF32 && (c.shape >= 0 || own > 120)) {
         char *codes = p.partial + kPartialBytes, *exponents = codes + up256((size_t)M * (K / 2));
         const lutq_status st = quantize_rows_on(X, src, M, nullptr, M, K, codes, exponents, s);
         if (st != LUTQ_OK) return st;
         p.x = codes; p.xe = exponents;
         src = kF32;
+        wide = 1;
     }
-    const int mb = rows > 16 ? 4 : 1;
-    const int waves = p.KQ < 8 ? p.KQ : 8;
-    if (src == kF16) launch_stream<kF16, 2, 1>(p, waves, s);
-    else if (src == kBF16) launch_stream<kBF16, 2, 1>(p, waves, s);
-    else if (mb == 1) launch_stream<kF32, 2, 1>(p, waves, s);
-    else if (K < 512) launch_stream<kF32, 4, 4>(p, waves < 4 ? waves : 4, s);
-    else {
-        const int cus = compute_units();
-        if (cus < 1) return LUTQ_ERR_DEVICE;
-        const TileChoice c = choose_tiles(M, p.NB, p.KT, offsets ? experts : 0, cus);
+    if (src == kF32 && groups > 4096) wide = p.KQ == 1 ? 4 : mean > 1 ? 2 : 1;
+    if (c.shape < 0) {
+        // Wavefronts of a workgroup, each with a quad or two of K: sixteen with one row block, eight with two (their registers) or where they
+        // quantise and workgroups are many, four where workgroups are so many that their beginnings count (64 experts of
+        // 1536 x 4096, a row each: 37.3 us with eight, 33.2 with four; 57344 x 8192, 1 row: 44.2 with eight, 42.2 with sixteen).
+        const int most = groups > 4096 ? 4 : wide > 1 || (src != kF32 && groups > 512) ? 8 : 16;
+        const int waves = wide == 4 ? (pieces < 4 ? (int)pieces : 4) : p.KQ < most ? p.KQ : most;
+        auto by_rows = [&](auto source) {
+            constexpr int SRC = decltype(source)::value;
+            if (mean > 4) launch_stream<SRC, 2, 16>(p, waves, s);
+            else if (mean > 1) wide == 2 ? launch_stream<SRC, 2, 4>(p, waves, s) : launch_stream<SRC, 1, 4>(p, waves, s);
+            else wide == 2 ? launch_stream<SRC, 2, 1>(p, waves, s) : launch_stream<SRC, 1, 1>(p, waves, s);
+        };
+        if (src == kF16) by_rows(std::integral_constant<int, kF16>());
+        else if (src == kBF16) by_rows(std::integral_constant<int, kBF16>());
+        else if (wide == 1) launch_stream<kF32, 1, 16>(p, waves, s);
+        else if (wide == 2) launch_stream<kF32, 2, 16>(p, waves, s);
+        else launch_stream<kF32, 4, 16>(p, waves, s);
+    } else {
         const hipError_t e = c.shape == 0   ? launch_tiles<8, 4, 2, 4, 2>(p, 1, cus, s)
                              : c.shape == 1 ? launch_tiles<4, 4, 2, 2, 2>(p, 1, cus, s)
                              : c.shape == 2 ? launch_tiles<4, 4, 2, 2, 4>(p, 1, cus, s)

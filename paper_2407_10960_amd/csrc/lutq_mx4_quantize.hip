@@ -38,19 +38,6 @@ template <int SRC> __device__ __forceinline__ Eight<SRC> load_eight(const void* 
     return r;
 }
 
-// The exponent byte of the block that this lane's quad holds, and the lane's word of codes.
-template <int SRC> __device__ __forceinline__ uint32_t quantize_eight(const Eight<SRC>& x, uint32_t& e) {
-    uint32_t a = 0;
-#pragma unroll
-    for (int j = 0; j < (SRC == kF32 ? 8 : 4); ++j) max_bits<SRC>(x.v[j / 4][j % 4], a);
-    // (quad_perm 1 0 3 2 and 2 3 0 1)
-    max_bits<SRC>((uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xb1, 0xf, 0xf, true), a);
-    max_bits<SRC>((uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4e, 0xf, 0xf, true), a);
-    e = exponent_byte<SRC>(a);
-    const uint32_t c = to_codes<SRC>(x, power_of(e));
-    return e == 255u ? 0u : c;
-}
-
 // Row form: UNITS units per sixteen lanes, all loaded before the first is used.
 template <int SRC, int UNITS>
 __global__ __launch_bounds__(kThreads) void quantize_rows(const QuantizeParams p) {

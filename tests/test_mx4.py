@@ -362,6 +362,27 @@ def test_product_by_expert(lutq, name, N, K, dense, dtype):
     assert p.guards_hold() and not p.ws[:65536].any().item()
 
 
+# (few rows per expert on average, and several in one of them; few and many workgroups of the streaming kernel)
+UNEVEN = [([9] + [0] * 11, 48, 640), ([2, 0, 13, 1, 0, 0], 48, 1152), ([11] + [0] * 14 + [4], 1296, 640), ([13, 3] + [2] * 14, 1296, 512),
+          ([1, 0, 16, 0] * 6, 2768, 512), ([2, 5, 0, 16] * 16, 1040, 640), ([17, 33, 0, 5] * 16, 1040, 384)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dense", [False, True])
+@pytest.mark.parametrize("case", range(len(UNEVEN)))
+def test_product_by_expert_of_uneven_rows(lutq, case, dense):
+    counts, N, K = UNEVEN[case]
+    off = counts_to_offsets(counts, 1)
+    p = Problem(lutq, int(off[-1]) + 2, N, K, "f16", experts=len(counts), seed=case)
+    x, e = p.args(dense)
+    y = p.out()
+    lutq.lutq_mx4_matmul_grouped(x, p.packed, to_gpu(off), y, p.ws, x_scales=e)
+    got, sums = as_f64(y), grouped_reference(p, off)
+    worst = np.max(np.abs(got - sums[0]) / off_by_at_most(got, sums, K, "f16"))
+    assert worst <= 1.0, worst
+    assert p.guards_hold()
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("rows", [6, 600])
 def test_offsets_outside_their_documented_range_stay_in_bounds(lutq, rows):
