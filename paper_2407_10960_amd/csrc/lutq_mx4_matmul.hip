@@ -278,6 +278,7 @@ template <int WN, int WM, int GN, int GM, int DEPTH> struct TileShape {
     static constexpr int kStep = (kRB + kMB) * 2048, kExps = (kRB + kMB) * 256;
     static constexpr int kExpPlaces = DEPTH;           // (a quad may be a single step: the last of a tile of Y)
     static constexpr int kLds = DEPTH * kStep + kExpPlaces * kExps + 16;
+    static constexpr bool kSlices = WN * WM <= 8;      // (the join of slices holds four times a tile's sums)
     static constexpr int kSums = kWaves * WN * WM * 1024;                      // bytes of a tile's sums
 };
 
@@ -509,7 +510,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         for (; s < it.steps; ++s) one_step(s, it, after.step / 2);
 
         bool finished = true;
-        if (p.slices > 1) {                            // the other slices of this tile
+        if (Shape::kSlices && p.slices > 1) {          // the other slices of this tile
             const auto sums = unbounded(p.partial + ((int64_t)it.tile * p.slices) * Shape::kSums);
             const uint32_t at = wave * (WN * WM * 1024) + lane * 16;
 #pragma unroll
@@ -528,14 +529,37 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             finished = __builtin_amdgcn_readfirstlane(*last);
             __syncthreads();                           // (the word is free for the next item)
             if (finished) {
+                // In the order of the slices, this one from its registers, the others two ahead.
+                f32x4 sum[WN][WM] = {}, even[WN][WM], odd[WN][WM];
+                auto ask = [&](int z, f32x4(&to)[WN][WM]) {
+                    if (z >= p.slices || z == it.slice) return;
+#pragma unroll
+                    for (int r = 0; r < WN; ++r)
+#pragma unroll
+                        for (int b = 0; b < WM; ++b) to[r][b] = load16_shared(sums, at + (r * WM + b) * 1024, z * Shape::kSums);
+                };
+                auto add = [&](const f32x4(&from)[WN][WM]) {
+#pragma unroll
+                    for (int r = 0; r < WN; ++r)
+#pragma unroll
+                        for (int b = 0; b < WM; ++b) sum[r][b] += from[r][b];
+                };
+                auto take = [&](int z, f32x4(&from)[WN][WM]) {
+                    if (z >= p.slices) return;
+                    if (z == it.slice) add(acc);
+                    else add(from);
+                    ask(z + 2, from);
+                };
+                ask(0, even);
+                ask(1, odd);
+                for (int z = 0; z < p.slices; z += 2) {
+                    take(z, even);
+                    take(z + 1, odd);
+                }
 #pragma unroll
                 for (int r = 0; r < WN; ++r)
 #pragma unroll
-                    for (int b = 0; b < WM; ++b) {
-                        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-                        for (int z = 0; z < p.slices; ++z) sum += load16_shared(sums, at + (r * WM + b) * 1024, z * Shape::kSums);
-                        acc[r][b] = sum;
-                    }
+                    for (int b = 0; b < WM; ++b) acc[r][b] = sum[r][b];
             }
         }
         // The lanes of a row of X hold four neighbouring sums each, of either row block of a pair.  The two blocks' words are exchanged between
@@ -611,7 +635,7 @@ hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
     constexpr int kAtOnce = 160 * 1024 / Shape::kLds < 8 / Shape::kWaves ? 160 * 1024 / Shape::kLds : 8 / Shape::kWaves;   // per compute unit
     const int64_t nx = (p.NB + Shape::kRB - 1) / Shape::kRB, pieces = most_pieces(p, 16 * Shape::kMB);
     // slices that the workspace has room for, of a quad at least
-    slices = slices < p.KQ ? slices : p.KQ;
+    slices = !Shape::kSlices ? 1 : slices < p.KQ ? slices : p.KQ;
     while (slices > 1 && (nx * pieces > kCounters || nx * pieces * slices * Shape::kSums > (int64_t)kPartialBytes)) --slices;
     p.slices = slices;
     const int64_t most = (int64_t(1) << 30) / (nx * slices);                   // pieces of rows per launch: tiles are counted in 32 bits
@@ -626,18 +650,19 @@ hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
     return e;
 }
 
-// Whether the weights are streamed past sixteen rows at a time, or which tile shape, and for the smallest how many slices of K: the least
+// Whether the weights are streamed past sixteen rows at a time, or which tile shape, and for the smaller ones how many slices of K: the least
 // of times estimated from the bytes of weights over the pieces of rows (B), or from the number of tiles on the busiest compute unit (n) and of
 // steps (S).  Microseconds, fitted to 120 products of 1 to 4096 rows on 1024 x 4096 to 28672 x 4096:
 //   streamed        2.3 + B / 6.6 TB/s
 //   256 x 256       3.0 + n (1.75 S + 5)                  one workgroup per compute unit; the 5 are its stores, all at once
 //   128 x 128       1.5 + 1.25 S per two, 0.95 S for one  two workgroups per unit, two steps of room each
-//   128 x 128 deep  3.2 + n (0.70 S + 1)                  one, four steps of room
-//   128 x 64 deep   3.0 + n (0.505 S + 0.4)
-//   64 x 64 deep    2.5 + 0.62 S per two, 0.39 S for one; in z slices 0.5 + 1.8 z more
+//   128 x 128 deep  3.2 + n (0.72 S + 1), 0.63 S for one  one of eight wavefronts, four steps of room; in z slices of K 2.5 + 1.6 z more
+//   128 x 64 deep   3.0 + n (0.505 S + 0.4)               the same; in z slices 3 + 0.8 z more
+//   64 x 64 deep    2.5 + 0.62 S per two, 0.39 S for one  two of four wavefronts; in z slices 1.8 + z more
 // Examples (us, shapes in this order): 17 rows, 6144 x 4096 6.2, and tiles at best 9.3; 28672 x 4096 21.8, and 15.5; 512 rows,
-// 4096 x 4096 -, 28.7, 14.7, 14.9, 11.5, 11.6; 8192 rows, 8192 x 8192 -, 250, 318, 378, 543, 569; 200 rows, 28672 x 4096 -, 35, 26.2, 28.9,
-// 38, 33.6; 64 rows, 4096 x 14336 -, 85, 53, 41, 32.6, 24.6, in four slices 16.0.
+// 4096 x 4096 -, 27.6, 15.2, 14.5, 11.5, 12.7; 8192 rows, 8192 x 8192 -, 240, 318, 378, 543, 569; 200 rows, 28672 x 4096 -, 34, 27.0, 28.6,
+// 35.3, 33.3; 200 rows, 5120 x 13824 -, 84, 48, 35.4, 26.7, 30.8, and 21.9 with 128 x 128 in three slices; 64 rows, 4096 x 14336 -, 83, 52, 36,
+// 33, 24.8, and 13.8 with 64 x 64 in four.
 // By expert the number of pieces is not known here: every expert is taken to have the mean number of rows and half a piece that is not full.
 struct TileChoice { int shape, slices; };             // shape -1: streamed
 
@@ -659,13 +684,16 @@ TileChoice choose_kernel(int64_t M, int64_t NB, int64_t KT, int64_t experts, int
     auto rounds = [&](double t) { return (double)(int64_t)((t + cus - 1) / cus); };
     auto pairs = [&](double n, double one, double two) { return two * (double)(int64_t)(n / 2) + ((int64_t)n % 2 ? one : 0.0); };
     const double t0 = tiles(16, 256), t1 = tiles(8, 128), t3 = tiles(8, 64), t4 = tiles(4, 64);
-    const double n0 = rounds(t0), n1 = rounds(t1), n3 = rounds(t3);
+    const double n0 = rounds(t0), n1 = rounds(t1);
     consider(0, 1, 3.0 + n0 * (1.75 * S + 5.0 * (t0 < cus ? t0 / cus : 1.0)));
     consider(1, 1, 1.5 + pairs(n1, 0.95, 1.25) * S + 1.3 * n1);
-    consider(2, 1, 3.2 + n1 * (0.70 * S + 1.0));
-    consider(3, 1, 3.0 + n3 * (0.505 * S + 0.4));
-    for (int z = 1; z <= 8 && (z == 1 || (!experts && z <= KQ && t4 * z <= 2.0 * cus)); ++z)
-        consider(4, z, 2.5 + pairs(rounds(t4 * z), 0.39, 0.62) * (double)((int64_t)(S + z - 1) / z) + (z > 1 ? 0.5 + 1.8 * z : 0.0));
+    for (int z = 1; z <= 8; ++z) {
+        const double steps = (double)((int64_t)(S + z - 1) / z);
+        if (z > 1 && (experts || z > KQ)) break;
+        if (z == 1 || t1 * z <= cus) consider(2, z, 3.2 + rounds(t1 * z) * ((t1 > cus ? 0.72 : 0.63) * steps + 1.0) + (z > 1 ? 2.5 + 1.6 * z : 0.0));
+        if (z == 1 || t3 * z <= cus) consider(3, z, 3.0 + rounds(t3 * z) * (0.505 * steps + 0.4) + (z > 1 ? 3.0 + 0.8 * z : 0.0));
+        if (z == 1 || t4 * z <= 2 * cus) consider(4, z, 2.5 + pairs(rounds(t4 * z), 0.39, 0.62) * steps + (z > 1 ? 1.8 + 1.0 * z : 0.0));
+    }
     return best;
 }
 
@@ -731,8 +759,8 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     } else {
         const hipError_t e = c.shape == 0   ? launch_tiles<8, 4, 2, 4, 2>(p, 1, cus, s)
                              : c.shape == 1 ? launch_tiles<4, 4, 2, 2, 2>(p, 1, cus, s)
-                             : c.shape == 2 ? launch_tiles<4, 4, 2, 2, 4>(p, 1, cus, s)
-                             : c.shape == 3 ? launch_tiles<4, 2, 2, 2, 4>(p, 1, cus, s)
+                             : c.shape == 2 ? launch_tiles<4, 2, 2, 4, 4>(p, c.slices, cus, s)
+                             : c.shape == 3 ? launch_tiles<2, 2, 4, 2, 4>(p, c.slices, cus, s)
                                             : launch_tiles<2, 2, 2, 2, 4>(p, c.slices, cus, s);
         return e == hipSuccess ? LUTQ_OK : LUTQ_ERR_DEVICE;
     }

@@ -322,6 +322,39 @@ def test_product(lutq, M, N, K, dense, dtype):
     assert np.array_equal(as_f64(again), got)
 
 
+# (each shape of tiles, with ragged edges; the long ones with K in two to five slices)
+TILED = [(103, 4112, 640), (199, 4112, 2176), (999, 2064, 1152), (1001, 4112, 1152), (2100, 4112, 1152), (130, 2064, 8320), (101, 2064, 8320),
+         (601, 272, 14336), (131, 1040, 16512), (131, 2064, 14336), (67, 4112, 14336), (131, 4112, 14336), (200, 4112, 8320), (259, 4112, 14336)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("case", range(len(TILED)))
+def test_product_of_many_rows(lutq, case):
+    import torch
+    M, N, K = TILED[case]
+    dtype = DTYPES[case % 2]
+    p = Problem(lutq, M, N, K, dtype)
+    y = p.out()
+    lutq.lutq_mx4_matmul(p.codes, p.packed, y, p.ws, x_scales=p.e)
+    got, sums = as_f64(y), mx.product(p.x, p.w[0])
+    worst = np.max(np.abs(got - sums[0]) / off_by_at_most(got, sums, K, dtype))
+    assert worst <= 1.0, worst
+    assert p.guards_hold() and not p.ws[:65536].any().item()
+    # the same bits again, from values, and when replayed
+    static = torch.empty_like(y)
+    graph = torch.cuda.CUDAGraph()
+    lutq.lutq_mx4_matmul(p.X, p.packed, static, p.ws)
+    assert torch.equal(static, y)
+    with torch.cuda.graph(graph):
+        lutq.lutq_mx4_matmul(p.X, p.packed, static, p.ws)
+    for _ in range(3):
+        static.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(static, y)
+    assert not p.ws[:65536].any().item()
+
+
 def counts_to_offsets(counts, first=0):
     return np.concatenate([[first], first + np.cumsum(counts)]).astype(np.int32)
 
@@ -379,6 +412,22 @@ def test_product_by_expert_of_uneven_rows(lutq, case, dense):
     lutq.lutq_mx4_matmul_grouped(x, p.packed, to_gpu(off), y, p.ws, x_scales=e)
     got, sums = as_f64(y), grouped_reference(p, off)
     worst = np.max(np.abs(got - sums[0]) / off_by_at_most(got, sums, K, "f16"))
+    assert worst <= 1.0, worst
+    assert p.guards_hold()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dense", [False, True])
+@pytest.mark.parametrize("counts,N,K", [([0, 171, 9], 2064, 512), ([33, 0, 70, 1, 16, 0, 49, 8, 3], 2064, 2176), ([129, 255, 10, 256, 0], 4112, 512),
+                                        ([2000, 0, 17, 900, 3000, 1, 128, 129, 1925], 272, 1152), ([1111, 2, 0, 3100, 287], 2064, 640)])
+def test_product_by_expert_of_many_rows(lutq, counts, N, K, dense):
+    off = counts_to_offsets(counts, 2)
+    p = Problem(lutq, int(off[-1]) + 3, N, K, "bf16", experts=len(counts))
+    x, e = p.args(dense)
+    y = p.out()
+    lutq.lutq_mx4_matmul_grouped(x, p.packed, to_gpu(off), y, p.ws, x_scales=e)
+    got, sums = as_f64(y), grouped_reference(p, off)
+    worst = np.max(np.abs(got - sums[0]) / off_by_at_most(got, sums, K, "bf16"))
     assert worst <= 1.0, worst
     assert p.guards_hold()
 
