@@ -453,8 +453,8 @@ lutq_status lutq_mx4_matmul(const void* X, const void* x_exponents, const void* 
  *   packed    device, `experts` packed forms of [N, K] one behind the other
  *   offsets   device, experts + 1 row numbers (int32), not decreasing, within 0 .. M: read on the device, so the sizes may
  *             come from a kernel before it on the stream, and a captured call follows them.  (Values outside are taken as the
- *             nearest inside, an expert whose end is before its start has no rows, and rows that several experts claim
- *             hold either's result.)
+ *             nearest inside, an expert whose end is before its start has no rows, and each value in rows that
+ *             several experts claim is one of theirs, or stays.)
  *   Y         [M, N]; rows before offsets[0] and from offsets[experts] on stay as they were
  *   workspace >= lutq_mx4_workspace_bytes(M, N, K, experts)
  * 1 <= experts <= 65536.  Everything else as for lutq_mx4_matmul. */

@@ -55,6 +55,9 @@ struct ProductParams {
 template <int ROWS> struct Pieces {
     const int32_t* offsets;
     int experts, M;
+    // More pieces than there can be, unless experts claim the same rows: sums stop there, so that none wraps around, and what comes behind
+    // is left out.
+    static constexpr int kMost = 1 << 29;
     int a, b, sum;             // of the lane's expert among the 64 last looked at: its rows, its pieces and those of the ones before it
 
     __device__ __forceinline__ void look(int base) {
@@ -68,7 +71,7 @@ template <int ROWS> struct Pieces {
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
             const int up = __shfl_up(sum, d);
-            if (lane >= d) sum += up;
+            if (lane >= d) sum = min(sum + up, kMost);
         }
     }
     __device__ __forceinline__ int mine() const { return b > a ? (b - a + ROWS - 1) / ROWS : 0; }
@@ -76,7 +79,7 @@ template <int ROWS> struct Pieces {
 
     __device__ __forceinline__ int count() {
         int n = 0;
-        for (int base = 0; base < experts; base += 64) { look(base); n += all(); }
+        for (int base = 0; base < experts; base += 64) { look(base); n = min(n + all(), kMost); }
         return n;
     }
     // The expert and the rows [first, end) of piece `slot`, which has to exist.  (Up to 64 experts, count() has looked already.)
@@ -92,7 +95,7 @@ template <int ROWS> struct Pieces {
                 end = min(__builtin_amdgcn_readlane(b, at), first + ROWS);
                 return;
             }
-            before += all();
+            before = min(before + all(), kMost);
         }
     }
 };

@@ -470,6 +470,48 @@ def test_not_a_number_stays_in_its_row(lutq, M, dense):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dense", [False, True])
+@pytest.mark.parametrize("M,N,K", [(103, 4112, 640), (199, 4112, 2176), (999, 2064, 1152), (1001, 4112, 1152), (2100, 4112, 1152), (101, 2064, 8320)])
+def test_not_a_number_among_many_rows(lutq, M, N, K, dense):
+    import torch
+    p = Problem(lutq, M, N, K, "bf16")
+    rows, columns = [0, M // 2, M - 1], [5, N - 16]
+    X, e, packed = p.X.clone(), p.e.clone(), p.packed.clone()
+    record = lutq.lutq_mx4_packed_bytes(16, K)
+    for r, k in zip(rows, (0, K // 2 + 7, K - 1)):
+        X[r, k] = float("nan")
+        e[r, k // 32] = 255
+    for n, o in zip(columns, (0, 3)):                                   # (a block of the first tile)
+        packed[0, n // 16 * record + K // 128 * 1024 + 4 * (16 * o + n % 16)] = 255
+    y = p.out()
+    lutq.lutq_mx4_matmul(X if dense else p.codes, packed, y, p.ws, x_scales=None if dense else e)
+    want = torch.zeros((M, N), dtype=torch.bool)
+    want[rows], want[:, columns] = True, True
+    assert torch.equal(torch.isnan(y).cpu(), want) and p.guards_hold()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,K", [(4112, 512), (48, 640)])
+def test_offsets_that_claim_rows_twice(lutq, N, K):
+    """Decreasing offsets and such that several experts claim the same rows: each value there is one claimant's (column tiles
+    are written by different workgroups, so a row may hold several's), and nothing outside is written."""
+    p = Problem(lutq, 650, N, K, "bf16", experts=5)
+    all_sums = [mx.product(p.x, p.w[g]) for g in range(5)]
+    for off in ([0, 650, 0, 650, 0, 650], [-9, 700, 100, 400, 390, 2 ** 31 - 1], [650, 600, 20, 20, 0, 3]):
+        y = p.out()
+        lutq.lutq_mx4_matmul_grouped(p.codes, p.packed, to_gpu(np.array(off, dtype=np.int32)), y, p.ws, x_scales=p.e)
+        got = as_f64(y)
+        fits = got == -7.0
+        claimed = np.zeros(650, dtype=bool)
+        for g in range(5):
+            a, b = min(max(off[g], 0), 650), min(max(off[g + 1], 0), 650)
+            claimed[a:b] = True
+            if b > a:
+                fits[a:b] |= (np.abs(got[a:b] - all_sums[g][0][a:b]) <= off_by_at_most(got[a:b], tuple(s[a:b] for s in all_sums[g]), K, "bf16"))
+        assert fits.all() and (got[~claimed] == -7.0).all() and p.guards_hold()
+
+
+@pytest.mark.gpu
 def test_sums_beyond_the_type_become_infinite(lutq):
     p = Problem(lutq, 20, 32, 256, "f16")
     e = p.e.clone()
