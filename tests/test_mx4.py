@@ -619,6 +619,55 @@ def test_streams_and_shared_python_path(lutq, monkeypatch, M):
 
 
 @pytest.mark.gpu
+def test_a_long_axis(lutq):
+    p = Problem(lutq, 19, 16, 1 << 20, "bf16")
+    for dense in (False, True):
+        x, e = p.args(dense)
+        y = p.out()
+        lutq.lutq_mx4_matmul(x, p.packed, y, p.ws, x_scales=e)
+        got, sums = as_f64(y), mx.product(p.x, p.w[0])
+        assert (np.abs(got - sums[0]) <= off_by_at_most(got, sums, p.K, "bf16")).all() and p.guards_hold()
+
+
+@pytest.mark.gpu
+def test_two_streams_and_two_graphs(lutq):
+    """Products whose slices are joined in the workspace: at once on two streams, each with a workspace of its own; and two graphs of one
+    workspace, replayed in turn."""
+    import torch
+    a, b = Problem(lutq, 200, 4112, 8320, "bf16"), Problem(lutq, 131, 2064, 14336, "bf16", seed=1)
+    want = []
+    for p in (a, b):
+        y = torch.empty((p.M, p.N), dtype=torch.bfloat16, device="cuda")
+        lutq.lutq_mx4_matmul(p.codes, p.packed, y, p.ws, x_scales=p.e)
+        sums = mx.product(p.x, p.w[0])
+        assert (np.abs(as_f64(y) - sums[0]) <= off_by_at_most(as_f64(y), sums, p.K, "bf16")).all()
+        want.append(y)
+    torch.cuda.synchronize()
+    streams, outs = (torch.cuda.Stream(), torch.cuda.Stream()), [[torch.zeros_like(w) for _ in range(8)] for w in want]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for p, s, o in zip((a, b), streams, outs):
+            lutq.lutq_mx4_matmul(p.codes, p.packed, o[i], p.ws, x_scales=p.e, stream=s)
+    torch.cuda.synchronize()
+    for w, o in zip(want, outs):
+        assert all(torch.equal(w, y) for y in o)
+    shared = lutq.new_mx4_workspace(200, 4112, 14336)
+    graphs = []
+    for p, o in zip((a, b), outs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            lutq.lutq_mx4_matmul(p.X, p.packed, o[0], shared)
+    for _ in range(4):
+        for g, w, o in zip(graphs, want, outs):
+            o[0].zero_()
+            g.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(w, o[0])
+        lutq.lutq_mx4_matmul(b.codes, b.packed, outs[1][1], shared, x_scales=b.e)
+        assert torch.equal(want[1], outs[1][1])
+
+
+@pytest.mark.gpu
 def test_binding_refusals(lutq):
     import torch
     p = Problem(lutq, 20, 64, 256, "f16", experts=2)
