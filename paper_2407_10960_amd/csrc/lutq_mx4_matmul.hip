@@ -26,7 +26,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t unbounded(const char* base) {
 }
 
 // Sixteen bytes per lane that workgroups on other dies read, or wrote, in the same launch: past the caches that are a die's own.
-constexpr int kSc1 = 16;
+constexpr int kSc1 = 16, kNonTemporal = 2;
 __device__ __forceinline__ void store16_shared(__amdgpu_buffer_rsrc_t to, uint32_t lane_at, int at, f32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, lane_at, at, kSc1);
 }
@@ -291,7 +291,8 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
     using Shape = TileShape<WN, WM, GN, GM, DEPTH>;
     constexpr int kWaves = Shape::kWaves, kRB = Shape::kRB, kMB = Shape::kMB, kStep = Shape::kStep, kExps = Shape::kExps;
     constexpr int kWLoads = kRB / kWaves, kXLoads = 2 * kMB / kWaves;          // per wavefront: pieces of weights, halves of pieces of X
-    constexpr int kLoads = 2 * kWLoads + kXLoads;
+    constexpr int kLoads = 2 * kWLoads + kXLoads, kStores = WN / 2 * WM;
+    constexpr uint32_t kNowhere = 0x7fffffff;
     // Of a step's copies, those that are asked for in the second half of a step; the others follow in the first half of the next, where
     // the steps are long or many enough for them to arrive in time.
     constexpr int kEarly = DEPTH > 2 || kWaves > 4 ? (2 * kLoads + 2) / 3 : kLoads;
@@ -452,11 +453,12 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
 #pragma unroll
             for (int b = 0; b < WM; ++b) asm volatile("" : "+v"(acc[r][b]));
     };
-    // Step s of `it`; its first tile is in the registers.
-    auto one_step = [&](int s, const Item& it, int first_quad) {
+    // Step s of `it`; its first tile is in the registers.  `first` of an item: all copies of the steps that there is room for have been asked for,
+    // and behind them kStores stores of the item before, if `stored`; those may still be under way when the next step has to be there.
+    auto one_step = [&](auto first, int s, const Item& it, int first_quad, bool stored) {
         constexpr int kLate = WN / 2;
         multiply(integral_constant<int, 0>(), here, []() {}, [&](int r) {
-            if (r < kLate) {
+            if (!first && r < kLate) {
 #pragma unroll
                 for (int j = kEarly + r * (kLoads - kEarly) / kLate; j < kEarly + (r + 1) * (kLoads - kEarly) / kLate; ++j) load_part(j);
             }
@@ -466,7 +468,8 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         multiply(integral_constant<int, 1>(), here, [&]() {
             // The next step is there, and nobody needs this one's place any more.  (Here and not before the first products, when the
             // operands read last may still be on their way.)
-            arrive<(DEPTH - 2) * kLoads>();
+            if (first && stored) arrive<(DEPTH - 2) * kLoads + kStores>();
+            else arrive<(DEPTH - 2) * kLoads>();
             __builtin_amdgcn_sched_barrier(0);
             load_exps();
         }, [&](int r) {
@@ -493,15 +496,16 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
     for (int t = 0; t < DEPTH; ++t) {
         load_exps();
 #pragma unroll
-        for (int j = 0; j < (t < DEPTH - 1 ? kLoads : kEarly); ++j) load_part(j);
+        for (int j = 0; j < kLoads; ++j) load_part(j);
         if (t < DEPTH - 1) next();
     }
-    arrive<(DEPTH - 2) * kLoads + kEarly>();
+    arrive<(DEPTH - 1) * kLoads>();
     read_exps(it.step / 2);
     read_x(0, 0);
 #pragma unroll
     for (int r = 0; r < WN; ++r) read_w(0, 0, r);
 
+    bool stored = false;
     for (int mine = (int)blockIdx.x;;) {
 #pragma unroll
         for (int r = 0; r < WN; ++r)
@@ -510,7 +514,10 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         mine += (int)gridDim.x;
         const Item after = mine < total ? item(mine) : it;
         int s = it.step;
-        for (; s < it.steps; ++s) one_step(s, it, after.step / 2);
+        one_step(std::true_type(), s, it, after.step / 2, stored);
+        for (++s; s < it.steps; ++s) one_step(std::false_type(), s, it, after.step / 2, false);
+#pragma unroll
+        for (int j = kEarly; j < kLoads; ++j) load_part(j);
 
         bool finished = true;
         if (Shape::kSlices && p.slices > 1) {          // the other slices of this tile
@@ -566,15 +573,22 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             }
         }
         // The lanes of a row of X hold four neighbouring sums each, of either row block of a pair.  The two blocks' words are exchanged between
-        // neighbouring rows of lanes, so that every lane stores sixteen bytes: those of even o of the first block, of odd o of the second.
+        // neighbouring rows of lanes, so that every lane has sixteen bytes: those of even o of the first block, of odd o of the second.  With four
+        // row blocks the lanes of rows i and i + 8 exchange one of their two sixteen bytes as well, and a store writes whole cache lines of
+        // eight rows, non-temporal ones: Y would drive the factors, which are read again, out of the caches.  (16384 rows, 28672 x 4096:
+        // 966 us with half lines and kept, 954 with whole ones, 923 non-temporal, 904 with both.  Half lines of the small tiles are kept:
+        // 512 rows, 4096 x 4096, 12.3 us, non-temporal 12.7.)
+        // Lanes whose row or row block does not exist store behind what the descriptor covers, which does nothing: so every wavefront has kStores
+        // stores under way, and the next item's first step need not wait for them (8192 rows, 8192 x 2048: 157 -> 154).
         static_assert(WN % 2 == 0, "row blocks in pairs");
         if (finished) {
+            const int last_rb = p.NB - 1 - it.rb0 - wn * WN - (o & 1);         // the lane's, from the wavefront's first
 #pragma unroll
             for (int b = 0; b < WM; ++b) {
-                const int m = it.m0 + 16 * (wm * WM + b) + i;
-                char* y = p.y + ((int64_t)m * p.N + 16 * (it.rb0 + wn * WN + (o & 1)) + 8 * (o >> 1)) * 2;
-#pragma unroll
-                for (int r = 0; r < WN; r += 2) {
+                const int m = it.m0 + 16 * (wm * WM + b);
+                const auto y = __builtin_amdgcn_make_buffer_rsrc(p.y + ((int64_t)m * p.N + 16 * (it.rb0 + wn * WN)) * 2, 0, 0x40000000, 0x00020000);
+                const int at = 16 * (o & 1) + 8 * (o >> 1);
+                auto pair_of = [&](int r) {
                     u32x4 out;
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
@@ -583,10 +597,36 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
                         out[h] = two[0];
                         out[2 + h] = two[1];
                     }
-                    if (m < it.m1 && it.rb0 + wn * WN + r + (o & 1) < p.NB) *reinterpret_cast<u32x4*>(y + r * 32) = out;
+                    return out;
+                };
+                if constexpr (WN % 4 == 0) {
+                    const bool low = i < 8;
+                    const uint32_t to = (uint32_t)((i & 7) * p.N + at) * 2 + (low ? 0 : 64);
+                    const uint32_t to1 = m + (i & 7) < it.m1 ? to : kNowhere, to2 = m + 8 + (i & 7) < it.m1 ? to + 16 * p.N : kNowhere;
+#pragma unroll
+                    for (int r = 0; r < WN; r += 4) {
+                        const u32x4 first = pair_of(r), second = pair_of(r + 2);
+                        u32x4 one, two;
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) {
+                            const uint32_t t = low ? second[h] : first[h];
+                            const uint32_t u = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0x128, 0xf, 0xf, true);   // row_ror 8
+                            one[h] = low ? first[h] : u;
+                            two[h] = low ? u : second[h];
+                        }
+                        const bool there = r + (low ? 0 : 2) <= last_rb;
+                        __builtin_amdgcn_raw_buffer_store_b128(one, y, there ? to1 : kNowhere, r * 32, kNonTemporal);
+                        __builtin_amdgcn_raw_buffer_store_b128(two, y, there ? to2 : kNowhere, r * 32, kNonTemporal);
+                    }
+                } else {
+                    const uint32_t to = m + i < it.m1 ? (uint32_t)(i * p.N + at) * 2 : kNowhere;
+#pragma unroll
+                    for (int r = 0; r < WN; r += 2)
+                        __builtin_amdgcn_raw_buffer_store_b128(pair_of(r), y, r <= last_rb ? to : kNowhere, r * 32, 0);
                 }
             }
         }
+        stored = finished;
         if (mine >= total) break;
         it = after;
     }
