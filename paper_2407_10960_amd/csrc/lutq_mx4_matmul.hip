@@ -82,21 +82,20 @@ template <int ROWS> struct Pieces {
         for (int base = 0; base < experts; base += 64) { look(base); n = min(n + all(), kMost); }
         return n;
     }
-    // The expert and the rows [first, end) of piece `slot`, which has to exist.  (Up to 64 experts, count() has looked already.)
-    __device__ __forceinline__ void find(int slot, int& expert, int& first, int& end) {
+    // Piece `slot`, which has to exist: its expert, that expert's rows [first, end) and pieces [begin, begin + pieces).  (Up to 64 experts,
+    // count() has looked already.)
+    struct Found { int expert, first, end, begin, pieces; };
+    __device__ __forceinline__ Found find(int slot) {
         int before = 0;
         for (int base = 0; base < experts; base += 64) {
             if (experts > 64) look(base);
             if (before + all() > slot) {
-                const int at = __builtin_ctzll(__ballot(before + sum > slot));
-                const int begin = before + __builtin_amdgcn_readlane(sum, at) - __builtin_amdgcn_readlane(mine(), at);
-                expert = base + at;
-                first = __builtin_amdgcn_readlane(a, at) + (slot - begin) * ROWS;
-                end = min(__builtin_amdgcn_readlane(b, at), first + ROWS);
-                return;
+                const int at = __builtin_ctzll(__ballot(before + sum > slot)), n = __builtin_amdgcn_readlane(mine(), at);
+                return {base + at, __builtin_amdgcn_readlane(a, at), __builtin_amdgcn_readlane(b, at), before + __builtin_amdgcn_readlane(sum, at) - n, n};
             }
             before = min(before + all(), kMost);
         }
+        return {0, 0, 0, 0, 1};
     }
 };
 
@@ -134,7 +133,10 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
     if constexpr (GROUPED) {
         Pieces<16> pieces{p.offsets, p.experts, p.M};
         if (slot >= pieces.count()) return;
-        pieces.find(slot, expert, m0, m1);
+        const auto in = pieces.find(slot);
+        expert = in.expert;
+        m0 = in.first + (slot - in.begin) * 16;
+        m1 = min(in.end, m0 + 16);
     }
     const int rb0 = (int)blockIdx.x * R, rows = m1 - m0;
     const char* w[R];
@@ -311,19 +313,31 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
     const int total = slots * nx * p.slices;           // tiles of Y, each `slices` times
 
     struct Item { int expert, m0, m1, rb0, tile, slice, step, steps; };        // step .. steps - 1 of the whole of K
-    // Tiles of Y are ordered in bands of kBand pieces of rows of X, so that what a die's cache holds of either factor is used several times.
+    // The tiles of an expert (without experts: all) are ordered in bands of at most kBand pieces of rows of X, so that what a die's cache holds
+    // of either factor is used several times; higher ones by expert, whose weights come from memory.  (Bands of four across experts, and so:
+    // 8 experts of 28672 x 4096, 2048 rows each, 1058 us and 1005; 32 of 4096 x 2304, 4099 rows, 58 and 54.  8192 rows, 8192 x 8192
+    // without experts: 243 us, in bands of eight 249.)
     auto item = [&](int number) {
-        constexpr int kBand = 4;
+        constexpr int kBand = GROUPED ? 8 : 4;
         Item it;
         const int id = by_die(number, total);
         it.tile = p.slices == 1 ? id : quotient(id, p.slices);
         it.slice = id - it.tile * p.slices;
-        const int band = quotient(it.tile, kBand * nx), inside = it.tile - band * kBand * nx, high = min(kBand, slots - band * kBand);
-        const int nt = quotient(inside, high), slot = p.slot0 + band * kBand + (inside - nt * high);
-        it.expert = 0;
-        it.m0 = slot * 16 * kMB;
-        it.m1 = min(p.M, it.m0 + 16 * kMB);
-        if constexpr (GROUPED) pieces.find(slot, it.expert, it.m0, it.m1);
+        int inside = it.tile, from = p.slot0, n = slots;                       // the tile's place among those of its expert's pieces
+        typename Pieces<16 * kMB>::Found in{0, 0, p.M, 0, 0};
+        if constexpr (GROUPED) {
+            in = pieces.find(p.slot0 + quotient(it.tile, nx));
+            from = max(in.begin, p.slot0);
+            n = min(in.begin + in.pieces, p.slot0 + slots) - from;
+            inside -= (from - p.slot0) * nx;
+        }
+        const int bands = (n + kBand - 1) / kBand, high = quotient(n + bands - 1, bands);
+        const int band = quotient(inside, high * nx), left = min(high, n - band * high);
+        inside -= band * high * nx;
+        const int nt = quotient(inside, left);
+        it.expert = in.expert;
+        it.m0 = in.first + (from + band * high + inside - nt * left - in.begin) * 16 * kMB;
+        it.m1 = min(in.end, it.m0 + 16 * kMB);
         it.rb0 = nt * kRB;
         it.step = 0;
         it.steps = (p.KT + 1) / 2;
@@ -390,6 +404,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             else copy16(esrc, efrom[j], min(step * 8, ebytes - 16), to + c * 1024);
         }
     };
+    Item ahead = {};
     auto next = [&]() {
         place = (place + 1) % DEPTH;
         if (++step < steps) return;
@@ -397,7 +412,8 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         // at every step.)
         if (number + (int)gridDim.x < total) {
             number += (int)gridDim.x;
-            aim(item(number));
+            ahead = item(number);
+            aim(ahead);
         } else --step;
     };
 
@@ -512,10 +528,11 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
 #pragma unroll
             for (int b = 0; b < WM; ++b) acc[r][b] = f32x4{0.f, 0.f, 0.f, 0.f};
         mine += (int)gridDim.x;
-        const Item after = mine < total ? item(mine) : it;
+        int first_quad = 0;                            // of the next item
+        if (Shape::kSlices && p.slices > 1 && mine < total) first_quad = item(mine).step / 2;
         int s = it.step;
-        one_step(std::true_type(), s, it, after.step / 2, stored);
-        for (++s; s < it.steps; ++s) one_step(std::false_type(), s, it, after.step / 2, false);
+        one_step(std::true_type(), s, it, first_quad, stored);
+        for (++s; s < it.steps; ++s) one_step(std::false_type(), s, it, first_quad, false);
 #pragma unroll
         for (int j = kEarly; j < kLoads; ++j) load_part(j);
 
@@ -628,7 +645,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         }
         stored = finished;
         if (mine >= total) break;
-        it = after;
+        it = number == mine ? ahead : item(mine);      // (the copies may be further ahead where items have fewer steps than there is room for)
     }
     arrive<0>();                                       // (no copy into this workgroup's LDS outlives it)
 }
