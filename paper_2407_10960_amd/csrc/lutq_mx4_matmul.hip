@@ -722,7 +722,7 @@ hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
 // Examples (us, shapes in this order): 17 rows, 6144 x 4096 6.2, and tiles at best 9.3; 28672 x 4096 21.8, and 15.5; 512 rows,
 // 4096 x 4096 -, 27.6, 15.2, 14.5, 11.5, 12.7; 8192 rows, 8192 x 8192 -, 240, 318, 378, 543, 569; 200 rows, 28672 x 4096 -, 34, 27.0, 28.6,
 // 35.3, 33.3; 200 rows, 5120 x 13824 -, 84, 48, 35.4, 26.7, 30.8, and 21.9 with 128 x 128 in three slices; 64 rows, 4096 x 14336 -, 83, 52, 36,
-// 33, 24.8, and 13.8 with 64 x 64 in four.
+// 33, 24.8, and 13.8 with 64 x 64 in four.  80 rows through 2 experts of 4096 x 14336: 27, in slices 17.8.
 // By expert the number of pieces is not known here: every expert is taken to have the mean number of rows and half a piece that is not full.
 struct TileChoice { int shape, slices; };             // shape -1: streamed
 
@@ -749,7 +749,7 @@ TileChoice choose_kernel(int64_t M, int64_t NB, int64_t KT, int64_t experts, int
     consider(1, 1, 1.5 + pairs(n1, 0.95, 1.25) * S + 1.3 * n1);
     for (int z = 1; z <= 8; ++z) {
         const double steps = (double)((int64_t)(S + z - 1) / z);
-        if (z > 1 && (experts || z > KQ)) break;
+        if (z > KQ) break;
         if (z == 1 || t1 * z <= cus) consider(2, z, 3.2 + rounds(t1 * z) * ((t1 > cus ? 0.72 : 0.63) * steps + 1.0) + (z > 1 ? 2.5 + 1.6 * z : 0.0));
         if (z == 1 || t3 * z <= cus) consider(3, z, 3.0 + rounds(t3 * z) * (0.505 * steps + 0.4) + (z > 1 ? 3.0 + 0.8 * z : 0.0));
         if (z == 1 || t4 * z <= 2 * cus) consider(4, z, 2.5 + pairs(rounds(t4 * z), 0.39, 0.62) * steps + (z > 1 ? 1.8 + 1.0 * z : 0.0));

@@ -419,7 +419,9 @@ def test_product_by_expert_of_uneven_rows(lutq, case, dense):
 @pytest.mark.gpu
 @pytest.mark.parametrize("dense", [False, True])
 @pytest.mark.parametrize("counts,N,K", [([0, 171, 9], 2064, 512), ([33, 0, 70, 1, 16, 0, 49, 8, 3], 2064, 2176), ([129, 255, 10, 256, 0], 4112, 512),
-                                        ([2000, 0, 17, 900, 3000, 1, 128, 129, 1925], 272, 1152), ([1111, 2, 0, 3100, 287], 2064, 640)])
+                                        ([2000, 0, 17, 900, 3000, 1, 128, 129, 1925], 272, 1152), ([1111, 2, 0, 3100, 287], 2064, 640),
+                                        # (with K in slices)
+                                        ([140, 0, 52], 1040, 8320), ([7, 31], 4112, 14336), ([1, 199], 4112, 8320), ([0, 90, 100, 110, 0], 528, 14336)])
 def test_product_by_expert_of_many_rows(lutq, counts, N, K, dense):
     off = counts_to_offsets(counts, 2)
     p = Problem(lutq, int(off[-1]) + 3, N, K, "bf16", experts=len(counts))
@@ -429,7 +431,10 @@ def test_product_by_expert_of_many_rows(lutq, counts, N, K, dense):
     got, sums = as_f64(y), grouped_reference(p, off)
     worst = np.max(np.abs(got - sums[0]) / off_by_at_most(got, sums, K, "bf16"))
     assert worst <= 1.0, worst
-    assert p.guards_hold()
+    assert p.guards_hold() and not p.ws[:65536].any().item()
+    again = p.out()
+    lutq.lutq_mx4_matmul_grouped(x, p.packed, to_gpu(off), again, p.ws, x_scales=e)
+    assert np.array_equal(as_f64(again), got)
 
 
 @pytest.mark.gpu
