@@ -712,13 +712,14 @@ hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
 
 // Whether the weights are streamed past sixteen rows at a time, or which tile shape, and for the smaller ones how many slices of K: the least
 // of times estimated from the bytes of weights over the pieces of rows (B), or from the number of tiles on the busiest compute unit (n) and of
-// steps (S).  Microseconds, fitted to 120 products of 1 to 4096 rows on 1024 x 4096 to 28672 x 4096:
+// steps (S).  Microseconds, fitted to some 300 products of 17 to 16384 rows, N 256 to 32768, K 512 to 16384
+// (the least of all shapes and slices tried was 2 % less on average, products by expert 3 %):
 //   streamed        2.3 + B / 6.6 TB/s
-//   256 x 256       3.0 + n (1.75 S + 5)                  one workgroup per compute unit; the 5 are its stores, all at once
-//   128 x 128       1.5 + 1.25 S per two, 0.95 S for one  two workgroups per unit, two steps of room each
+//   256 x 256       6.0 + n (1.75 S + 4.5)                one workgroup per compute unit; the 4.5 are its stores
+//   128 x 128       1.5 + 1.25 S + 2.6 per two, 0.95 S + 1.3 for one; two workgroups per unit, two steps of room each
 //   128 x 128 deep  3.2 + n (0.72 S + 1), 0.63 S for one  one of eight wavefronts, four steps of room; in z slices of K 2.5 + 1.6 z more
-//   128 x 64 deep   3.0 + n (0.505 S + 0.4)               the same; in z slices 3 + 0.8 z more
-//   64 x 64 deep    2.5 + 0.62 S per two, 0.39 S for one  two of four wavefronts; in z slices 1.8 + z more
+//   128 x 64 deep   3.2 + n (0.50 S + 0.7)                the same; in z slices 3 + 0.8 z more
+//   64 x 64 deep    3.0 + 0.62 S + 0.9 per two, 0.37 S + 0.9 for one; two of four wavefronts; in z slices 1.8 + z more
 // Examples (us, shapes in this order): 17 rows, 6144 x 4096 6.2, and tiles at best 9.3; 28672 x 4096 21.8, and 15.5; 512 rows,
 // 4096 x 4096 -, 27.6, 15.2, 14.5, 11.5, 12.7; 8192 rows, 8192 x 8192 -, 240, 318, 378, 543, 569; 200 rows, 28672 x 4096 -, 34, 27.0, 28.6,
 // 35.3, 33.3; 200 rows, 5120 x 13824 -, 84, 48, 35.4, 26.7, 30.8, and 21.9 with 128 x 128 in three slices; 64 rows, 4096 x 14336 -, 83, 52, 36,
@@ -745,14 +746,14 @@ TileChoice choose_kernel(int64_t M, int64_t NB, int64_t KT, int64_t experts, int
     auto pairs = [&](double n, double one, double two) { return two * (double)(int64_t)(n / 2) + ((int64_t)n % 2 ? one : 0.0); };
     const double t0 = tiles(16, 256), t1 = tiles(8, 128), t3 = tiles(8, 64), t4 = tiles(4, 64);
     const double n0 = rounds(t0), n1 = rounds(t1);
-    consider(0, 1, 3.0 + n0 * (1.75 * S + 5.0 * (t0 < cus ? t0 / cus : 1.0)));
+    consider(0, 1, 6.0 + n0 * (1.75 * S + 4.5 * (t0 < cus ? t0 / cus : 1.0)));
     consider(1, 1, 1.5 + pairs(n1, 0.95, 1.25) * S + 1.3 * n1);
     for (int z = 1; z <= 8; ++z) {
         const double steps = (double)((int64_t)(S + z - 1) / z);
         if (z > KQ) break;
         if (z == 1 || t1 * z <= cus) consider(2, z, 3.2 + rounds(t1 * z) * ((t1 > cus ? 0.72 : 0.63) * steps + 1.0) + (z > 1 ? 2.5 + 1.6 * z : 0.0));
-        if (z == 1 || t3 * z <= cus) consider(3, z, 3.0 + rounds(t3 * z) * (0.505 * steps + 0.4) + (z > 1 ? 3.0 + 0.8 * z : 0.0));
-        if (z == 1 || t4 * z <= 2 * cus) consider(4, z, 2.5 + pairs(rounds(t4 * z), 0.39, 0.62) * steps + (z > 1 ? 1.8 + 1.0 * z : 0.0));
+        if (z == 1 || t3 * z <= cus) consider(3, z, 3.2 + rounds(t3 * z) * (0.50 * steps + 0.7) + (z > 1 ? 3.0 + 0.8 * z : 0.0));
+        if (z == 1 || t4 * z <= 2 * cus) consider(4, z, 3.0 + pairs(rounds(t4 * z), 0.37 * steps + 0.9, 0.62 * steps + 0.9) + (z > 1 ? 1.8 + 1.0 * z : 0.0));
     }
     return best;
 }
@@ -785,7 +786,7 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     // 10.5, 4 rows (112) 10.1 and 10.7, 8 rows (224) 14.4 and 11.1; 6144 x 4096, 13 rows (104) 7.4 and 7.9; 1024 x 8192, 8 rows (128) 7.4 and 6.3).
     // Two row blocks per workgroup halve it, and leave fewer wavefronts to hide the reads (28672 x 4096, 1 row 13.4 and 13.6, 2 rows 14.7 and
     // 13.9 with one; 128 experts of 1536 x 4096, 64 rows, 34.4 and 35.3).  Codes alone gain by two where workgroups are many and share their
-    // weights (64 experts, 250 rows: 36.8 and 38.1; 500 rows 37.4 and 39.4) and lose with a row each (34.1 and 33.2).  A single quad of K
+    // weights (64 experts, 250 rows: 36.8 and 38.1; 500 rows 37.4 and 39.4) and lose with a row or two each (34.1 and 33.2).  A single quad of K
     // leaves nothing to hide: 8192 rows, 8192 x 384, 71 us with four row blocks, 97 with one.
     const int64_t pieces = offsets ? (M < experts ? M : experts) : (M + 15) / 16, groups = p.NB * pieces, mean = (M + pieces - 1) / pieces;
     int wide = src != kF32 && (groups > 1024 || mean > 4) ? 2 : 1;             // row blocks per streaming workgroup
@@ -798,12 +799,15 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
         src = kF32;
         wide = 1;
     }
-    if (src == kF32 && groups > 4096) wide = p.KQ == 1 ? 4 : mean > 1 ? 2 : 1;
+    if (src == kF32 && groups > (offsets ? 2048 : 4096)) wide = p.KQ == 1 ? 4 : mean > 2 ? 2 : 1;
     if (c.shape < 0) {
-        // Wavefronts of a workgroup, each with a quad or two of K: sixteen with one row block, eight with two (their registers) or where they
-        // quantise and workgroups are many, four where workgroups are so many that their beginnings count (64 experts of
-        // 1536 x 4096, a row each: 37.3 us with eight, 33.2 with four; 57344 x 8192, 1 row: 44.2 with eight, 42.2 with sixteen).
-        const int most = groups > 4096 ? 4 : wide > 1 || (src != kF32 && groups > 512) ? 8 : 16;
+        // Wavefronts of a workgroup: sixteen with one row block, eight with two (their registers) or where they quantise and workgroups are many,
+        // four where workgroups are so many that their beginnings count (57344 x 8192, 1 row: 44.2 us with eight, 42.2 with sixteen).
+        // By expert, where X is codes, four from fewer workgroups on, and fewer with two quads each where there are very many, as some
+        // find that there is nothing for them, and the others lie all over the weights (65 experts of 720 x 6272, 35 rows: 13.2 with thirteen, 9.6
+        // with four; 50 of 3376 x 2688, 28 rows: 7.4 with four, 6.2 with three; 41 of 480 x 1408, 40 rows: 4.2 with three, 4.5 with two).
+        const int many = groups > 2048 ? (p.KQ < 4 ? 2 : p.KQ < 8 ? p.KQ / 2 : 4) : 4;
+        const int most = offsets && src == kF32 && groups > 900 ? many : groups > 4096 ? 4 : wide > 1 || (src != kF32 && groups > 512) ? 8 : 16;
         const int waves = wide == 4 ? (pieces < 4 ? (int)pieces : 4) : p.KQ < most ? p.KQ : most;
         auto by_rows = [&](auto source) {
             constexpr int SRC = decltype(source)::value;
