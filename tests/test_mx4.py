@@ -324,7 +324,8 @@ def test_product(lutq, M, N, K, dense, dtype):
 
 # (each shape of tiles, with ragged edges; the long ones with K in two to five slices)
 TILED = [(103, 4112, 640), (199, 4112, 2176), (999, 2064, 1152), (1001, 4112, 1152), (2100, 4112, 1152), (130, 2064, 8320), (101, 2064, 8320),
-         (601, 272, 14336), (131, 1040, 16512), (131, 2064, 14336), (67, 4112, 14336), (131, 4112, 14336), (200, 4112, 8320), (259, 4112, 14336)]
+         (601, 272, 14336), (131, 1040, 16512), (131, 2064, 14336), (67, 4112, 14336), (131, 4112, 14336), (200, 4112, 8320), (259, 4112, 14336),
+         (601, 1072, 1152), (300, 2064, 1664), (2100, 4112, 2176), (3001, 4112, 1152)]
 
 
 @pytest.mark.gpu
@@ -421,7 +422,8 @@ def test_product_by_expert_of_uneven_rows(lutq, case, dense):
 @pytest.mark.parametrize("counts,N,K", [([0, 171, 9], 2064, 512), ([33, 0, 70, 1, 16, 0, 49, 8, 3], 2064, 2176), ([129, 255, 10, 256, 0], 4112, 512),
                                         ([2000, 0, 17, 900, 3000, 1, 128, 129, 1925], 272, 1152), ([1111, 2, 0, 3100, 287], 2064, 640),
                                         # (with K in slices)
-                                        ([140, 0, 52], 1040, 8320), ([7, 31], 4112, 14336), ([1, 199], 4112, 8320), ([0, 90, 100, 110, 0], 528, 14336)])
+                                        ([140, 0, 52], 1040, 8320), ([7, 31], 4112, 14336), ([1, 199], 4112, 8320), ([0, 90, 100, 110, 0], 528, 14336),
+                                        ([3, 774, 0], 1040, 640), ([900, 1, 2303, 0, 1300, 700, 2000, 255, 641], 1072, 2176)])
 def test_product_by_expert_of_many_rows(lutq, counts, N, K, dense):
     off = counts_to_offsets(counts, 2)
     p = Problem(lutq, int(off[-1]) + 3, N, K, "bf16", experts=len(counts))
@@ -476,7 +478,8 @@ def test_not_a_number_stays_in_its_row(lutq, M, dense):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dense", [False, True])
-@pytest.mark.parametrize("M,N,K", [(103, 4112, 640), (199, 4112, 2176), (999, 2064, 1152), (1001, 4112, 1152), (2100, 4112, 1152), (101, 2064, 8320)])
+@pytest.mark.parametrize("M,N,K", [(103, 4112, 640), (199, 4112, 2176), (999, 2064, 1152), (1001, 4112, 1152), (2100, 4112, 1152), (101, 2064, 8320),
+                                   (601, 1072, 1152), (2100, 4112, 2176), (130, 2064, 8320)])
 def test_not_a_number_among_many_rows(lutq, M, N, K, dense):
     import torch
     p = Problem(lutq, M, N, K, "bf16")
