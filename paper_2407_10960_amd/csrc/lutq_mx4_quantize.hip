@@ -30,11 +30,13 @@ struct QuantizeParams {
     uint32_t K;
 };
 
+// The dense side, read or written once, is non-temporal: it would drive the codes, which are read soon, out of the caches, and itself does
+// not stay (bf16 8192 x 4096 to codes 18.9 us, so 17.1, and back 18.8, so 14.1; one after the other 38.1 and 30.5).
 template <int SRC> __device__ __forceinline__ Eight<SRC> load_eight(const void* x, int64_t at) {
     Eight<SRC> r;
     const char* p = static_cast<const char*>(x) + at * (SRC == kF32 ? 4 : 2);
-    r.v[0] = *reinterpret_cast<const u32x4*>(p);
-    if constexpr (SRC == kF32) r.v[1] = *reinterpret_cast<const u32x4*>(p + 16);
+    r.v[0] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    if constexpr (SRC == kF32) r.v[1] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p + 16));
     return r;
 }
 
@@ -119,7 +121,7 @@ __global__ __launch_bounds__(kThreads) void dequant_rows(const DequantParams p) 
 #pragma unroll
     for (int t = 0; t < WORDS; ++t) {
         const int64_t w = first + t * kThreads;
-        if (w < p.words) p.out[w] = from_codes<BF16>(c[t], power_of(e[t]));
+        if (w < p.words) __builtin_nontemporal_store(from_codes<BF16>(c[t], power_of(e[t])), &p.out[w]);
     }
 }
 
@@ -137,7 +139,7 @@ __global__ __launch_bounds__(kThreads) void dequant_packed(const DequantParams p
     u32x4* out = p.out + ((int64_t)rb * 16 + i) * (p.K / 8) + q * 64 + j;
 #pragma unroll
     for (uint32_t t = 0; t < 4; ++t)
-        if (t < tiles) out[t * 16] = from_codes<BF16>(c[t], power_of((word >> (8 * t)) & 255u));
+        if (t < tiles) __builtin_nontemporal_store(from_codes<BF16>(c[t], power_of((word >> (8 * t)) & 255u)), &out[t * 16]);
 }
 
 namespace {
