@@ -48,6 +48,7 @@ struct ProductParams {
     int slot0, slots;          // first piece of rows of this launch, and how many
     int slices;                // of K
     int bf16;                  // type of Y
+    int once;                  // streaming: every row block of weights is read by few workgroups
 };
 
 // The rows of X in pieces of at most ROWS that do not straddle experts, numbered in order of the experts.  Every lane of a wavefront looks
@@ -152,9 +153,17 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             we[r] = *reinterpret_cast<const uint32_t*>(w[r] + (int64_t)p.KT * 1024 + q * 256 + lane * 4);
+        }
+        if (p.once) {
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
-                wv[r][t] = *reinterpret_cast<const u32x4*>(w[r] + (int64_t)(4 * q + min(t, tiles - 1)) * 1024 + lane * 16);
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) wv[r][t] = __builtin_amdgcn_raw_buffer_load_b128(unbounded(w[r]), lane * 16, (4 * q + min(t, tiles - 1)) * 1024, kNonTemporal);
+        } else {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) wv[r][t] = __builtin_amdgcn_raw_buffer_load_b128(unbounded(w[r]), lane * 16, (4 * q + min(t, tiles - 1)) * 1024, 0);
         }
         auto multiply = [&](int t, u32x4 xv, uint32_t xe) {                    // `t` is a constant where this is called
 #pragma unroll
@@ -801,6 +810,11 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     }
     if (src == kF32 && groups > (offsets ? 2048 : 4096)) wide = p.KQ == 1 ? 4 : mean > 2 ? 2 : 1;
     if (c.shape < 0) {
+        // Weights that are read once and take more than half of the 256 MB cache are read past it (57344 x 8192, 250 MB, 1 row:
+        // 44.9 us, so 38.9; 64 experts of 2816 x 2048, 250 rows: 34.1 and 31.2).  Smaller ones may still be there at the next call: 28672 x 4096,
+        // three in turn, 13 rows 13.1, past the cache 14.7, though of nine in turn 14.1 and 13.6.  Nor where several workgroups read the same
+        // ones (8 experts of 4096 x 4096, 64 rows: 12.7 and 14.3).
+        p.once = (offsets ? mean <= 4 : M <= 16) && groups * p.record > (int64_t(128) << 20);
         // Wavefronts of a workgroup: sixteen with one row block, eight with two (their registers) or where they quantise and workgroups are many,
         // four where workgroups are so many that their beginnings count (57344 x 8192, 1 row: 44.2 us with eight, 42.2 with sixteen).
         // By expert, where X is codes, four from fewer workgroups on, and fewer with two quads each where there are very many, as some
