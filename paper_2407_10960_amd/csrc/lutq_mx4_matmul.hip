@@ -17,16 +17,17 @@ namespace mx4 {
 lutq_status quantize_rows_on(const void* X, int source, int64_t source_rows, const int32_t* rows, int64_t M, int64_t K,
                              void* codes, void* exponents, hipStream_t stream);
 
+constexpr int kSc1 = 16, kNonTemporal = 2;             // past the caches that are a die's own; past the order of all caches
+
 // Sixteen bytes per lane from memory to LDS, where lane l's go to `to` + 16 l.
-__device__ __forceinline__ void copy16(__amdgpu_buffer_rsrc_t from, uint32_t lane_at, int at, char* to) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_at, at, 0, 0);
+template <int HOW = 0> __device__ __forceinline__ void copy16(__amdgpu_buffer_rsrc_t from, uint32_t lane_at, int at, char* to) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)to, 16, lane_at, at, 0, HOW);
 }
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t unbounded(const char* base) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base), 0, (uint32_t)-1, 0x00020000);
 }
 
-// Sixteen bytes per lane that workgroups on other dies read, or wrote, in the same launch: past the caches that are a die's own.
-constexpr int kSc1 = 16, kNonTemporal = 2;
+// Sixteen bytes per lane that workgroups on other dies read, or wrote, in the same launch.
 __device__ __forceinline__ void store16_shared(__amdgpu_buffer_rsrc_t to, uint32_t lane_at, int at, f32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, lane_at, at, kSc1);
 }
@@ -48,7 +49,7 @@ struct ProductParams {
     int slot0, slots;          // first piece of rows of this launch, and how many
     int slices;                // of K
     int bf16;                  // type of Y
-    int once;                  // streaming: every row block of weights is read by few workgroups
+    int once;                  // weights that are read once and do not stay in the caches: past them
 };
 
 // The rows of X in pieces of at most ROWS that do not straddle experts, numbered in order of the experts.  Every lane of a wavefront looks
@@ -296,7 +297,7 @@ template <int WN, int WM, int GN, int GM, int DEPTH> struct TileShape {
     static constexpr int kSums = kWaves * WN * WM * 1024;                      // bytes of a tile's sums
 };
 
-template <int WN, int WM, int GN, int GM, int DEPTH, bool GROUPED>
+template <int WN, int WM, int GN, int GM, int DEPTH, bool GROUPED, bool ONCE>
 __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductParams p) {
     using std::integral_constant;
     using Shape = TileShape<WN, WM, GN, GM, DEPTH>;
@@ -393,7 +394,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         const bool whole = 2 * step + 1 < p.KT;
         if (j < 2 * kWLoads) {
             const int c = wave + kWaves * (j >> 1), second = j & 1;
-            copy16(wsrc, wfrom[j >> 1], step * 2048 + (second && whole ? 1024 : 0), to + c * 2048 + second * 1024);
+            copy16<ONCE ? kNonTemporal : 0>(wsrc, wfrom[j >> 1], step * 2048 + (second && whole ? 1024 : 0), to + c * 2048 + second * 1024);
         } else {
             const int c = wave + kWaves * (j - 2 * kWLoads);
             const uint32_t at = xfrom[j - 2 * kWLoads], from = whole ? at : at - ((block ^ (4 * (c & 1))) & 4) * 16;
@@ -713,8 +714,14 @@ hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
         p.slot0 = (int)at;
         p.slots = (int)(pieces - at < most ? pieces - at : most);
         const int64_t items = nx * p.slots * slices, grid = items < (int64_t)cus * kAtOnce ? items : (int64_t)cus * kAtOnce;
-        e = p.offsets ? launch(tile_kernel<WN, WM, GN, GM, DEPTH, true>, dim3((unsigned)grid), Shape::kThreads, Shape::kLds, p, s)
-                      : launch(tile_kernel<WN, WM, GN, GM, DEPTH, false>, dim3((unsigned)grid), Shape::kThreads, Shape::kLds, p, s);
+        auto run = [&](auto once) {
+            constexpr bool ONCE = decltype(once)::value;
+            const dim3 g((unsigned)grid);
+            return p.offsets ? launch(tile_kernel<WN, WM, GN, GM, DEPTH, true, ONCE>, g, Shape::kThreads, Shape::kLds, p, s)
+                             : launch(tile_kernel<WN, WM, GN, GM, DEPTH, false, ONCE>, g, Shape::kThreads, Shape::kLds, p, s);
+        };
+        if constexpr (Shape::kMB <= 8) e = p.once ? run(std::true_type()) : run(std::false_type());
+        else e = run(std::false_type());
     }
     return e;
 }
@@ -809,12 +816,13 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
         wide = 1;
     }
     if (src == kF32 && groups > (offsets ? 2048 : 4096)) wide = p.KQ == 1 ? 4 : mean > 2 ? 2 : 1;
+    // Weights that are read once and take more than half of the 256 MB cache are read past it (57344 x 8192, 250 MB, 1 row:
+    // 44.9 us, so 38.9; 64 experts of 2816 x 2048, 250 rows: 34.1 and 31.2; of 1536 x 4096, 1100 rows: 52.4 and 48.5).  Smaller ones may still be
+    // there at the next call: 28672 x 4096, three in turn, 13 rows 13.1, past the cache 14.7, though of nine in turn 14.1 and 13.6.  Nor where
+    // several workgroups read the same ones (8 experts of 4096 x 4096, 64 rows: 12.7 and 14.3; 1024 rows, 5120 x 5120: 28.7 and 33.7).
+    const int64_t shared = c.shape >= 0 ? (c.shape == 3 || c.shape == 4 ? 64 : 128) : offsets ? 4 : 16;
+    p.once = (offsets ? mean : M) <= shared && p.NB * (offsets ? pieces : 1) * p.record > (int64_t(128) << 20);
     if (c.shape < 0) {
-        // Weights that are read once and take more than half of the 256 MB cache are read past it (57344 x 8192, 250 MB, 1 row:
-        // 44.9 us, so 38.9; 64 experts of 2816 x 2048, 250 rows: 34.1 and 31.2).  Smaller ones may still be there at the next call: 28672 x 4096,
-        // three in turn, 13 rows 13.1, past the cache 14.7, though of nine in turn 14.1 and 13.6.  Nor where several workgroups read the same
-        // ones (8 experts of 4096 x 4096, 64 rows: 12.7 and 14.3).
-        p.once = (offsets ? mean <= 4 : M <= 16) && groups * p.record > (int64_t(128) << 20);
         // Wavefronts of a workgroup: sixteen with one row block, eight with two (their registers) or where they quantise and workgroups are many,
         // four where workgroups are so many that their beginnings count (57344 x 8192, 1 row: 44.2 us with eight, 42.2 with sixteen).
         // By expert, where X is codes, four from fewer workgroups on, and fewer with two quads each where there are very many, as some

@@ -649,28 +649,30 @@ def test_weights_larger_than_half_the_cache(lutq, dense):
     lutq.lutq_mx4_quantize_packed(W, packed)
     lutq.lutq_mx4_dequant_packed(packed, W)
     w = W.double()
-    X = torch.randn((20, K), generator=gen, device="cuda", dtype=torch.bfloat16)
-    codes, e, values = torch.empty((20, K // 2), dtype=torch.uint8, device="cuda"), torch.empty((20, K // 32), dtype=torch.uint8, device="cuda"), X.clone()
+    X = torch.randn((400, K), generator=gen, device="cuda", dtype=torch.bfloat16)
+    codes, e, values = torch.empty((400, K // 2), dtype=torch.uint8, device="cuda"), torch.empty((400, K // 32), dtype=torch.uint8, device="cuda"), X.clone()
     lutq.lutq_mx4_quantize(X, codes, e)
     lutq.lutq_mx4_dequant(codes, e, values)
     x = values.double()
-    for M in (1, 3, 13):
+    for M in (1, 3, 13, 40, 100, 128):
         y = torch.full((M, N), -7.0, dtype=torch.bfloat16, device="cuda")
         lutq.lutq_mx4_matmul(X[:M] if dense else codes[:M], packed, y, lutq.new_mx4_workspace(M, N, K), x_scales=None if dense else e[:M])
         sums = as_f64(x[:M] @ w.T), as_f64(x[:M].abs() @ w.abs().T)
         assert (np.abs(as_f64(y) - sums[0]) <= off_by_at_most(as_f64(y), sums, K, "bf16")).all()
     n = N // experts
-    off = counts_to_offsets([1, 0, 2, 1, 1, 0, 0, 5, 1, 1, 1, 2, 3, 1])
-    y = torch.full((20, n), -7.0, dtype=torch.bfloat16, device="cuda")
-    lutq.lutq_mx4_matmul_grouped(X if dense else codes, packed.view(experts, -1), to_gpu(off), y, lutq.new_mx4_workspace(20, n, K, experts),
-                                 x_scales=None if dense else e)
-    for g in range(experts):
-        a, b = int(off[g]), int(off[g + 1])
-        if b > a:
-            wg = w[g * n:(g + 1) * n]
-            sums = as_f64(x[a:b] @ wg.T), as_f64(x[a:b].abs() @ wg.abs().T)
-            assert (np.abs(as_f64(y[a:b]) - sums[0]) <= off_by_at_most(as_f64(y[a:b]), sums, K, "bf16")).all()
-    assert int(off[-1]) == 19 and (y[19:] == -7.0).all().item()
+    for counts in ([1, 0, 2, 1, 1, 0, 0, 5, 1, 1, 1, 2, 3, 1], [20, 41, 0, 7, 33, 16, 17, 90, 1, 35, 64, 5, 22, 40]):
+        off = counts_to_offsets(counts)
+        M = int(off[-1]) + 1
+        y = torch.full((M, n), -7.0, dtype=torch.bfloat16, device="cuda")
+        lutq.lutq_mx4_matmul_grouped(X[:M] if dense else codes[:M], packed.view(experts, -1), to_gpu(off), y,
+                                     lutq.new_mx4_workspace(M, n, K, experts), x_scales=None if dense else e[:M])
+        for g in range(experts):
+            a, b = int(off[g]), int(off[g + 1])
+            if b > a:
+                wg = w[g * n:(g + 1) * n]
+                sums = as_f64(x[a:b] @ wg.T), as_f64(x[a:b].abs() @ wg.abs().T)
+                assert (np.abs(as_f64(y[a:b]) - sums[0]) <= off_by_at_most(as_f64(y[a:b]), sums, K, "bf16")).all()
+        assert (y[M - 1:] == -7.0).all().item()
 
 
 @pytest.mark.gpu
