@@ -26,8 +26,8 @@ inline int64_t tile_index(int64_t rb, int64_t kt, int64_t KT, int SB) { return (
 }  // namespace layout
 
 // The packed form of the microscaled 4-bit weights (include/lutq.h): a record per row block of 16 rows, K tiles of 128
-// columns and 1 KiB, then 256 bytes of exponents per four tiles.  The record's length is an odd number of 256-byte pieces
-// more than a power of two for the usual K, so that row blocks streamed side by side do not start in the same memory channel.
+// columns and 1 KiB, then 256 bytes of exponents per four tiles (so a record's length is no power of two where K is one, and
+// row blocks streamed side by side do not all start in the same memory channel).
 namespace mx4 {
 
 inline int64_t k_tiles(int64_t K) { return K / 128; }
