@@ -112,8 +112,9 @@ __device__ __forceinline__ int by_die(int id, int n) {
 
 // Few rows: a workgroup owns R row blocks of weights and sixteen rows of X over all of K; its wavefronts take the quads in turn, and
 // their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the weights, which go from memory into the operand
-// registers as they lie, all of a quad asked for before X is looked at: 28672 x 4096, 62 MB, 1 row 12.7 us (4.9 TB/s), and 13 rows 14.1; smaller
-// ones by the time that one load after another takes to arrive (2048 x 256, 1 row: 2.4 us).
+// registers as they lie, all of a quad asked for before X is looked at: 28672 x 4096, 62 MB, 1 row 12.7 us (4.9 TB/s), and 13 rows 14.0; smaller
+// ones by the time that one load after another takes to arrive (2048 x 256, 1 row: 2.4 us).  X is asked for before the weights (4096 x 14336,
+// 4 rows of bf16: 10.7 us after them, 10.0 so).
 // X is read as its cache lines lie and passes through a place of the wavefront's own in LDS into the order of the operands.  (A lane per row
 // would make 64 requests of every load: 4096 x 14336, 13 rows of codes 14.5 us, so 9.5; of bf16, 6144 x 4096, 8 rows, 7.5 and 6.9.)
 // 16-bit values (SRC 1, 2) are quantised on the way.  ROWS 1 or 4: that many rows at a time, by the four lanes that hold a block, and the
@@ -149,12 +150,39 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
     f32x4 acc[R] = {};
     for (int q = solo ? 0 : wave; q < p.KQ; q += waves) {
         const int tiles = min(4, p.KT - 4 * q);
+        // X first: loads are waited for in order, and it has further to go.  Rows that do not exist stay unread, or are the last row, and what lies
+        // in their places is multiplied: their sums are not stored.
+        constexpr bool values = SRC != kF32 && ROWS == 16;
+        u32x4 v[values ? 4 : 1][4];
+        Eight<SRC == kF32 ? kF16 : SRC> few[ROWS];
+        uint32_t e = 0;
+        const bool word = (lane >> 2) < rows && (lane & 3) < tiles, there = o < tiles;
+        auto ask_few = [&](int first) {                // lane 16 tile + 4 block + piece
+            const char* from = p.x + ((int64_t)(m0 + first) * p.K + q * 512 + lane * 8) * 2;
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k)
+                if (first + k < rows && there) few[k].v[0] = *reinterpret_cast<const u32x4*>(from + (int64_t)k * p.K * 2);
+        };
+        if constexpr (SRC == kF32) {                   // (sixteen lanes take a row's sixteen blocks, four lanes its four words of exponents)
+            const char* from = p.x + (int64_t)(m0 + (lane >> 4)) * (p.K / 2) + q * 256 + (lane & 15) * 16;
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                if (4 * g + (lane >> 4) < rows && (lane & 15) < 4 * tiles) v[0][g] = *reinterpret_cast<const u32x4*>(from + (int64_t)g * 2 * p.K);
+            if (word) e = *reinterpret_cast<const uint32_t*>(p.xe + (int64_t)(m0 + (lane >> 2)) * (p.K / 32) + q * 16 + (lane & 3) * 4);
+        } else if constexpr (values) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+                    if (4 * g < rows)
+                        v[t][g] = *reinterpret_cast<const u32x4*>(p.x + ((int64_t)min(m0 + 4 * g + o, m1 - 1) * p.K + q * 512 + min(t, tiles - 1) * 128 + i * 8) * 2);
+        } else {
+            ask_few(0);
+        }
         uint32_t we[R];
         u32x4 wv[R][4];
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            we[r] = *reinterpret_cast<const uint32_t*>(w[r] + (int64_t)p.KT * 1024 + q * 256 + lane * 4);
-        }
+        for (int r = 0; r < R; ++r) we[r] = *reinterpret_cast<const uint32_t*>(w[r] + (int64_t)p.KT * 1024 + q * 256 + lane * 4);
         if (p.once) {
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -175,15 +203,7 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
                 if (t == 3) acc[r] = product<3, 3>(wv[r][3], xv, acc[r], we[r], xe);
             }
         };
-        if constexpr (SRC != kF32 && ROWS == 16) {
-            // (rows that do not exist: the last row's values, or what lies in their places, whose sums are not stored)
-            u32x4 v[4][4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    if (4 * g < rows)
-                        v[t][g] = *reinterpret_cast<const u32x4*>(p.x + ((int64_t)min(m0 + 4 * g + o, m1 - 1) * p.K + q * 512 + min(t, tiles - 1) * 128 + i * 8) * 2);
+        if constexpr (values) {
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
                 if (t >= tiles) break;
@@ -196,46 +216,32 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
                 for (int j = 0; j < 4; ++j) block[j].v[0] = *reinterpret_cast<const u32x4*>(place + i * kPlane + o * 64 + j * 16);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) max_bits<SRC>(block[j / 4].v[0][j % 4], a);
-                const uint32_t e = exponent_byte<SRC>(a);                      // (255 makes the products NaN whatever the codes)
+                const uint32_t exponent = exponent_byte<SRC>(a);               // (255 makes the products NaN whatever the codes)
                 u32x4 xv;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) xv[j] = to_codes<SRC>(block[j], power_of(e));
-                multiply(t, xv, e << (8 * t));
+                for (int j = 0; j < 4; ++j) xv[j] = to_codes<SRC>(block[j], power_of(exponent));
+                multiply(t, xv, exponent << (8 * t));
             }
             continue;
         }
-        // Rows that do not exist stay unread, and what lies in their places is multiplied: their sums are not stored.
-        if constexpr (SRC == kF32) {                   // (sixteen lanes take a row's sixteen blocks, four lanes its four words of exponents)
-            const char* from = p.x + (int64_t)(m0 + (lane >> 4)) * (p.K / 2) + q * 256 + (lane & 15) * 16;
-            u32x4 c[4];
-            uint32_t e = 0;
-#pragma unroll
-            for (int g = 0; g < 4; ++g)
-                if (4 * g + (lane >> 4) < rows && (lane & 15) < 4 * tiles) c[g] = *reinterpret_cast<const u32x4*>(from + (int64_t)g * 2 * p.K);
-            const bool word = (lane >> 2) < rows && (lane & 3) < tiles;
-            if (word) e = *reinterpret_cast<const uint32_t*>(p.xe + (int64_t)(m0 + (lane >> 2)) * (p.K / 32) + q * 16 + (lane & 3) * 4);
+        if constexpr (SRC == kF32) {
 #pragma unroll
             for (int g = 0; g < 4; ++g)
                 if (4 * g + (lane >> 4) < rows && (lane & 15) < 4 * tiles)
-                    *reinterpret_cast<u32x4*>(place + (lane & 15) * kPlane + (4 * g + (lane >> 4)) * 16) = c[g];
+                    *reinterpret_cast<u32x4*>(place + (lane & 15) * kPlane + (4 * g + (lane >> 4)) * 16) = v[0][g];
             if (word)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) exps[k * 64 + lane] = (char)(e >> (8 * k));
-        } else {                                       // lane 16 tile + 4 block + piece
-            const bool there = o < tiles;
+        } else {
             for (int first = 0; first < rows; first += ROWS) {
-                const char* from = p.x + ((int64_t)(m0 + first) * p.K + q * 512 + lane * 8) * 2;
-                Eight<SRC> v[ROWS];
-#pragma unroll
-                for (int k = 0; k < ROWS; ++k)
-                    if (first + k < rows && there) v[k].v[0] = *reinterpret_cast<const u32x4*>(from + (int64_t)k * p.K * 2);
+                if (first > 0) ask_few(first);
 #pragma unroll
                 for (int k = 0; k < ROWS; ++k) {
                     if (first + k >= rows || !there) continue;
-                    uint32_t e;
-                    const uint32_t c = quantize_eight<SRC>(v[k], e);
+                    uint32_t exponent;
+                    const uint32_t c = quantize_eight<SRC>(few[k], exponent);
                     *reinterpret_cast<uint32_t*>(place + (lane >> 2) * kPlane + (first + k) * 16 + (lane & 3) * 4) = c;
-                    if ((lane & 3) == 0) exps[((lane >> 2) & 3) * 64 + (first + k) * 4 + o] = (char)e;
+                    if ((lane & 3) == 0) exps[((lane >> 2) & 3) * 64 + (first + k) * 4 + o] = (char)exponent;
                 }
             }
         }
