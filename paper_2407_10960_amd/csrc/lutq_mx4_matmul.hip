@@ -803,17 +803,20 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     const int cus = compute_units();
     if (cus < 1) return LUTQ_ERR_DEVICE;
     const TileChoice c = choose_kernel(M, p.NB, p.KT, offsets ? experts : 0, p.record, cus);
-    // Where the streaming workgroups quantise X on the way in, every one of them does it for all its rows.  Beyond some hundred rows and quads
-    // per compute unit that takes longer than a launch which does it once (us, so and with that launch: 4096 x 14336, 1 row (28) 8.9 and
-    // 10.5, 4 rows (112) 10.1 and 10.7, 8 rows (224) 14.4 and 11.1; 6144 x 4096, 13 rows (104) 7.4 and 7.9; 1024 x 8192, 8 rows (128) 7.4 and 6.3).
+    // Where the streaming workgroups quantise X on the way in, every one of them does it for all its rows.  Up to four rows, beyond some 160 rows
+    // and quads per compute unit that takes longer than a launch which does it once (us, so and with that launch: 4096 x 14336, 1 row (28) 8.7
+    // and 10.5; 28672 x 4096, 4 rows (128) 14.9 and 15.4; 512 x 16384, 4 rows (128) 6.2 and 7.1; 4096 x 14336, 6 rows (168) 14.4 and 11.2).  More
+    // rows cost the same however many they are, like twenty (16 rows, 4096 x 4096 (8 quads) 6.3 and 6.8, 6144 x 4096 (8) 7.2 and 8.2; 6 rows,
+    // 1024 x 8192 (16) 7.5 and 6.5, 13824 x 5120 (20) 14.4 and 12.4; 211 rows through 41 experts of 288 x 640 (4) 5.9 and 6.8).
     // Two row blocks per workgroup halve it, and leave fewer wavefronts to hide the reads (28672 x 4096, 1 row 13.4 and 13.6, 2 rows 14.7 and
     // 13.9 with one; 128 experts of 1536 x 4096, 64 rows, 34.4 and 35.3).  Codes alone gain by two where workgroups are many and share their
     // weights (64 experts, 250 rows: 36.8 and 38.1; 500 rows 37.4 and 39.4) and lose with a row or two each (34.1 and 33.2).  A single quad of K
     // leaves nothing to hide: 8192 rows, 8192 x 384, 71 us with four row blocks, 97 with one.
     const int64_t pieces = offsets ? (M < experts ? M : experts) : (M + 15) / 16, groups = p.NB * pieces, mean = (M + pieces - 1) / pieces;
     int wide = src != kF32 && (groups > 1024 || mean > 4) ? 2 : 1;             // row blocks per streaming workgroup
-    const int64_t own = (groups / wide + cus - 1) / cus * p.KQ * mean;         // quads of rows that a compute unit would quantise
-    if (src != kF32 && (c.shape >= 0 || own > 120)) {
+    const int64_t rounds = (groups / wide + cus - 1) / cus;                    // of workgroups
+    const bool apart = rounds * p.KQ * (mean > 4 ? 20 : mean) > 160;
+    if (src != kF32 && (c.shape >= 0 || apart)) {
         char *codes = p.partial + kPartialBytes, *exponents = codes + up256((size_t)M * (K / 2));
         const lutq_status st = quantize_rows_on(X, src, M, nullptr, M, K, codes, exponents, s);
         if (st != LUTQ_OK) return st;
