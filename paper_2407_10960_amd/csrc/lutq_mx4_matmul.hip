@@ -110,6 +110,58 @@ __device__ __forceinline__ int by_die(int id, int n) {
     return id < per * 8 ? (id & 7) * per + (id >> 3) : id;
 }
 
+// Sixteen rows of Y, WN row blocks wide, from the sums of `row block`, of which `rows` and `blocks` exist.
+// The lanes of a row of X hold four neighbouring sums each, of either row block of a pair.  The two blocks' words are exchanged between
+// neighbouring rows of lanes, so that every lane has sixteen bytes: those of even o of the first block, of odd o of the second.  With four
+// row blocks the lanes of rows i and i + 8 exchange one of their two sixteen bytes as well, and a store writes whole cache lines of
+// eight rows, non-temporal ones: Y would drive the factors, which are read again, out of the caches.  (16384 rows, 28672 x 4096:
+// 966 us with half lines and kept, 954 with whole ones, 923 non-temporal, 904 with both.  Half lines of the small tiles are kept:
+// 512 rows, 4096 x 4096, 12.3 us, non-temporal 12.7.)
+// Lanes whose row or row block does not exist store behind what the descriptor covers, which does nothing: always WN / 2 stores.
+template <int WN, typename F>
+__device__ __forceinline__ void store_rows(F sum, char* y, int rows, int blocks, int N, int bf16) {
+    static_assert(WN % 2 == 0, "row blocks in pairs");
+    constexpr uint32_t kNowhere = 0x7fffffff;
+    const int lane = threadIdx.x & 63, i = lane & 15, o = lane >> 4, at = 16 * (o & 1) + 8 * (o >> 1);
+    const int mine = blocks - (o & 1);
+    const auto to = __builtin_amdgcn_make_buffer_rsrc(y, 0, 0x40000000, 0x00020000);
+    auto pair_of = [&](int r) {
+        const f32x4 a = sum(r), b = sum(r + 1);
+        u32x4 out;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const auto two = __builtin_amdgcn_permlane16_swap(round_pair(a[2 * h], a[2 * h + 1], bf16), round_pair(b[2 * h], b[2 * h + 1], bf16), false, false);
+            out[h] = two[0];
+            out[2 + h] = two[1];
+        }
+        return out;
+    };
+    if constexpr (WN % 4 == 0) {
+        const bool low = i < 8;
+        const uint32_t from = (uint32_t)((i & 7) * N + at) * 2 + (low ? 0 : 64);
+        const uint32_t to1 = (i & 7) < rows ? from : kNowhere, to2 = 8 + (i & 7) < rows ? from + 16 * N : kNowhere;
+#pragma unroll
+        for (int r = 0; r < WN; r += 4) {
+            const u32x4 first = pair_of(r), second = pair_of(r + 2);
+            u32x4 one, two;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) {
+                const uint32_t t = low ? second[h] : first[h];
+                const uint32_t u = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0x128, 0xf, 0xf, true);   // row_ror 8
+                one[h] = low ? first[h] : u;
+                two[h] = low ? u : second[h];
+            }
+            const bool there = r + (low ? 0 : 2) < mine;
+            __builtin_amdgcn_raw_buffer_store_b128(one, to, there ? to1 : kNowhere, r * 32, kNonTemporal);
+            __builtin_amdgcn_raw_buffer_store_b128(two, to, there ? to2 : kNowhere, r * 32, kNonTemporal);
+        }
+    } else {
+        const uint32_t from = i < rows ? (uint32_t)(i * N + at) * 2 : kNowhere;
+#pragma unroll
+        for (int r = 0; r < WN; r += 2) __builtin_amdgcn_raw_buffer_store_b128(pair_of(r), to, r < mine ? from : kNowhere, r * 32, 0);
+    }
+}
+
 // Few rows: a workgroup owns R row blocks of weights and sixteen rows of X over all of K; its wavefronts take the quads in turn, and
 // their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the weights, which go from memory into the operand
 // registers as they lie, all of a quad asked for before X is looked at: 28672 x 4096, 62 MB, 1 row 12.7 us (4.9 TB/s), and 13 rows 14.0; smaller
@@ -253,14 +305,8 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
         }
     }
 
-    auto store = [&](int r, const f32x4& sum) {
-        if (i >= rows || rb0 + r >= p.NB) return;
-        const u32x2 out = {round_pair(sum[0], sum[1], p.bf16), round_pair(sum[2], sum[3], p.bf16)};
-        *reinterpret_cast<u32x2*>(p.y + ((int64_t)(m0 + i) * p.N + 16 * (rb0 + r) + 4 * o) * 2) = out;
-    };
     if constexpr (solo) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) store(r, acc[r]);
+        store_rows<R>([&](int r) { return acc[r]; }, p.y + ((int64_t)m0 * p.N + 16 * rb0) * 2, rows, p.NB - rb0, p.N, p.bf16);
         return;
     }
     __syncthreads();
@@ -271,7 +317,10 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
     for (int r = wave; r < R; r += waves) {
         f32x4 sum = sums[r * 64 + lane];
         for (int v = 1; v < waves; ++v) sum += sums[(v * R + r) * 64 + lane];
-        store(r, sum);
+        if (i < rows && rb0 + r < p.NB) {
+            const u32x2 out = {round_pair(sum[0], sum[1], p.bf16), round_pair(sum[2], sum[3], p.bf16)};
+            *reinterpret_cast<u32x2*>(p.y + ((int64_t)(m0 + i) * p.N + 16 * (rb0 + r) + 4 * o) * 2) = out;
+        }
     }
 }
 
@@ -310,7 +359,6 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
     constexpr int kWaves = Shape::kWaves, kRB = Shape::kRB, kMB = Shape::kMB, kStep = Shape::kStep, kExps = Shape::kExps;
     constexpr int kWLoads = kRB / kWaves, kXLoads = 2 * kMB / kWaves;          // per wavefront: pieces of weights, halves of pieces of X
     constexpr int kLoads = 2 * kWLoads + kXLoads, kStores = WN / 2 * WM;
-    constexpr uint32_t kNowhere = 0x7fffffff;
     // Of a step's copies, those that are asked for in the second half of a step; the others follow in the first half of the next, where
     // the steps are long or many enough for them to arrive in time.
     constexpr int kEarly = DEPTH > 2 || kWaves > 4 ? (2 * kLoads + 2) / 3 : kLoads;
@@ -605,58 +653,12 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
                     for (int b = 0; b < WM; ++b) acc[r][b] = sum[r][b];
             }
         }
-        // The lanes of a row of X hold four neighbouring sums each, of either row block of a pair.  The two blocks' words are exchanged between
-        // neighbouring rows of lanes, so that every lane has sixteen bytes: those of even o of the first block, of odd o of the second.  With four
-        // row blocks the lanes of rows i and i + 8 exchange one of their two sixteen bytes as well, and a store writes whole cache lines of
-        // eight rows, non-temporal ones: Y would drive the factors, which are read again, out of the caches.  (16384 rows, 28672 x 4096:
-        // 966 us with half lines and kept, 954 with whole ones, 923 non-temporal, 904 with both.  Half lines of the small tiles are kept:
-        // 512 rows, 4096 x 4096, 12.3 us, non-temporal 12.7.)
-        // Lanes whose row or row block does not exist store behind what the descriptor covers, which does nothing: so every wavefront has kStores
-        // stores under way, and the next item's first step need not wait for them (8192 rows, 8192 x 2048: 157 -> 154).
-        static_assert(WN % 2 == 0, "row blocks in pairs");
+        // (kStores stores by every wavefront, which the next item's first step need not wait for: 8192 rows, 8192 x 2048, 157 -> 154)
         if (finished) {
-            const int last_rb = p.NB - 1 - it.rb0 - wn * WN - (o & 1);         // the lane's, from the wavefront's first
 #pragma unroll
             for (int b = 0; b < WM; ++b) {
-                const int m = it.m0 + 16 * (wm * WM + b);
-                const auto y = __builtin_amdgcn_make_buffer_rsrc(p.y + ((int64_t)m * p.N + 16 * (it.rb0 + wn * WN)) * 2, 0, 0x40000000, 0x00020000);
-                const int at = 16 * (o & 1) + 8 * (o >> 1);
-                auto pair_of = [&](int r) {
-                    u32x4 out;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const auto two = __builtin_amdgcn_permlane16_swap(round_pair(acc[r][b][2 * h], acc[r][b][2 * h + 1], p.bf16),
-                                                                          round_pair(acc[r + 1][b][2 * h], acc[r + 1][b][2 * h + 1], p.bf16), false, false);
-                        out[h] = two[0];
-                        out[2 + h] = two[1];
-                    }
-                    return out;
-                };
-                if constexpr (WN % 4 == 0) {
-                    const bool low = i < 8;
-                    const uint32_t to = (uint32_t)((i & 7) * p.N + at) * 2 + (low ? 0 : 64);
-                    const uint32_t to1 = m + (i & 7) < it.m1 ? to : kNowhere, to2 = m + 8 + (i & 7) < it.m1 ? to + 16 * p.N : kNowhere;
-#pragma unroll
-                    for (int r = 0; r < WN; r += 4) {
-                        const u32x4 first = pair_of(r), second = pair_of(r + 2);
-                        u32x4 one, two;
-#pragma unroll
-                        for (int h = 0; h < 4; ++h) {
-                            const uint32_t t = low ? second[h] : first[h];
-                            const uint32_t u = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)t, 0x128, 0xf, 0xf, true);   // row_ror 8
-                            one[h] = low ? first[h] : u;
-                            two[h] = low ? u : second[h];
-                        }
-                        const bool there = r + (low ? 0 : 2) <= last_rb;
-                        __builtin_amdgcn_raw_buffer_store_b128(one, y, there ? to1 : kNowhere, r * 32, kNonTemporal);
-                        __builtin_amdgcn_raw_buffer_store_b128(two, y, there ? to2 : kNowhere, r * 32, kNonTemporal);
-                    }
-                } else {
-                    const uint32_t to = m + i < it.m1 ? (uint32_t)(i * p.N + at) * 2 : kNowhere;
-#pragma unroll
-                    for (int r = 0; r < WN; r += 2)
-                        __builtin_amdgcn_raw_buffer_store_b128(pair_of(r), y, r <= last_rb ? to : kNowhere, r * 32, 0);
-                }
+                const int m = it.m0 + 16 * (wm * WM + b), rb = it.rb0 + wn * WN;
+                store_rows<WN>([&](int r) { return acc[r][b]; }, p.y + ((int64_t)m * p.N + 16 * rb) * 2, it.m1 - m, p.NB - rb, p.N, p.bf16);
             }
         }
         stored = finished;
@@ -811,7 +813,7 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     // Two row blocks per workgroup halve it, and leave fewer wavefronts to hide the reads (28672 x 4096, 1 row 13.4 and 13.6, 2 rows 14.7 and
     // 13.9 with one; 128 experts of 1536 x 4096, 64 rows, 34.4 and 35.3).  Codes alone gain by two where workgroups are many and share their
     // weights (64 experts, 250 rows: 36.8 and 38.1; 500 rows 37.4 and 39.4) and lose with a row or two each (34.1 and 33.2).  A single quad of K
-    // leaves nothing to hide: 8192 rows, 8192 x 384, 71 us with four row blocks, 97 with one.
+    // leaves nothing to hide: 8192 rows, 8192 x 384, 97 us with one row block, 71 with four, 60 with whole lines of Y stored.
     const int64_t pieces = offsets ? (M < experts ? M : experts) : (M + 15) / 16, groups = p.NB * pieces, mean = (M + pieces - 1) / pieces;
     int wide = src != kF32 && (groups > 1024 || mean > 4) ? 2 : 1;             // row blocks per streaming workgroup
     const int64_t rounds = (groups / wide + cus - 1) / cus;                    // of workgroups
