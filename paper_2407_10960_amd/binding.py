@@ -593,6 +593,12 @@ def _mx4_bytes(name, *tensors):
             raise TypeError(f"{name}: codes, exponents, packed and workspace must be uint8")
 
 
+def _mx4_has_exponents(name, exponents):
+    """(to the native part a call without exponents is one of the packed form)"""
+    if exponents is None:
+        raise TypeError(f"{name}: exponents must be uint8, [M, K / 32]")
+
+
 def _mx4_source(x, name) -> tuple:
     """(whether it is fp32, dtype code) of dense values."""
     torch = _torch()
@@ -606,6 +612,7 @@ def _mx4_source(x, name) -> tuple:
 def lutq_mx4_quantize(X, codes_out, exponents_out, rows=None, stream=None):
     """Quantises X [., K] (float32, float16, bfloat16) to codes [M, K / 2] and exponent bytes [M, K / 32] (uint8).  With rows
     (int32, [M], on the device) output row m is row rows[m] of X, zeros where that is no row of X."""
+    _mx4_has_exponents("lutq_mx4_quantize", exponents_out)
     if stream is None and _done(_native().mx4_quantize(X, codes_out, exponents_out, rows), "lutq_mx4_quantize"):
         return codes_out, exponents_out
     torch = _torch()
@@ -644,6 +651,7 @@ def lutq_mx4_quantize_packed(W, packed_out, stream=None):
 
 def lutq_mx4_dequant(codes, exponents, X_out, stream=None):
     """X_out [M, K] (float16 or bfloat16) = the values that codes and exponents stand for."""
+    _mx4_has_exponents("lutq_mx4_dequant", exponents)
     if stream is None and _done(_native().mx4_dequant(codes, exponents, X_out), "lutq_mx4_dequant"):
         return X_out
     torch = _torch()
