@@ -28,6 +28,7 @@ struct QuantizeParams {
     uint32_t ku;               // K / 128
     uint32_t magic, shift;     // u / ku = (u * magic) >> shift for u < 2^31
     uint32_t K;
+    uint32_t block0;           // of this launch's workgroups the first
 };
 
 // The dense side, read or written once, is non-temporal: it would drive the codes, which are read soon, out of the caches, and itself does
@@ -48,7 +49,7 @@ __global__ __launch_bounds__(kThreads) void quantize_rows(const QuantizeParams p
     Eight<SRC> x[UNITS];
 #pragma unroll
     for (int t = 0; t < UNITS; ++t) {
-        u[t] = ((uint32_t)blockIdx.x * UNITS + t) * (kThreads / 16) + team;
+        u[t] = ((p.block0 + (uint32_t)blockIdx.x) * UNITS + t) * (kThreads / 16) + team;
         x[t].v[0] = u32x4{0, 0, 0, 0};
         if constexpr (SRC == kF32) x[t].v[1] = u32x4{0, 0, 0, 0};
         if (u[t] >= p.units) continue;
@@ -79,7 +80,8 @@ __global__ __launch_bounds__(kThreads) void quantize_rows(const QuantizeParams p
 template <int SRC>
 __global__ __launch_bounds__(kThreads) void quantize_packed(const QuantizeParams p) {
     const uint32_t j = threadIdx.x & 15u, i = threadIdx.x >> 4, o = j >> 2;
-    const uint32_t quads = (p.ku + 3) >> 2, rb = (uint32_t)(((uint64_t)blockIdx.x * p.magic) >> p.shift), q = blockIdx.x - rb * quads;
+    const uint32_t id = p.block0 + (uint32_t)blockIdx.x;
+    const uint32_t quads = (p.ku + 3) >> 2, rb = (uint32_t)(((uint64_t)id * p.magic) >> p.shift), q = id - rb * quads;
     const int64_t row = (int64_t)rb * 16 + i;
     const uint32_t tiles = min(4u, p.ku - 4 * q);
     Eight<SRC> x[4];
@@ -107,12 +109,13 @@ struct DequantParams {
     int64_t words;             // row form: M * K / 8
     uint32_t ku, magic, shift;
     uint32_t K;
+    uint32_t block0;           // of this launch's workgroups the first
 };
 
 template <bool BF16, int WORDS>
 __global__ __launch_bounds__(kThreads) void dequant_rows(const DequantParams p) {
     uint32_t c[WORDS], e[WORDS];
-    const int64_t first = (int64_t)blockIdx.x * (WORDS * kThreads) + threadIdx.x;
+    const int64_t first = (int64_t)(p.block0 + (uint32_t)blockIdx.x) * (WORDS * kThreads) + threadIdx.x;
 #pragma unroll
     for (int t = 0; t < WORDS; ++t) {
         const int64_t w = first + t * kThreads;
@@ -128,7 +131,8 @@ __global__ __launch_bounds__(kThreads) void dequant_rows(const DequantParams p) 
 template <bool BF16>
 __global__ __launch_bounds__(kThreads) void dequant_packed(const DequantParams p) {
     const uint32_t j = threadIdx.x & 15u, i = threadIdx.x >> 4, o = j >> 2;
-    const uint32_t quads = (p.ku + 3) >> 2, rb = (uint32_t)(((uint64_t)blockIdx.x * p.magic) >> p.shift), q = blockIdx.x - rb * quads;
+    const uint32_t id = p.block0 + (uint32_t)blockIdx.x;
+    const uint32_t quads = (p.ku + 3) >> 2, rb = (uint32_t)(((uint64_t)id * p.magic) >> p.shift), q = id - rb * quads;
     const uint32_t tiles = min(4u, p.ku - 4 * q);
     const char* record = reinterpret_cast<const char*>(p.codes) + rb * p.record;
     const uint32_t word = *reinterpret_cast<const uint32_t*>(record + (int64_t)p.ku * 1024 + q * 256 + (16 * o + i) * 4);
@@ -154,12 +158,22 @@ void division(uint32_t d, uint32_t* magic, uint32_t* shift) {
     *magic = (uint32_t)((uint64_t(1) << (31 + s)) / d + 1);
 }
 
+// A launch has fewer than 2^32 threads, which the largest matrices reach.
+template <typename P, typename F> void in_launches(P p, uint32_t blocks, F launch) {
+    constexpr uint32_t kMost = (uint32_t)((uint64_t(1) << 32) / kThreads) - 1;
+    for (uint32_t at = 0; at < blocks; at += kMost) {
+        p.block0 = at;
+        launch(p, blocks - at < kMost ? blocks - at : kMost);
+    }
+}
+
 lutq_status launched() { return hipGetLastError() == hipSuccess ? LUTQ_OK : LUTQ_ERR_DEVICE; }
 
 template <int SRC> void launch_rows(const QuantizeParams& p, hipStream_t s) {
     // Four units per team where that still leaves work for every compute unit, one where latency is all that counts.
     const uint32_t teams = kThreads / 16;
-    if (p.units >= 4u * teams * 512u) quantize_rows<SRC, 4><<<(p.units + 4 * teams - 1) / (4 * teams), kThreads, 0, s>>>(p);
+    if (p.units >= 4u * teams * 512u)
+        in_launches(p, (p.units + 4 * teams - 1) / (4 * teams), [&](const QuantizeParams& q, uint32_t grid) { quantize_rows<SRC, 4><<<grid, kThreads, 0, s>>>(q); });
     else quantize_rows<SRC, 1><<<(p.units + teams - 1) / teams, kThreads, 0, s>>>(p);
 }
 
@@ -205,12 +219,14 @@ extern "C" lutq_status lutq_mx4_quantize_packed(const void* W, int w_is_f32, lut
     QuantizeParams p{};
     p.x = W; p.codes = static_cast<uint32_t*>(packed_out); p.record = record_bytes(K);
     p.ku = (uint32_t)(K / 128); p.K = (uint32_t)K;
-    const uint32_t quads = (uint32_t)k_quads(K), grid = (uint32_t)(N / 16) * quads;
+    const uint32_t quads = (uint32_t)k_quads(K);
     division(quads, &p.magic, &p.shift);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (w_is_f32) quantize_packed<kF32><<<grid, kThreads, 0, s>>>(p);
-    else if (dtype == LUTQ_F16) quantize_packed<kF16><<<grid, kThreads, 0, s>>>(p);
-    else quantize_packed<kBF16><<<grid, kThreads, 0, s>>>(p);
+    in_launches(p, (uint32_t)(N / 16) * quads, [&](const QuantizeParams& q, uint32_t grid) {
+        if (w_is_f32) quantize_packed<kF32><<<grid, kThreads, 0, s>>>(q);
+        else if (dtype == LUTQ_F16) quantize_packed<kF16><<<grid, kThreads, 0, s>>>(q);
+        else quantize_packed<kBF16><<<grid, kThreads, 0, s>>>(q);
+    });
     return launched();
 }
 
@@ -226,12 +242,14 @@ extern "C" lutq_status lutq_mx4_dequant(const void* codes, const void* exponents
     p.out = static_cast<u32x4*>(X_out); p.words = M * (K / 8);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     const bool many = p.words >= int64_t(4) * kThreads * 1024;
-    const uint32_t per = many ? 4 * kThreads : kThreads, grid = (uint32_t)((p.words + per - 1) / per);
-    if (dtype == LUTQ_BF16) {
-        if (many) dequant_rows<true, 4><<<grid, kThreads, 0, s>>>(p); else dequant_rows<true, 1><<<grid, kThreads, 0, s>>>(p);
-    } else {
-        if (many) dequant_rows<false, 4><<<grid, kThreads, 0, s>>>(p); else dequant_rows<false, 1><<<grid, kThreads, 0, s>>>(p);
-    }
+    const uint32_t per = many ? 4 * kThreads : kThreads;
+    in_launches(p, (uint32_t)((p.words + per - 1) / per), [&](const DequantParams& q, uint32_t grid) {
+        if (dtype == LUTQ_BF16) {
+            if (many) dequant_rows<true, 4><<<grid, kThreads, 0, s>>>(q); else dequant_rows<true, 1><<<grid, kThreads, 0, s>>>(q);
+        } else {
+            if (many) dequant_rows<false, 4><<<grid, kThreads, 0, s>>>(q); else dequant_rows<false, 1><<<grid, kThreads, 0, s>>>(q);
+        }
+    });
     return launched();
 }
 
@@ -243,10 +261,12 @@ extern "C" lutq_status lutq_mx4_dequant_packed(const void* packed, int64_t N, in
     DequantParams p{};
     p.codes = static_cast<const uint32_t*>(packed); p.out = static_cast<u32x4*>(W_out); p.record = record_bytes(K);
     p.ku = (uint32_t)(K / 128); p.K = (uint32_t)K;
-    const uint32_t quads = (uint32_t)k_quads(K), grid = (uint32_t)(N / 16) * quads;
+    const uint32_t quads = (uint32_t)k_quads(K);
     division(quads, &p.magic, &p.shift);
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dtype == LUTQ_BF16) dequant_packed<true><<<grid, kThreads, 0, s>>>(p);
-    else dequant_packed<false><<<grid, kThreads, 0, s>>>(p);
+    in_launches(p, (uint32_t)(N / 16) * quads, [&](const DequantParams& q, uint32_t grid) {
+        if (dtype == LUTQ_BF16) dequant_packed<true><<<grid, kThreads, 0, s>>>(q);
+        else dequant_packed<false><<<grid, kThreads, 0, s>>>(q);
+    });
     return launched();
 }

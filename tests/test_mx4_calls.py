@@ -26,3 +26,25 @@ def test_the_row_form_needs_its_exponents_on_the_device(lutq):
             call()
     torch.cuda.synchronize()
     assert (p == 0xA5).all().item() and (x == 1.0).all().item()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [(1 << 30) - 1, (1 << 30) - 64])
+def test_as_many_picked_rows_as_there_may_be(lutq, M):
+    """Sixteen lanes take four blocks of 128 columns: the largest calls have 2^32 threads and fewer.  64 GiB of codes."""
+    import torch
+    torch.cuda.empty_cache()
+    x = edge_values("bf16", 50, 128, 9)
+    codes, e = mx.quantize(as_f64(x))
+    want_c, want_e = to_gpu(mx.row_bytes(codes)), to_gpu(e)
+    rows = torch.arange(M, dtype=torch.int32, device="cuda")
+    rows.remainder_(50)
+    c, s = torch.empty((M + 4, 64), dtype=torch.uint8, device="cuda"), torch.empty((M + 16, 4), dtype=torch.uint8, device="cuda")
+    c[M - 20000:], s[M - 20000:] = 0xA5, 0xA5
+    lutq.lutq_mx4_quantize(x.cuda(), c[:M], s[:M], rows=rows)
+    for at in (slice(0, 20000), slice(M - 20000, M), slice(1, M, 4999)):
+        r = rows[at].long()
+        assert torch.equal(c[at], want_c[r]) and torch.equal(s[at], want_e[r])
+    assert (c[M:] == 0xA5).all().item() and (s[M:] == 0xA5).all().item()
+    del rows, c, s
+    torch.cuda.empty_cache()
