@@ -35,6 +35,10 @@ __device__ __forceinline__ f32x4 load16_shared(__amdgpu_buffer_rsrc_t from, uint
     return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(from, lane_at, at, kSc1));
 }
 
+// Between what lanes of a wavefront write to LDS and what others of it read there, in either order.  LDS serves a wavefront in order, so this
+// is no instruction: it keeps the compiler, to which each lane is a program of its own, from moving the accesses past each other.
+__device__ __forceinline__ void between_lanes() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local"); }
+
 struct ProductParams {
     const char* x;             // row form: codes; or 16-bit values
     const char* xe;            // row form: exponents
@@ -262,6 +266,7 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
                     if (4 * g < rows) *reinterpret_cast<u32x4*>(place + (4 * g + o) * kPlane + i * 16) = v[t][g];
+                between_lanes();
                 Eight<SRC> block[4];
                 uint32_t a = 0;
 #pragma unroll
@@ -273,6 +278,7 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
 #pragma unroll
                 for (int j = 0; j < 4; ++j) xv[j] = to_codes<SRC>(block[j], power_of(exponent));
                 multiply(t, xv, exponent << (8 * t));
+                between_lanes();
             }
             continue;
         }
@@ -297,12 +303,14 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
                 }
             }
         }
+        between_lanes();
         const uint32_t xe = *reinterpret_cast<const uint32_t*>(exps + lane * 4);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
             if (t >= tiles) break;
             multiply(t, *reinterpret_cast<const u32x4*>(place + (4 * t + o) * kPlane + i * 16), xe);
         }
+        between_lanes();
     }
 
     if constexpr (solo) {
