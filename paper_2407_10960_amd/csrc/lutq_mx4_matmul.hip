@@ -4,6 +4,7 @@
 // The instruction's first operand is the weights, so a lane's four sums are neighbours in a row of Y.
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <type_traits>
 
@@ -691,28 +692,40 @@ int64_t most_pieces(const ProductParams& p, int rows) {
     return p.offsets ? p.M / rows + (p.M < p.experts ? p.M : p.experts) : (p.M + rows - 1) / rows;
 }
 
+// More than 64 KiB of LDS has to be enabled once per kernel and device.
+template <auto KERNEL> hipError_t launch(dim3 grid, int threads, size_t lds, const ProductParams& p, hipStream_t s) {
+    if (lds > 64 * 1024) {
+        static std::atomic<uint64_t> enabled{0};       // one bit per device
+        int device = 0;
+        hipError_t e = hipGetDevice(&device);
+        if (e != hipSuccess) return e;
+        const uint64_t bit = device < 64 ? uint64_t(1) << device : 0;
+        if (!(enabled.load(std::memory_order_relaxed) & bit)) {
+            e = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
+            if (e != hipSuccess) return e;
+            enabled.fetch_or(bit, std::memory_order_relaxed);
+        }
+    }
+    KERNEL<<<grid, threads, lds, s>>>(p);
+    return hipGetLastError();
+}
+
 template <int SRC, int R, int ROWS>
-void launch_stream(ProductParams p, int waves, hipStream_t s) {
+hipError_t launch_stream(ProductParams p, int waves, hipStream_t s) {
     const int nx = (p.NB + R - 1) / R;
     const size_t lds = (size_t)waves * kStreamPlace;
     // (a launch has fewer than 2^16 workgroups along y and 2^32 threads)
     int64_t most = (int64_t(1) << 31) / (int64_t(nx) * waves * 64);
     most = most > 65535 ? 65535 : most;
     const int64_t each = R == 4 ? waves : 1, pieces = most_pieces(p, 16), slots = (pieces + each - 1) / each;
-    for (int64_t at = 0; at < slots; at += most) {
+    hipError_t e = hipSuccess;
+    for (int64_t at = 0; at < slots && e == hipSuccess; at += most) {
         p.slot0 = (int)(at * each);
         const dim3 grid(nx, (unsigned)(slots - at < most ? slots - at : most));
-        if (p.offsets) stream_kernel<SRC, R, ROWS, true><<<grid, waves * 64, lds, s>>>(p);
-        else stream_kernel<SRC, R, ROWS, false><<<grid, waves * 64, lds, s>>>(p);
+        e = p.offsets ? launch<stream_kernel<SRC, R, ROWS, true>>(grid, waves * 64, lds, p, s)
+                      : launch<stream_kernel<SRC, R, ROWS, false>>(grid, waves * 64, lds, p, s);
     }
-}
-
-// The kernel with `lds` bytes of LDS, which may be more than a launch gets unasked.
-template <typename K> hipError_t launch(K kernel, dim3 grid, int threads, int lds, const ProductParams& p, hipStream_t s) {
-    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (e != hipSuccess) return e;
-    kernel<<<grid, threads, lds, s>>>(p);
-    return hipGetLastError();
+    return e;
 }
 
 template <int WN, int WM, int GN, int GM, int DEPTH>
@@ -733,8 +746,8 @@ hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
         auto run = [&](auto once) {
             constexpr bool ONCE = decltype(once)::value;
             const dim3 g((unsigned)grid);
-            return p.offsets ? launch(tile_kernel<WN, WM, GN, GM, DEPTH, true, ONCE>, g, Shape::kThreads, Shape::kLds, p, s)
-                             : launch(tile_kernel<WN, WM, GN, GM, DEPTH, false, ONCE>, g, Shape::kThreads, Shape::kLds, p, s);
+            return p.offsets ? launch<tile_kernel<WN, WM, GN, GM, DEPTH, true, ONCE>>(g, Shape::kThreads, Shape::kLds, p, s)
+                             : launch<tile_kernel<WN, WM, GN, GM, DEPTH, false, ONCE>>(g, Shape::kThreads, Shape::kLds, p, s);
         };
         if constexpr (Shape::kMB <= 8) e = p.once ? run(std::true_type()) : run(std::false_type());
         else e = run(std::false_type());
@@ -841,6 +854,7 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     // several workgroups read the same ones (8 experts of 4096 x 4096, 64 rows: 12.7 and 14.3; 1024 rows, 5120 x 5120: 28.7 and 33.7).
     const int64_t shared = c.shape >= 0 ? (c.shape == 3 || c.shape == 4 ? 64 : 128) : offsets ? 4 : 16;
     p.once = (offsets ? mean : M) <= shared && p.NB * (offsets ? pieces : 1) * p.record > (int64_t(128) << 20);
+    hipError_t e;
     if (c.shape < 0) {
         // Wavefronts of a workgroup: sixteen with one row block, eight with two (their registers) or where they quantise and workgroups are many,
         // four where workgroups are so many that their beginnings count (57344 x 8192, 1 row: 44.2 us with eight, 42.2 with sixteen).
@@ -852,24 +866,23 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
         const int waves = wide == 4 ? (pieces < 4 ? (int)pieces : 4) : p.KQ < most ? p.KQ : most;
         auto by_rows = [&](auto source) {
             constexpr int SRC = decltype(source)::value;
-            if (mean > 4) launch_stream<SRC, 2, 16>(p, waves, s);
-            else if (mean > 1) wide == 2 ? launch_stream<SRC, 2, 4>(p, waves, s) : launch_stream<SRC, 1, 4>(p, waves, s);
-            else wide == 2 ? launch_stream<SRC, 2, 1>(p, waves, s) : launch_stream<SRC, 1, 1>(p, waves, s);
+            if (mean > 4) return launch_stream<SRC, 2, 16>(p, waves, s);
+            if (mean > 1) return wide == 2 ? launch_stream<SRC, 2, 4>(p, waves, s) : launch_stream<SRC, 1, 4>(p, waves, s);
+            return wide == 2 ? launch_stream<SRC, 2, 1>(p, waves, s) : launch_stream<SRC, 1, 1>(p, waves, s);
         };
-        if (src == kF16) by_rows(std::integral_constant<int, kF16>());
-        else if (src == kBF16) by_rows(std::integral_constant<int, kBF16>());
-        else if (wide == 1) launch_stream<kF32, 1, 16>(p, waves, s);
-        else if (wide == 2) launch_stream<kF32, 2, 16>(p, waves, s);
-        else launch_stream<kF32, 4, 16>(p, waves, s);
+        e = src == kF16    ? by_rows(std::integral_constant<int, kF16>())
+            : src == kBF16 ? by_rows(std::integral_constant<int, kBF16>())
+            : wide == 1    ? launch_stream<kF32, 1, 16>(p, waves, s)
+            : wide == 2    ? launch_stream<kF32, 2, 16>(p, waves, s)
+                           : launch_stream<kF32, 4, 16>(p, waves, s);
     } else {
-        const hipError_t e = c.shape == 0   ? launch_tiles<8, 4, 2, 4, 2>(p, 1, cus, s)
-                             : c.shape == 1 ? launch_tiles<4, 4, 2, 2, 2>(p, 1, cus, s)
-                             : c.shape == 2 ? launch_tiles<4, 2, 2, 4, 4>(p, c.slices, cus, s)
-                             : c.shape == 3 ? launch_tiles<2, 2, 4, 2, 4>(p, c.slices, cus, s)
-                                            : launch_tiles<2, 2, 2, 2, 4>(p, c.slices, cus, s);
-        return e == hipSuccess ? LUTQ_OK : LUTQ_ERR_DEVICE;
+        e = c.shape == 0   ? launch_tiles<8, 4, 2, 4, 2>(p, 1, cus, s)
+            : c.shape == 1 ? launch_tiles<4, 4, 2, 2, 2>(p, 1, cus, s)
+            : c.shape == 2 ? launch_tiles<4, 2, 2, 4, 4>(p, c.slices, cus, s)
+            : c.shape == 3 ? launch_tiles<2, 2, 4, 2, 4>(p, c.slices, cus, s)
+                           : launch_tiles<2, 2, 2, 2, 4>(p, c.slices, cus, s);
     }
-    return hipGetLastError() == hipSuccess ? LUTQ_OK : LUTQ_ERR_DEVICE;
+    return e == hipSuccess ? LUTQ_OK : LUTQ_ERR_DEVICE;
 }
 
 }  // namespace

@@ -48,3 +48,17 @@ def test_as_many_picked_rows_as_there_may_be(lutq, M):
     assert (c[M:] == 0xA5).all().item() and (s[M:] == 0xA5).all().item()
     del rows, c, s
     torch.cuda.empty_cache()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dense", [False, True])
+@pytest.mark.parametrize("M", [1, 4, 16])
+@pytest.mark.parametrize("K", [7168, 7680, 8192, 16384])
+def test_a_wavefront_per_quad_up_to_sixteen(lutq, K, M, dense):
+    """With one row block per workgroup: fourteen wavefronts have 63 KiB of LDS, fifteen and sixteen more than 64."""
+    p = Problem(lutq, M, 48, K, "bf16")
+    x, e = p.args(dense)
+    y = p.out()
+    lutq.lutq_mx4_matmul(x, p.packed, y, p.ws, x_scales=e)
+    got, sums = as_f64(y), mx.product(p.x, p.w[0])
+    assert (np.abs(got - sums[0]) <= off_by_at_most(got, sums, K, "bf16")).all() and p.guards_hold()
