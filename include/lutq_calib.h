@@ -58,6 +58,15 @@ int lutq_calib_route(int bits, int group_size, int64_t M, int64_t N, int64_t K, 
 int lutq_calib_plan(int bits, int group_size, int64_t M, int64_t N, int64_t K, int dtype, int compute_units,
                     size_t workspace_bytes, const lutq_plan* plan, int row_tables, lutq_plan* runs);
 
+/* How lutq_mx4_matmul (experts 0) or lutq_mx4_matmul_grouped (experts >= 1) is launched for M >= 1 rows, as codes (x_is_codes) or 16-bit values,
+ * on a device with `compute_units` compute units (1..4096).  Host logic only, no device is touched.
+ *   launch[0] = 1 if a launch of its own quantises X first;  [1], [2] = output channels and rows of Y that a workgroup makes at a time (streamed
+ *   with the rows of a wavefront each where that is 64 by 16);  [3] = wavefronts of a workgroup;  [4] = steps of K there is room for in
+ *   LDS, 0: the weights are streamed through registers;  [5] = slices of K;  [6] = rows of X that are quantised at a time in the same
+ *   launch (0: none);  [7] = 1 if the weights are read past the caches.
+ * Return values: 0, 1 (launch NULL) or 4 (shape, M < 1 or compute units out of range). */
+int lutq_calib_mx4_launch(int64_t M, int64_t N, int64_t K, int64_t experts, int x_is_codes, int compute_units, int launch[8]);
+
 #ifdef __cplusplus
 }
 #endif

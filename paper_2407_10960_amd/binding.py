@@ -15,7 +15,7 @@ _NATIVE = None       # _lutq_torch: plain calls on the current stream (see _nati
 EXPORTED_SYMBOLS = (
     "lutq_status_string", "lutq_packed_bytes", "lutq_pack", "lutq_unpack", "lutq_workspace_bytes",
     "lutq_plan_default", "lutq_plan_default_for", "lutq_plan_check", "lutq_pack_layout", "lutq_plan_table_set", "lutq_plan_table_lookup", "lutq_matmul", "lutq_matmul_plan", "lutq_matmul_static", "lutq_matmul_channel", "lutq_matmul_pairs", "lutq_matmul_quads", "lutq_tune", "lutq_tune_candidates", "lutq_quantize", "lutq_dequant",
-    "lutq_calib_stream_read", "lutq_calib_copy", "lutq_calib_matmul_trace", "lutq_calib_route", "lutq_calib_plan",
+    "lutq_calib_stream_read", "lutq_calib_copy", "lutq_calib_matmul_trace", "lutq_calib_route", "lutq_calib_plan", "lutq_calib_mx4_launch",
     "lutq_mx4_packed_bytes", "lutq_mx4_pack", "lutq_mx4_unpack", "lutq_mx4_quantize", "lutq_mx4_quantize_packed", "lutq_mx4_dequant",
     "lutq_mx4_dequant_packed", "lutq_mx4_workspace_bytes", "lutq_mx4_matmul", "lutq_mx4_matmul_grouped",
 )
@@ -139,6 +139,8 @@ def load_library():
     lib.lutq_calib_route.argtypes = [ci, ci, i64, i64, i64, ci, ci, sz, ctypes.POINTER(ctypes.c_int)]
     lib.lutq_calib_plan.restype = ci
     lib.lutq_calib_plan.argtypes = [ci, ci, i64, i64, i64, ci, ci, sz, ctypes.POINTER(_CPlan), ci, ctypes.POINTER(_CPlan)]
+    lib.lutq_calib_mx4_launch.restype = ci
+    lib.lutq_calib_mx4_launch.argtypes = [i64, i64, i64, i64, ci, ci, ctypes.POINTER(ctypes.c_int)]
     lib.lutq_mx4_packed_bytes.restype = sz
     lib.lutq_mx4_packed_bytes.argtypes = [i64, i64]
     lib.lutq_mx4_workspace_bytes.restype = sz
@@ -766,6 +768,26 @@ def calib_plan(bits: int, group_size: int, M: int, N: int, K: int, dtype_code: i
                                           ctypes.byref(runs)), "lutq_calib_plan")
     return Plan(runs.row_blocks_per_wave, runs.grid, runs.waves_per_workgroup, runs.tiles_in_flight,
                 runs.row_groups_per_workgroup, runs.scheduling, runs.tiles_per_item)
+
+
+@dataclass(frozen=True)
+class Mx4Launch:
+    """How a microscaled product is launched (include/lutq_calib.h)."""
+    quantised_first: bool
+    channels: int
+    rows: int
+    waves: int
+    room: int                  # steps of K in LDS; 0: streamed
+    slices: int
+    rows_quantised: int
+    past_caches: bool
+
+
+def calib_mx4_launch(M: int, N: int, K: int, experts: int = 0, codes: bool = False, compute_units: int = 256) -> Mx4Launch:
+    """The launch of lutq_mx4_matmul (experts 0) or lutq_mx4_matmul_grouped.  Host logic, no device needed."""
+    r = (ctypes.c_int * 8)()
+    _check(load_library().lutq_calib_mx4_launch(M, N, K, experts, int(codes), compute_units, r), "lutq_calib_mx4_launch")
+    return Mx4Launch(bool(r[0]), r[1], r[2], r[3], r[4], r[5], r[6], bool(r[7]))
 
 
 TRACE_STAMPS = ("start", "arguments arrived", "first loads issued", "table built", "first tile multiplied",

@@ -9,6 +9,7 @@
 #include <type_traits>
 
 #include "lutq.h"
+#include "lutq_calib.h"
 #include "lutq_layout.hpp"
 #include "lutq_mx4_device.hpp"
 
@@ -688,9 +689,10 @@ bool aligned(const void* p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 size_t up256(size_t n) { return (n + 255) & ~size_t(255); }
 
 // How many pieces of ROWS rows there can be: by expert, at most one short one for each that has rows.
-int64_t most_pieces(const ProductParams& p, int rows) {
-    return p.offsets ? p.M / rows + (p.M < p.experts ? p.M : p.experts) : (p.M + rows - 1) / rows;
+int64_t most_pieces(int64_t M, int64_t experts, int rows) {
+    return experts ? M / rows + (M < experts ? M : experts) : (M + rows - 1) / rows;
 }
+int64_t most_pieces(const ProductParams& p, int rows) { return most_pieces(p.M, p.offsets ? p.experts : 0, rows); }
 
 // More than 64 KiB of LDS has to be enabled once per kernel and device.
 template <auto KERNEL> hipError_t launch(dim3 grid, int threads, size_t lds, const ProductParams& p, hipStream_t s) {
@@ -728,21 +730,23 @@ hipError_t launch_stream(ProductParams p, int waves, hipStream_t s) {
     return e;
 }
 
-template <int WN, int WM, int GN, int GM, int DEPTH>
-hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
+// Output channels and rows of a tile, wavefronts, and steps of room, by shape.
+struct TileSize { int channels, rows, waves, room; };
+constexpr TileSize kTiles[] = {{256, 256, 8, 2}, {128, 128, 4, 2}, {128, 128, 8, 4}, {128, 64, 8, 4}, {64, 64, 4, 4}};
+
+template <int SHAPE, int WN, int WM, int GN, int GM, int DEPTH>
+hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
     using Shape = TileShape<WN, WM, GN, GM, DEPTH>;
+    static_assert(kTiles[SHAPE].channels == 16 * Shape::kRB && kTiles[SHAPE].rows == 16 * Shape::kMB && kTiles[SHAPE].waves == Shape::kWaves &&
+                  kTiles[SHAPE].room == DEPTH, "as the choice knows it");
     constexpr int kAtOnce = 160 * 1024 / Shape::kLds < 8 / Shape::kWaves ? 160 * 1024 / Shape::kLds : 8 / Shape::kWaves;   // per compute unit
     const int64_t nx = (p.NB + Shape::kRB - 1) / Shape::kRB, pieces = most_pieces(p, 16 * Shape::kMB);
-    // slices that the workspace has room for, of a quad at least
-    slices = !Shape::kSlices ? 1 : slices < p.KQ ? slices : p.KQ;
-    while (slices > 1 && (nx * pieces > kCounters || nx * pieces * slices * Shape::kSums > (int64_t)kPartialBytes)) --slices;
-    p.slices = slices;
-    const int64_t most = (int64_t(1) << 30) / (nx * slices);                   // pieces of rows per launch: tiles are counted in 32 bits
+    const int64_t most = (int64_t(1) << 30) / (nx * p.slices);                 // pieces of rows per launch: tiles are counted in 32 bits
     hipError_t e = hipSuccess;
     for (int64_t at = 0; at < pieces && e == hipSuccess; at += most) {
         p.slot0 = (int)at;
         p.slots = (int)(pieces - at < most ? pieces - at : most);
-        const int64_t items = nx * p.slots * slices, grid = items < (int64_t)cus * kAtOnce ? items : (int64_t)cus * kAtOnce;
+        const int64_t items = nx * p.slots * p.slices, grid = items < (int64_t)cus * kAtOnce ? items : (int64_t)cus * kAtOnce;
         auto run = [&](auto once) {
             constexpr bool ONCE = decltype(once)::value;
             const dim3 g((unsigned)grid);
@@ -772,7 +776,7 @@ hipError_t launch_tiles(ProductParams p, int slices, int cus, hipStream_t s) {
 // By expert the number of pieces is not known here: every expert is taken to have the mean number of rows and half a piece that is not full.
 struct TileChoice { int shape, slices; };             // shape -1: streamed
 
-TileChoice choose_kernel(int64_t M, int64_t NB, int64_t KT, int64_t experts, int64_t record, int cus) {
+TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int64_t record, int cus) {
     const double S = (double)((KT + 1) / 2);
     const int64_t KQ = (KT + 3) / 4;
     TileChoice best{-1, 1};
@@ -800,7 +804,70 @@ TileChoice choose_kernel(int64_t M, int64_t NB, int64_t KT, int64_t experts, int
         if (z == 1 || t3 * z <= cus) consider(3, z, 3.2 + rounds(t3 * z) * (0.50 * steps + 0.7) + (z > 1 ? 3.0 + 0.8 * z : 0.0));
         if (z == 1 || t4 * z <= 2 * cus) consider(4, z, 3.0 + pairs(rounds(t4 * z), 0.37 * steps + 0.9, 0.62 * steps + 0.9) + (z > 1 ? 1.8 + 1.0 * z : 0.0));
     }
+    if (best.slices > 1) {                             // as many as the workspace has room for
+        const TileSize t = kTiles[best.shape];
+        const int64_t most = (NB * 16 + t.channels - 1) / t.channels * most_pieces(M, experts, t.rows);
+        while (best.slices > 1 && (most > kCounters || most * best.slices * t.channels * t.rows * 4 > (int64_t)kPartialBytes)) --best.slices;
+    }
     return best;
+}
+
+// How a product is launched.
+struct Choice {
+    TileChoice tiles;
+    bool apart;                // X of 16 bits is quantised by a launch of its own
+    bool once;                 // weights past the caches
+    // streamed:
+    int wide;                  // row blocks per workgroup
+    int rows;                  // of X that are quantised at a time, 0: X is codes
+    int waves;                 // per workgroup
+};
+
+// `experts`: 0 without.
+Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int64_t record, bool codes, int cus) {
+    Choice c{};
+    const int KQ = (int)((KT + 3) / 4);
+    c.tiles = choose_tiles(M, NB, KT, experts, record, cus);
+    // Where the streaming workgroups quantise X on the way in, every one of them does it for all its rows.  Up to four rows, beyond some 160 rows
+    // and quads per compute unit that takes longer than a launch which does it once (us, so and with that launch: 4096 x 14336, 1 row (28) 8.7
+    // and 10.5; 28672 x 4096, 4 rows (128) 14.9 and 15.4; 512 x 16384, 4 rows (128) 6.2 and 7.1; 4096 x 14336, 6 rows (168) 14.4 and 11.2).  More
+    // rows cost the same however many they are, like twenty (16 rows, 4096 x 4096 (8 quads) 6.3 and 6.8, 6144 x 4096 (8) 7.2 and 8.2; 6 rows,
+    // 1024 x 8192 (16) 7.5 and 6.5, 13824 x 5120 (20) 14.4 and 12.4; 211 rows through 41 experts of 288 x 640 (4) 5.9 and 6.8).
+    // Two row blocks per workgroup halve it, and leave fewer wavefronts to hide the reads (28672 x 4096, 1 row 13.4 and 13.6, 2 rows 14.7 and
+    // 13.9 with one; 128 experts of 1536 x 4096, 64 rows, 34.4 and 35.3).  Codes alone gain by two where workgroups are many and share their
+    // weights (64 experts, 250 rows: 36.8 and 38.1; 500 rows 37.4 and 39.4) and lose with a row or two each (34.1 and 33.2).  A single quad of K
+    // leaves nothing to hide: 8192 rows, 8192 x 384, 97 us with one row block, 71 with four, 60 with whole lines of Y stored.
+    const int64_t pieces = experts ? (M < experts ? M : experts) : (M + 15) / 16, groups = NB * pieces, mean = (M + pieces - 1) / pieces;
+    int wide = !codes && (groups > 1024 || mean > 4) ? 2 : 1;
+    const int64_t rounds = (groups / wide + cus - 1) / cus;                    // of workgroups
+    const bool apart = rounds * KQ * (mean > 4 ? 20 : mean) > 160;
+    c.apart = !codes && (c.tiles.shape >= 0 || apart);
+    if (c.apart) {
+        codes = true;
+        wide = 1;
+    }
+    if (codes && groups > (experts ? 2048 : 4096)) wide = KQ == 1 ? 4 : mean > 2 ? 2 : 1;
+    // Weights that are read once and take more than half of the 256 MB cache are read past it (57344 x 8192, 250 MB, 1 row:
+    // 44.9 us, so 38.9; 64 experts of 2816 x 2048, 250 rows: 34.1 and 31.2; of 1536 x 4096, 1100 rows: 52.4 and 48.5).  Smaller ones may still be
+    // there at the next call: 28672 x 4096, three in turn, 13 rows 13.1, past the cache 14.7, though of nine in turn 14.1 and 13.6.  Nor where
+    // several workgroups read the same ones (8 experts of 4096 x 4096, 64 rows: 12.7 and 14.3; 1024 rows, 5120 x 5120: 28.7 and 33.7).
+    const int64_t shared = c.tiles.shape >= 0 ? (c.tiles.shape == 3 || c.tiles.shape == 4 ? 64 : 128) : experts ? 4 : 16;
+    c.once = (experts ? mean : M) <= shared && NB * (experts ? pieces : 1) * record > (int64_t(128) << 20);
+    // Wavefronts of a workgroup: sixteen with one row block, eight with two (their registers) or where they quantise and workgroups are many,
+    // four where workgroups are so many that their beginnings count (57344 x 8192, 1 row: 44.2 us with eight, 42.2 with sixteen).
+    // By expert, where X is codes, four from fewer workgroups on, and fewer with two quads each where there are very many, as some
+    // find that there is nothing for them, and the others lie all over the weights (65 experts of 720 x 6272, 35 rows: 13.2 with thirteen, 9.6
+    // with four; 50 of 3376 x 2688, 28 rows: 7.4 with four, 6.2 with three; 41 of 480 x 1408, 40 rows: 4.2 with three, 4.5 with two).
+    const int many = groups > 2048 ? (KQ < 4 ? 2 : KQ < 8 ? KQ / 2 : 4) : 4;
+    const int most = experts && codes && groups > 900 ? many : groups > 4096 ? 4 : wide > 1 || (!codes && groups > 512) ? 8 : 16;
+    c.waves = wide == 4 ? (pieces < 4 ? (int)pieces : 4) : KQ < most ? KQ : most;
+    c.wide = wide;
+    c.rows = codes ? 0 : mean > 4 ? 16 : mean > 1 ? 4 : 1;
+    return c;
+}
+
+template <int R, int ROWS> hipError_t launch_stream_of(int src, const ProductParams& p, int waves, hipStream_t s) {
+    return src == kF16 ? launch_stream<kF16, R, ROWS>(p, waves, s) : launch_stream<kBF16, R, ROWS>(p, waves, s);
 }
 
 lutq_status product_on(const void* X, const void* xe, const void* packed, const int32_t* offsets, int64_t experts, int64_t M,
@@ -825,62 +892,30 @@ lutq_status product_on(const void* X, const void* xe, const void* packed, const 
     int src = xe ? kF32 : dtype == LUTQ_F16 ? kF16 : kBF16;
     const int cus = compute_units();
     if (cus < 1) return LUTQ_ERR_DEVICE;
-    const TileChoice c = choose_kernel(M, p.NB, p.KT, offsets ? experts : 0, p.record, cus);
-    // Where the streaming workgroups quantise X on the way in, every one of them does it for all its rows.  Up to four rows, beyond some 160 rows
-    // and quads per compute unit that takes longer than a launch which does it once (us, so and with that launch: 4096 x 14336, 1 row (28) 8.7
-    // and 10.5; 28672 x 4096, 4 rows (128) 14.9 and 15.4; 512 x 16384, 4 rows (128) 6.2 and 7.1; 4096 x 14336, 6 rows (168) 14.4 and 11.2).  More
-    // rows cost the same however many they are, like twenty (16 rows, 4096 x 4096 (8 quads) 6.3 and 6.8, 6144 x 4096 (8) 7.2 and 8.2; 6 rows,
-    // 1024 x 8192 (16) 7.5 and 6.5, 13824 x 5120 (20) 14.4 and 12.4; 211 rows through 41 experts of 288 x 640 (4) 5.9 and 6.8).
-    // Two row blocks per workgroup halve it, and leave fewer wavefronts to hide the reads (28672 x 4096, 1 row 13.4 and 13.6, 2 rows 14.7 and
-    // 13.9 with one; 128 experts of 1536 x 4096, 64 rows, 34.4 and 35.3).  Codes alone gain by two where workgroups are many and share their
-    // weights (64 experts, 250 rows: 36.8 and 38.1; 500 rows 37.4 and 39.4) and lose with a row or two each (34.1 and 33.2).  A single quad of K
-    // leaves nothing to hide: 8192 rows, 8192 x 384, 97 us with one row block, 71 with four, 60 with whole lines of Y stored.
-    const int64_t pieces = offsets ? (M < experts ? M : experts) : (M + 15) / 16, groups = p.NB * pieces, mean = (M + pieces - 1) / pieces;
-    int wide = src != kF32 && (groups > 1024 || mean > 4) ? 2 : 1;             // row blocks per streaming workgroup
-    const int64_t rounds = (groups / wide + cus - 1) / cus;                    // of workgroups
-    const bool apart = rounds * p.KQ * (mean > 4 ? 20 : mean) > 160;
-    if (src != kF32 && (c.shape >= 0 || apart)) {
+    const Choice c = choose(M, p.NB, p.KT, offsets ? experts : 0, p.record, xe != nullptr, cus);
+    if (c.apart) {
         char *codes = p.partial + kPartialBytes, *exponents = codes + up256((size_t)M * (K / 2));
         const lutq_status st = quantize_rows_on(X, src, M, nullptr, M, K, codes, exponents, s);
         if (st != LUTQ_OK) return st;
         p.x = codes; p.xe = exponents;
         src = kF32;
-        wide = 1;
     }
-    if (src == kF32 && groups > (offsets ? 2048 : 4096)) wide = p.KQ == 1 ? 4 : mean > 2 ? 2 : 1;
-    // Weights that are read once and take more than half of the 256 MB cache are read past it (57344 x 8192, 250 MB, 1 row:
-    // 44.9 us, so 38.9; 64 experts of 2816 x 2048, 250 rows: 34.1 and 31.2; of 1536 x 4096, 1100 rows: 52.4 and 48.5).  Smaller ones may still be
-    // there at the next call: 28672 x 4096, three in turn, 13 rows 13.1, past the cache 14.7, though of nine in turn 14.1 and 13.6.  Nor where
-    // several workgroups read the same ones (8 experts of 4096 x 4096, 64 rows: 12.7 and 14.3; 1024 rows, 5120 x 5120: 28.7 and 33.7).
-    const int64_t shared = c.shape >= 0 ? (c.shape == 3 || c.shape == 4 ? 64 : 128) : offsets ? 4 : 16;
-    p.once = (offsets ? mean : M) <= shared && p.NB * (offsets ? pieces : 1) * p.record > (int64_t(128) << 20);
+    p.once = c.once;
+    p.slices = c.tiles.slices;
     hipError_t e;
-    if (c.shape < 0) {
-        // Wavefronts of a workgroup: sixteen with one row block, eight with two (their registers) or where they quantise and workgroups are many,
-        // four where workgroups are so many that their beginnings count (57344 x 8192, 1 row: 44.2 us with eight, 42.2 with sixteen).
-        // By expert, where X is codes, four from fewer workgroups on, and fewer with two quads each where there are very many, as some
-        // find that there is nothing for them, and the others lie all over the weights (65 experts of 720 x 6272, 35 rows: 13.2 with thirteen, 9.6
-        // with four; 50 of 3376 x 2688, 28 rows: 7.4 with four, 6.2 with three; 41 of 480 x 1408, 40 rows: 4.2 with three, 4.5 with two).
-        const int many = groups > 2048 ? (p.KQ < 4 ? 2 : p.KQ < 8 ? p.KQ / 2 : 4) : 4;
-        const int most = offsets && src == kF32 && groups > 900 ? many : groups > 4096 ? 4 : wide > 1 || (src != kF32 && groups > 512) ? 8 : 16;
-        const int waves = wide == 4 ? (pieces < 4 ? (int)pieces : 4) : p.KQ < most ? p.KQ : most;
-        auto by_rows = [&](auto source) {
-            constexpr int SRC = decltype(source)::value;
-            if (mean > 4) return launch_stream<SRC, 2, 16>(p, waves, s);
-            if (mean > 1) return wide == 2 ? launch_stream<SRC, 2, 4>(p, waves, s) : launch_stream<SRC, 1, 4>(p, waves, s);
-            return wide == 2 ? launch_stream<SRC, 2, 1>(p, waves, s) : launch_stream<SRC, 1, 1>(p, waves, s);
-        };
-        e = src == kF16    ? by_rows(std::integral_constant<int, kF16>())
-            : src == kBF16 ? by_rows(std::integral_constant<int, kBF16>())
-            : wide == 1    ? launch_stream<kF32, 1, 16>(p, waves, s)
-            : wide == 2    ? launch_stream<kF32, 2, 16>(p, waves, s)
-                           : launch_stream<kF32, 4, 16>(p, waves, s);
-    } else {
-        e = c.shape == 0   ? launch_tiles<8, 4, 2, 4, 2>(p, 1, cus, s)
-            : c.shape == 1 ? launch_tiles<4, 4, 2, 2, 2>(p, 1, cus, s)
-            : c.shape == 2 ? launch_tiles<4, 2, 2, 4, 4>(p, c.slices, cus, s)
-            : c.shape == 3 ? launch_tiles<2, 2, 4, 2, 4>(p, c.slices, cus, s)
-                           : launch_tiles<2, 2, 2, 2, 4>(p, c.slices, cus, s);
+    switch (c.tiles.shape) {
+        case 0: e = launch_tiles<0, 8, 4, 2, 4, 2>(p, cus, s); break;
+        case 1: e = launch_tiles<1, 4, 4, 2, 2, 2>(p, cus, s); break;
+        case 2: e = launch_tiles<2, 4, 2, 2, 4, 4>(p, cus, s); break;
+        case 3: e = launch_tiles<3, 2, 2, 4, 2, 4>(p, cus, s); break;
+        case 4: e = launch_tiles<4, 2, 2, 2, 2, 4>(p, cus, s); break;
+        default:
+            if (c.rows == 0) e = c.wide == 1   ? launch_stream<kF32, 1, 16>(p, c.waves, s)
+                                 : c.wide == 2 ? launch_stream<kF32, 2, 16>(p, c.waves, s)
+                                               : launch_stream<kF32, 4, 16>(p, c.waves, s);
+            else if (c.rows == 16) e = launch_stream_of<2, 16>(src, p, c.waves, s);
+            else if (c.rows == 4) e = c.wide == 2 ? launch_stream_of<2, 4>(src, p, c.waves, s) : launch_stream_of<1, 4>(src, p, c.waves, s);
+            else e = c.wide == 2 ? launch_stream_of<2, 1>(src, p, c.waves, s) : launch_stream_of<1, 1>(src, p, c.waves, s);
     }
     return e == hipSuccess ? LUTQ_OK : LUTQ_ERR_DEVICE;
 }
@@ -907,4 +942,16 @@ extern "C" lutq_status lutq_mx4_matmul_grouped(const void* X, const void* x_expo
                                                void* workspace, size_t workspace_bytes, void* stream) {
     if (M > 0 && !offsets) return LUTQ_ERR_NULL;
     return product_on(X, x_exponents, packed, offsets, experts, M, N, K, dtype, Y, workspace, workspace_bytes, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int lutq_calib_mx4_launch(int64_t M, int64_t N, int64_t K, int64_t experts, int x_is_codes, int compute_units, int* launch) {
+    if (!launch) return LUTQ_ERR_NULL;
+    if (experts < 0 || lutq_mx4_workspace_bytes(M, N, K, experts ? experts : 1) == 0 || M < 1 || compute_units < 1 || compute_units > 4096)
+        return LUTQ_ERR_SHAPE;
+    const Choice c = choose(M, N / 16, k_tiles(K), experts, record_bytes(K), x_is_codes != 0, compute_units);
+    const bool streamed = c.tiles.shape < 0;
+    const TileSize t = streamed ? TileSize{16 * c.wide, 16, c.waves, 0} : kTiles[c.tiles.shape];
+    const int out[8] = {c.apart, t.channels, t.rows, t.waves, t.room, c.tiles.slices, streamed ? c.rows : 0, c.once && c.tiles.shape != 0};
+    for (int i = 0; i < 8; ++i) launch[i] = out[i];
+    return LUTQ_OK;
 }
