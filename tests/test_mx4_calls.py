@@ -62,3 +62,29 @@ def test_a_wavefront_per_quad_up_to_sixteen(lutq, K, M, dense):
     lutq.lutq_mx4_matmul(x, p.packed, y, p.ws, x_scales=e)
     got, sums = as_f64(y), mx.product(p.x, p.w[0])
     assert (np.abs(got - sums[0]) <= off_by_at_most(got, sums, K, "bf16")).all() and p.guards_hold()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dense", [False, True])
+@pytest.mark.parametrize("counts", [[2, 0, 5, 1], [40, 0, 7, 23, 16], [300, 0, 129, 60]])
+def test_by_expert_with_and_without_the_native_part(lutq, monkeypatch, counts, dense):
+    """The values of either path, and the same bits."""
+    import torch
+    off = counts_to_offsets(counts, 1)
+    p = Problem(lutq, int(off[-1]) + 2, 272, 640, "bf16", experts=len(counts))
+    x, e = p.args(dense)
+    sums, results, offsets = grouped_reference(p, off), [], to_gpu(off)
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(lutq.binding, "_NATIVE", lutq.binding._NoNative)
+        y = p.out()
+        lutq.lutq_mx4_matmul_grouped(x, p.packed, offsets, y, p.ws, x_scales=e)
+        assert (np.abs(as_f64(y) - sums[0]) <= off_by_at_most(as_f64(y), sums, 640, "bf16")).all() and p.guards_hold()
+        results.append(y)
+    assert torch.equal(*results)
+    side = torch.cuda.Stream()                          # (a given stream is served by the shared path)
+    y = p.out()
+    side.wait_stream(torch.cuda.current_stream())
+    lutq.lutq_mx4_matmul_grouped(x, p.packed, offsets, y, p.ws, x_scales=e, stream=side)
+    side.synchronize()
+    assert torch.equal(y, results[0])
