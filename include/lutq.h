@@ -438,7 +438,8 @@ lutq_status lutq_mx4_dequant_packed(const void* packed, int64_t N, int64_t K, lu
 /* Bytes of device scratch of the products below for up to M rows; experts = 1 for lutq_mx4_matmul.  0 if unsupported. */
 size_t lutq_mx4_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t experts);
 
-/* Y[m, n] = sum_k X[m, k] * W[n, k] over the 4-bit values of both, accumulated in fp32, rounded once to `dtype`.
+/* Y[m, n] = sum_k X[m, k] * W[n, k] over the 4-bit values of both, accumulated in fp32 (subnormal sums are kept, sums beyond its
+ * largest number are infinite), rounded once to `dtype`.
  *   X, x_exponents   device: the row form of the activations; or, x_exponents NULL, activations [M, K] of `dtype`, which
  *                    are quantised on the way in, to what lutq_mx4_quantize would make of them
  *   packed           device, the packed form of W [N, K]

@@ -5,6 +5,7 @@ import pytest
 from gpu_util import torch_dtype
 from oracle import mx4_oracle as mx
 from test_mx4 import Problem, as_f64, counts_to_offsets, edge_values, grouped_reference, off_by_at_most, to_gpu
+from test_mx4_launches import Factors, pack_on_device, values_on_device
 
 
 def test_the_row_form_needs_its_exponents(lutq):
@@ -88,3 +89,44 @@ def test_by_expert_with_and_without_the_native_part(lutq, monkeypatch, counts, d
     lutq.lutq_mx4_matmul_grouped(x, p.packed, offsets, y, p.ws, x_scales=e, stream=side)
     side.synchronize()
     assert torch.equal(y, results[0])
+
+
+def opposite_exponents(M, N, K, dtype, power, top, seed):
+    """Factors whose exponent bytes are anything from 0 to `top`, block by block, one as large as the other is small: every product of two
+    codes is some 2^power times what the codes stand for."""
+    import torch
+    p = Factors(M, N, K, 0, dtype, seed)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed + 1000)
+    x = torch.randint(0, top + 1, (K // 32,), generator=g, device="cuda")
+    x[::3] = torch.tensor([0, 1, 2, top - 2, top - 1, top], device="cuda").repeat(K)[:x[::3].numel()]
+    jitter = torch.randint(-3, 1, (N, K // 32), generator=g, device="cuda")
+    p.e = x.to(torch.uint8).repeat(M, 1)
+    p.w = [(p.w[0][0], (254 + power - x + jitter).clamp(0, 254).to(torch.uint8))]
+    # (where the clamp at 0 or 254 has moved a block, its products are larger or smaller: zero codes where they are too large)
+    larger = (p.w[0][1].long() + x - 254 > power).repeat_interleave(16, 1)
+    p.w[0][0][larger] = 0
+    p.packed = pack_on_device(*p.w[0])
+    p.X = values_on_device(p.codes, p.e).to(torch_dtype(dtype))
+    return p
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(1, 48, 640), (3, 48, 1152), (13, 272, 640), (33, 304, 640), (8, 64, 128), (17, 29120, 640), (17, 29216, 512),
+                                   (65, 16928, 1152), (17, 10768, 6784), (130, 49296, 896), (49, 5312, 5248)])
+@pytest.mark.parametrize("dtype,power", [("bf16", -140), ("bf16", -3), ("bf16", 105), ("f16", -24), ("f16", -1)])
+def test_exponents_from_end_to_end(lutq, M, N, K, dtype, power):
+    """Streamed and tiled, an odd number of tiles of K and slices among them.  Sums down to the last place of fp32, and below the type's
+    smallest normal number: none is flushed.  (A sum that fp32 holds as a subnormal number is off by at most its quantum, 2^-149, an addition.)"""
+    import torch
+    ws = lutq.new_mx4_workspace(M, N, K)
+    for as_codes in ((True, False) if dtype == "bf16" else (True,)):    # (bf16 values hold 6 2^(e - 127) up to e = 252)
+        p = opposite_exponents(M, N, K, dtype, power, 254 if as_codes else 252, M + K)
+        y = torch.full((M, N), 7.0, dtype=torch_dtype(dtype), device="cuda")
+        x, e = p.args(as_codes)
+        assert as_codes or x.isfinite().all().item()
+        lutq.lutq_mx4_matmul(x, p.packed, y, ws, x_scales=e)
+        worst = p.worst(y, 0, M, 0, 2.0 ** -149)
+        assert worst <= 1.0, (as_codes, worst)
+        assert y.any().item() or power == -24
+        assert power != -140 or (y.abs() < 2.0 ** -126).any().item()

@@ -163,15 +163,15 @@ class Factors:
     def args(self, codes):
         return (self.codes, self.e) if codes else (self.X, None)
 
-    def worst(self, got, a, b, expert):
-        """Largest error of rows a .. b of a result in units of its bound."""
+    def worst(self, got, a, b, expert, quantum=0.0):
+        """Largest error of rows a .. b of a result in units of its bound; every sum may be off by a quantum of fp32 as well."""
         import torch
         x, w = values_on_device(self.codes[a:b], self.e[a:b]), values_on_device(*self.w[expert])
         ref, mag = x @ w.T, x.abs() @ w.abs().T
         mantissa, least, largest = (10, -14, 65504.0) if self.dtype == "f16" else (7, -126, 3.3895313892515355e38)
         exponent = torch.frexp(ref.abs().clamp(max=largest)).exponent.long() - 1
         step = torch.exp2((exponent.clamp(min=least) - mantissa).double())
-        off = (got[a:b].double() - ref).abs() / (0.5 * step + (x.shape[1] // 128 + 12) * 2.0 ** -22 * mag)
+        off = (got[a:b].double() - ref).abs() / (0.5 * step + (x.shape[1] // 128 + 12) * (2.0 ** -22 * mag + quantum))
         return off.max().item() if not off.isnan().any().item() else math.inf
 
 
