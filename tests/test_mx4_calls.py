@@ -130,3 +130,36 @@ def test_exponents_from_end_to_end(lutq, M, N, K, dtype, power):
         assert worst <= 1.0, (as_codes, worst)
         assert y.any().item() or power == -24
         assert power != -140 or (y.abs() < 2.0 ** -126).any().item()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("src", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("M,K", [(8209, 1152), (14593, 640), (262145, 128)])
+def test_more_rows_than_teams_with_a_remainder(lutq, src, M, K):
+    """Four units per team and four words per lane, as large calls take them, where the last workgroup is not full; picked rows as well."""
+    import torch
+    x = edge_values(src, 61, K, M)
+    codes, e = mx.quantize(as_f64(x))
+    rows = np.random.default_rng(K).integers(-1, 61, M).astype(np.int32)
+    rows[-1] = 60
+    ok = rows >= 0
+    x, want_c, want_e, r = x.cuda(), to_gpu(mx.row_bytes(codes)), to_gpu(e), to_gpu(np.where(ok, rows, 0)).long()
+    want_c, want_e = (torch.where(to_gpu(ok)[:, None], t[r], 0).to(torch.uint8) for t in (want_c, want_e))
+    assert M * (K // 128) >= 32768 and M * (K // 128) % 64 and M * K // 8 >= 1 << 20 and M * K // 8 % 1024      # (the kernels' sizes)
+    for pick in (False, True):
+        c = torch.full((M + 2, K // 2), 0xA5, dtype=torch.uint8, device="cuda")
+        s = torch.full((M + 16, K // 32), 0xA5, dtype=torch.uint8, device="cuda")
+        source = x if pick else torch.where(to_gpu(ok)[:, None], x[r], 0)
+        lutq.lutq_mx4_quantize(source, c[:M], s[:M], rows=to_gpu(rows) if pick else None)
+        assert torch.equal(c[:M], want_c) and torch.equal(s[:M], want_e)
+        assert (c[M:] == 0xA5).all().item() and (s[M:] == 0xA5).all().item()
+    if src == "f32":
+        return
+    back = torch.full((M + 2, K), 7.0, dtype=x.dtype, device="cuda")
+    lutq.lutq_mx4_dequant(c[:M], s[:M], back[:M])
+    with np.errstate(over="ignore"):
+        want = torch.from_numpy(mx.values(codes, e).astype(np.float32)).to(x.dtype).cuda()
+    want = torch.where(to_gpu(ok)[:, None], want[r], 0)
+    nan = want.isnan()
+    assert torch.equal(back[:M].isnan(), nan) and torch.equal(torch.where(nan, 0, back[:M]), torch.where(nan, 0, want))
+    assert (back[M:] == 7.0).all().item()
