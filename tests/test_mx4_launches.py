@@ -219,3 +219,47 @@ def test_a_call_of_every_launch(lutq, call):
             assert worst <= 1.0, (as_codes, worst)
         assert (guarded[:16] == -7.0).all().item() and (guarded[16 + M:] == -7.0).all().item() and not ws[:65536].any().item()
         assert torch.equal(y, again)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dense", [False, True])
+def test_more_pieces_of_rows_than_one_launch_takes(lutq, dense):
+    """A launch has at most 65535 workgroups along the rows, four pieces of sixteen rows each here: a second launch has the rest."""
+    import torch
+    M, N, K = 65535 * 64 + 40, 16, 128
+    r = lutq.calib_mx4_launch(M, N, K, 0, not dense)
+    assert (r.room, r.channels, r.waves) == (0, 64, 4)
+    p = Factors(M, N, K, 0, "bf16", 5)
+    y = torch.full((M + 16, N), -7.0, dtype=torch.bfloat16, device="cuda")
+    x, e = p.args(not dense)
+    lutq.lutq_mx4_matmul(x, p.packed, y[:M], lutq.new_mx4_workspace(M, N, K), x_scales=e)
+    for a in range(0, M, 1 << 19):
+        worst = p.worst(y, a, min(M, a + (1 << 19)), 0)
+        assert worst <= 1.0, (a, worst)
+    assert (y[M:] == -7.0).all().item()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dense", [False, True])
+def test_as_many_experts_as_there_may_be(lutq, dense):
+    """65536 of them, 70000 rows: more pieces than a launch has workgroups along the rows."""
+    import torch
+    experts, M, N, K = 65536, 70000, 16, 640
+    assert lutq.calib_mx4_launch(M, N, K, experts, not dense).channels == 16
+    p = Factors(M, experts * N, K, 0, "bf16", 6)
+    g = torch.Generator().manual_seed(7)
+    expert = torch.randint(0, experts, (M - 3,), generator=g).sort().values
+    offsets = torch.cat((torch.zeros(1, dtype=torch.long), torch.bincount(expert, minlength=experts).cumsum(0))).int().cuda()
+    expert = expert.cuda()
+    y = torch.full((M, N), -7.0, dtype=torch.bfloat16, device="cuda")
+    x, e = p.args(not dense)
+    lutq.lutq_mx4_matmul_grouped(x, p.packed.view(experts, -1), offsets, y, lutq.new_mx4_workspace(M, N, K, experts), x_scales=e)
+    codes, scales = (t.view(experts, N, -1) for t in p.w[0])
+    for a in range(0, M - 3, 4096):
+        mine = expert[a:a + 4096]
+        b = a + mine.numel()
+        products = values_on_device(codes[mine].flatten(0, 1), scales[mine].flatten(0, 1)).view(-1, N, K) * values_on_device(p.codes[a:b], p.e[a:b])[:, None]
+        ref, mag = products.sum(-1), products.abs().sum(-1)
+        step = torch.exp2((torch.frexp(ref).exponent - 1).clamp(min=-126).double() - 7)
+        assert ((y[a:b].double() - ref).abs() <= 0.5 * step + (K // 128 + 12) * 2.0 ** -22 * mag).all().item(), a
+    assert (y[M - 3:] == -7.0).all().item()
