@@ -403,7 +403,9 @@ lutq_status lutq_dequant(const void* packed, const void* scales, const void* lut
  * 4 * l is the exponent of that lane's block in tile t (zero where the quad has no such tile).
  *
  * Domain: N a multiple of 16, K of 128, both up to 2^24; rows 0 <= M < 2^30 with M * K / 128 < 2^30 (no rows: nothing is
- * done and no pointer is looked at); device pointers 16-byte aligned (rows and offsets: 4).
+ * done and no pointer is looked at; the quantiser of weights and its inverse take N as M here); device pointers 16-byte aligned (rows and
+ * offsets: 4).  A K of whole blocks that is no multiple of 128, as 2880 is, is padded by the caller, in both factors: columns of
+ * zeros, or exponents and codes of 0, behind each row add nothing to the sums; and N with rows of zeros, whose columns of Y are zeros.
  * ------------------------------------------------------------------------- */
 
 /* Bytes of the packed form of an [N, K] matrix; 0 if the arguments are unsupported.  The experts of a grouped product are

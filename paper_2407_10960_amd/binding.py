@@ -558,6 +558,18 @@ def lutq_mx4_unpack(packed, N: int, K: int) -> tuple:
     return c, e
 
 
+_MX4_DOMAIN = "N must be a multiple of 16 and K of 128 (zeros behind the rows of both factors fill K up)"
+
+
+def _mx4_packed_fits(packed, N, K, experts=1, which=""):
+    """Raises unless `packed` is as long as that many experts' packed forms of [N, K]."""
+    each = lutq_mx4_packed_bytes(N, K)
+    if each == 0:
+        raise ValueError(f"unsupported shape: {_MX4_DOMAIN}")
+    if experts < 1 or packed.numel() != experts * each:
+        raise ValueError("packed buffer has the wrong size for (N, K)" + which)
+
+
 def lutq_mx4_workspace_bytes(M: int, N: int, K: int, experts: int = 1) -> int:
     return int(load_library().lutq_mx4_workspace_bytes(M, N, K, experts))
 
@@ -567,7 +579,7 @@ def new_mx4_workspace(M: int, N: int, K: int, experts: int = 1, device="cuda"):
     torch = _torch()
     n = lutq_mx4_workspace_bytes(M, N, K, experts)
     if n == 0:
-        raise ValueError("unsupported problem")
+        raise ValueError(f"unsupported problem: {_MX4_DOMAIN}, M and experts within their limits")
     return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
@@ -643,8 +655,7 @@ def lutq_mx4_quantize_packed(W, packed_out, stream=None):
     _mx4_bytes("lutq_mx4_quantize_packed", packed_out)
     f32, code = _mx4_source(W, "lutq_mx4_quantize_packed")
     N, K = W.shape
-    if packed_out.numel() == 0 or packed_out.numel() != lutq_mx4_packed_bytes(N, K):
-        raise ValueError("packed buffer has the wrong size for (N, K)")
+    _mx4_packed_fits(packed_out, N, K)
     with torch.cuda.device(device):
         _check(load_library().lutq_mx4_quantize_packed(W.data_ptr(), f32, code, N, K, packed_out.data_ptr(), on),
                "lutq_mx4_quantize_packed")
@@ -678,8 +689,7 @@ def lutq_mx4_dequant_packed(packed, W_out, stream=None):
     _mx4_bytes("lutq_mx4_dequant_packed", packed)
     code = _dtype_code(W_out)
     N, K = W_out.shape
-    if packed.numel() == 0 or packed.numel() != lutq_mx4_packed_bytes(N, K):
-        raise ValueError("packed buffer has the wrong size for (N, K)")
+    _mx4_packed_fits(packed, N, K)
     with torch.cuda.device(device):
         _check(load_library().lutq_mx4_dequant_packed(packed.data_ptr(), N, K, code, W_out.data_ptr(), on),
                "lutq_mx4_dequant_packed")
@@ -706,8 +716,7 @@ def _mx4_product(name, X, packed, offsets, Y, workspace, x_scales, stream):
         experts = offsets.shape[0] - 1
     if x_scales is not None and (K % 32 != 0 or tuple(x_scales.shape) != (M, K // 32)):
         raise ValueError("inconsistent shapes")
-    if experts < 1 or packed.numel() == 0 or packed.numel() != experts * lutq_mx4_packed_bytes(N, K):
-        raise ValueError("packed buffer has the wrong size for (N, K)" + ("" if offsets is None else " and the number of experts"))
+    _mx4_packed_fits(packed, N, K, experts, "" if offsets is None else " and the number of experts")
     head = [X.data_ptr(), x_scales.data_ptr() if x_scales is not None else None, packed.data_ptr()]
     tail = [M, N, K, code, Y.data_ptr(), workspace.data_ptr(), workspace.numel(), on]
     with torch.cuda.device(device):

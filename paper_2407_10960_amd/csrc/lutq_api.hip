@@ -810,7 +810,7 @@ extern "C" const char* lutq_status_string(lutq_status s) {
         case LUTQ_ERR_NULL: return "null pointer";
         case LUTQ_ERR_BITS: return "bits must be 2, 3 or 4";
         case LUTQ_ERR_GROUP: return "group_size must be 32, 64, 128 or 256 and divide K";
-        case LUTQ_ERR_SHAPE: return "unsupported shape (1 <= M <= 128, N % 16 == 0, K % K-tile == 0)";
+        case LUTQ_ERR_SHAPE: return "unsupported shape (N % 16 == 0; table-quantised: 1 <= M <= 128, K % K-tile == 0; microscaled: K % 128 == 0)";
         case LUTQ_ERR_ALIGN: return "device pointer not 16-byte aligned";
         case LUTQ_ERR_INDEX_RANGE: return "index out of range for the bit width";
         case LUTQ_ERR_WORKSPACE: return "workspace missing or too small";

@@ -163,3 +163,37 @@ def test_more_rows_than_teams_with_a_remainder(lutq, src, M, K):
     nan = want.isnan()
     assert torch.equal(back[:M].isnan(), nan) and torch.equal(torch.where(nan, 0, back[:M]), torch.where(nan, 0, want))
     assert (back[M:] == 7.0).all().item()
+
+
+def test_refusals_of_a_shape_name_the_domain(lutq):
+    with pytest.raises(ValueError, match="K of 128"):
+        lutq.new_mx4_workspace(1, 16, 2880)
+    with pytest.raises(lutq.LutqError, match="K % 128"):
+        lutq.lutq_mx4_pack(np.zeros((16, 1440)), np.zeros((16, 90)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M", [1, 5, 33, 200])
+def test_blocks_that_fill_no_tile_are_padded_with_zeros(lutq, M):
+    """K = 2880, 22 1/2 tiles: columns of zeros behind the rows, as values and as codes; and 40 output channels, eight rows of zeros behind."""
+    import torch
+    N, K, NP, KP = 40, 2880, 48, 2944
+    rng = np.random.default_rng(M)
+    x, w = rng.standard_normal((M, K)), rng.standard_normal((N, K))
+    x, w = torch.from_numpy(x).bfloat16(), torch.from_numpy(w).bfloat16()
+    with pytest.raises(ValueError, match="K of 128"):
+        lutq.lutq_mx4_quantize_packed(w.cuda(), torch.zeros(1 << 20, dtype=torch.uint8, device="cuda"))
+    padded = torch.zeros((M, KP), dtype=torch.bfloat16, device="cuda")
+    padded[:, :K] = x.cuda()
+    weights = torch.zeros((NP, KP), dtype=torch.bfloat16, device="cuda")
+    weights[:N, :K] = w.cuda()
+    packed = torch.empty(lutq.lutq_mx4_packed_bytes(NP, KP), dtype=torch.uint8, device="cuda")
+    lutq.lutq_mx4_quantize_packed(weights, packed)
+    codes, e = torch.zeros((M, KP // 2), dtype=torch.uint8, device="cuda"), torch.zeros((M, KP // 32), dtype=torch.uint8, device="cuda")
+    c, s = mx.quantize(as_f64(x))
+    codes[:, :K // 2], e[:, :K // 32] = to_gpu(mx.row_bytes(c)), to_gpu(s)
+    sums = mx.product(mx.values(c, s), mx.values(*mx.quantize(as_f64(w))))
+    y, ws = torch.full((M, NP), 7.0, dtype=torch.bfloat16, device="cuda"), lutq.new_mx4_workspace(M, NP, KP)
+    for args in ((padded, None), (codes, e)):
+        lutq.lutq_mx4_matmul(args[0], packed, y, ws, x_scales=args[1])
+        assert (np.abs(as_f64(y[:, :N]) - sums[0]) <= off_by_at_most(None, sums, KP, "bf16")).all() and not y[:, N:].any().item()
