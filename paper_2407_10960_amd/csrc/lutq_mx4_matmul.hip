@@ -170,7 +170,7 @@ __device__ __forceinline__ void store_rows(F sum, char* y, int rows, int blocks,
 
 // Few rows: a workgroup owns R row blocks of weights and sixteen rows of X over all of K; its wavefronts take the quads in turn, and
 // their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the weights, which go from memory into the operand
-// registers as they lie, all of a quad asked for before X is looked at: 28672 x 4096, 62 MB, 1 row 12.7 us (4.9 TB/s), and 13 rows 14.0; smaller
+// registers as they lie, all of a quad asked for before X is looked at: 28672 x 4096, 62 MB, 1 row 13.0 us (4.8 TB/s), and 13 rows 14.3; smaller
 // ones by the time that one load after another takes to arrive (2048 x 256, 1 row: 2.4 us).  X is asked for before the weights (4096 x 14336,
 // 4 rows of bf16: 10.7 us after them, 10.0 so).
 // X is read as its cache lines lie and passes through a place of the wavefront's own in LDS into the order of the operands.  (A lane per row
@@ -663,7 +663,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
                     for (int b = 0; b < WM; ++b) acc[r][b] = sum[r][b];
             }
         }
-        // (kStores stores by every wavefront, which the next item's first step need not wait for: 8192 rows, 8192 x 2048, 157 -> 154)
+        // (kStores stores by every wavefront, which the next item's first step need not wait for; 8192 rows, 8192 x 2048, 77 us either way)
         if (finished) {
 #pragma unroll
             for (int b = 0; b < WM; ++b) {
@@ -761,19 +761,22 @@ hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
 
 // Whether the weights are streamed past sixteen rows at a time, or which tile shape, and for the smaller ones how many slices of K: the least
 // of times estimated from the bytes of weights over the pieces of rows (B), or from the number of tiles on the busiest compute unit (n) and of
-// steps (S).  Microseconds, fitted to some 300 products of 17 to 16384 rows, N 256 to 32768, K 512 to 16384
-// (the least of all shapes and slices tried was 2 % less on average, products by expert 3 %):
+// steps (S).  Microseconds, fitted to some 300 products of 17 to 16384 rows, N 256 to 32768, K 512 to 16384.  On 130 other ones the least
+// of all shapes and slices was 2 % less on average, on 130 by expert 4 %, and most where many experts have a short K: 1764 rows
+// through 87 of 1344 x 768 take 28.2, the 128 x 128 tiles of two workgroups per unit 17.9.
 //   streamed        2.3 + B / 6.6 TB/s
 //   256 x 256       6.0 + n (1.75 S + 4.5)                one workgroup per compute unit; the 4.5 are its stores
 //   128 x 128       1.5 + 1.25 S + 2.6 per two, 0.95 S + 1.3 for one; two workgroups per unit, two steps of room each
 //   128 x 128 deep  3.2 + n (0.72 S + 1), 0.63 S for one  one of eight wavefronts, four steps of room; in z slices of K 2.5 + 1.6 z more
 //   128 x 64 deep   3.2 + n (0.50 S + 0.7)                the same; in z slices 3 + 0.8 z more
 //   64 x 64 deep    3.0 + 0.62 S + 0.9 per two, 0.37 S + 0.9 for one; two of four wavefronts; in z slices 1.8 + z more
-// Examples (us, shapes in this order): 17 rows, 6144 x 4096 6.2, and tiles at best 9.3; 28672 x 4096 21.8, and 15.5; 512 rows,
-// 4096 x 4096 -, 27.6, 15.2, 14.5, 11.5, 12.7; 8192 rows, 8192 x 8192 -, 240, 318, 378, 543, 569; 200 rows, 28672 x 4096 -, 34, 27.0, 28.6,
-// 35.3, 33.3; 200 rows, 5120 x 13824 -, 84, 48, 35.4, 26.7, 30.8, and 21.9 with 128 x 128 in three slices; 64 rows, 4096 x 14336 -, 83, 52, 36,
-// 33, 24.8, and 13.8 with 64 x 64 in four.  80 rows through 2 experts of 4096 x 14336: 27, in slices 17.8.
+// Examples (us, shapes in this order, weights from memory): 17 rows, 6144 x 4096 6.2, and tiles at best 9.2; 28672 x 4096 21.9, and 15.9; 512
+// rows, 4096 x 4096 18.6, 30.3, 18.2, 15.8, 12.4, 14.7; 8192 rows, 8192 x 8192 -, 249, 322, 379, 512, 563; 200 rows, 28672 x 4096 112, 33.5, 26.6,
+// 29.2, 36.6, 33.4; 200 rows, 5120 x 13824 39.6, 86, 51.5, 37.7, 28.1, 31.1, and 23.0 with 128 x 128 in three slices; 64 rows, 4096 x 14336 17.1, 84,
+// 52.9, 38.0, 33.8, 24.5, and 13.2 with 64 x 64 in four.  80 rows through 2 experts of 4096 x 14336: 26.8, in slices 21.7.
 // By expert the number of pieces is not known here: every expert is taken to have the mean number of rows and half a piece that is not full.
+// Few rows on average stay with the streaming kernel also where one expert has most of them and its weights are read again for every sixteen
+// (64 experts of 2816 x 2048, 500 rows, 454 of them one expert's: 29.2, tiles at best 28.2; 16 of 4096 x 4096, 250 rows, 228: 29.6 and 25.9).
 struct TileChoice { int shape, slices; };             // shape -1: streamed
 
 TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int64_t record, int cus) {
@@ -828,15 +831,17 @@ Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int64_t record
     Choice c{};
     const int KQ = (int)((KT + 3) / 4);
     c.tiles = choose_tiles(M, NB, KT, experts, record, cus);
-    // Where the streaming workgroups quantise X on the way in, every one of them does it for all its rows.  Up to four rows, beyond some 160 rows
-    // and quads per compute unit that takes longer than a launch which does it once (us, so and with that launch: 4096 x 14336, 1 row (28) 8.7
-    // and 10.5; 28672 x 4096, 4 rows (128) 14.9 and 15.4; 512 x 16384, 4 rows (128) 6.2 and 7.1; 4096 x 14336, 6 rows (168) 14.4 and 11.2).  More
-    // rows cost the same however many they are, like twenty (16 rows, 4096 x 4096 (8 quads) 6.3 and 6.8, 6144 x 4096 (8) 7.2 and 8.2; 6 rows,
-    // 1024 x 8192 (16) 7.5 and 6.5, 13824 x 5120 (20) 14.4 and 12.4; 211 rows through 41 experts of 288 x 640 (4) 5.9 and 6.8).
-    // Two row blocks per workgroup halve it, and leave fewer wavefronts to hide the reads (28672 x 4096, 1 row 13.4 and 13.6, 2 rows 14.7 and
-    // 13.9 with one; 128 experts of 1536 x 4096, 64 rows, 34.4 and 35.3).  Codes alone gain by two where workgroups are many and share their
-    // weights (64 experts, 250 rows: 36.8 and 38.1; 500 rows 37.4 and 39.4) and lose with a row or two each (34.1 and 33.2).  A single quad of K
-    // leaves nothing to hide: 8192 rows, 8192 x 384, 97 us with one row block, 71 with four, 60 with whole lines of Y stored.
+    // (Figures: us, weights from memory.)  Where the streaming workgroups quantise X on the way in, every one of them does it for all its rows.  Up to
+    // four rows, beyond some 160 rows and quads per compute unit that takes longer than a launch which does it once (so and with that launch:
+    // 4096 x 14336, 1 row (28) 8.5 and 10.7; 28672 x 4096, 4 rows (128) 15.2 and 15.5; 512 x 16384, 4 rows (128) 8.6 and 8.7; 4096 x 14336, 6 rows
+    // (168) 14.1 and 10.9).  More rows cost the same however many they are, like twenty (16 rows, 4096 x 4096 (8 quads) 6.7 and 7.2,
+    // 6144 x 4096 (8) 7.1 and 8.4; 6 rows, 1024 x 8192 (16) 8.7 and 7.4, 13824 x 5120 (20) 14.4 and 12.2; 211 rows through 41 experts of 288 x 640 (4)
+    // 6.1 and 6.8).
+    // Two row blocks per workgroup halve it, and leave fewer wavefronts to hide the reads (one and two: 28672 x 4096, 1 row 13.9 and 13.3;
+    // 128256 x 4096, 1 row 47.2 and 45.1; 128 experts of 1536 x 4096, 64 rows 26.7 and 23.1; but 28672 x 4096, 2 rows 13.3 and 14.3, 4 rows 14.3 and
+    // 15.2).  Codes gain by two where workgroups are many and share their weights (64 experts of 2816 x 2048, 500 rows 39.3 and 37.0;
+    // 128256 x 4096, 13 rows 53.2 and 47.9); with a row or two each it is much the same (60 rows 22.9 and 22.2; 1 row 44.6 and 45.5).  A single quad
+    // of K leaves nothing to hide: 8192 rows, 8192 x 384, 101 with one row block, 82 with two, 55 with four.
     const int64_t pieces = experts ? (M < experts ? M : experts) : (M + 15) / 16, groups = NB * pieces, mean = (M + pieces - 1) / pieces;
     int wide = !codes && (groups > 1024 || mean > 4) ? 2 : 1;
     const int64_t rounds = (groups / wide + cus - 1) / cus;                    // of workgroups
@@ -847,17 +852,22 @@ Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int64_t record
         wide = 1;
     }
     if (codes && groups > (experts ? 2048 : 4096)) wide = KQ == 1 ? 4 : mean > 2 ? 2 : 1;
-    // Weights that are read once and take more than half of the 256 MB cache are read past it (57344 x 8192, 250 MB, 1 row:
-    // 44.9 us, so 38.9; 64 experts of 2816 x 2048, 250 rows: 34.1 and 31.2; of 1536 x 4096, 1100 rows: 52.4 and 48.5).  Smaller ones may still be
-    // there at the next call: 28672 x 4096, three in turn, 13 rows 13.1, past the cache 14.7, though of nine in turn 14.1 and 13.6.  Nor where
-    // several workgroups read the same ones (8 experts of 4096 x 4096, 64 rows: 12.7 and 14.3; 1024 rows, 5120 x 5120: 28.7 and 33.7).
+    // Weights that are read once and take more than half of the 256 MB cache are read past it (kept and past: 57344 x 8192, 250 MB, 1 row
+    // 45.4 and 42.9; 128256 x 4096 52.2 and 45.5; 64 experts of 2816 x 2048, 250 rows 35.1 and 31.8; of 1536 x 4096, 1100 rows 49.8 and 47.0).  Smaller
+    // ones may still be there at the next call: 28672 x 4096, 13 rows, three matrices in turn 11.4 and 12.5.  Where they are not, because
+    // the program reads a cache full of others in between, they lose what past the cache would save, 3 to 9 % from 24 MB on (the same
+    // from memory: 14.3 and 13.2).  Nor where several workgroups read the same ones (8 experts of 4096 x 4096, 64 rows, in
+    // turn 14.9 and 16.8; 1024 rows, 5120 x 5120 28.9 and 33.0).
     const int64_t shared = c.tiles.shape >= 0 ? (c.tiles.shape == 3 || c.tiles.shape == 4 ? 64 : 128) : experts ? 4 : 16;
     c.once = (experts ? mean : M) <= shared && NB * (experts ? pieces : 1) * record > (int64_t(128) << 20);
-    // Wavefronts of a workgroup: sixteen with one row block, eight with two (their registers) or where they quantise and workgroups are many,
-    // four where workgroups are so many that their beginnings count (57344 x 8192, 1 row: 44.2 us with eight, 42.2 with sixteen).
-    // By expert, where X is codes, four from fewer workgroups on, and fewer with two quads each where there are very many, as some
-    // find that there is nothing for them, and the others lie all over the weights (65 experts of 720 x 6272, 35 rows: 13.2 with thirteen, 9.6
-    // with four; 50 of 3376 x 2688, 28 rows: 7.4 with four, 6.2 with three; 41 of 480 x 1408, 40 rows: 4.2 with three, 4.5 with two).
+    // Wavefronts of a workgroup, up to one per quad: sixteen with one row block (values, 1 row, 4096 x 14336: 12.3 with four, 9.6 with eight, 8.5 with
+    // sixteen); eight with two (their registers) or where they quantise and workgroups are many (1 row, with eight and sixteen: 8192 x 8192, 512
+    // workgroups, 9.4 and 9.0; 10240 x 8192, 640, 11.1 and 11.4); four where they are so many that their beginnings count (128256 x 4096, 8016 groups: 13
+    // rows of codes 47.9 and with eight 48.9; 57344 x 4096, 3584, 1 row 24.6 and 23.4).  By expert, where X is codes, four from fewer workgroups
+    // on, and fewer with two quads each where there are very many, as some find that there is nothing for them, and the others lie all
+    // over the weights (16 experts of 2048 x 4096, 64 rows: 15.1 with four, 16.2 with eight; 32 of 480 x 4096, 30 rows, 900: 6.7 and 6.8; 65 of
+    // 720 x 6272, 100 rows: 24.7 with four, 32.9 with thirteen; 128 of 1536 x 3584, 128 rows: 39.4 with three, 57.0 with seven; 50 of 3376 x 2688, 28
+    // rows: 18.8 with three, 19.7 with four; 41 of 480 x 1408, 40 rows, 1200: 4.8 with three, 5.4 with two).
     const int many = groups > 2048 ? (KQ < 4 ? 2 : KQ < 8 ? KQ / 2 : 4) : 4;
     const int most = experts && codes && groups > 900 ? many : groups > 4096 ? 4 : wide > 1 || (!codes && groups > 512) ? 8 : 16;
     c.waves = wide == 4 ? (pieces < 4 ? (int)pieces : 4) : KQ < most ? KQ : most;
