@@ -404,7 +404,7 @@ lutq_status lutq_dequant(const void* packed, const void* scales, const void* lut
  *
  * Domain: N a multiple of 16, K of 128, both up to 2^24; rows 0 <= M < 2^30 with M * K / 128 < 2^30 (no rows: nothing is
  * done and no pointer is looked at; the quantiser of weights and its inverse take N as M here); device pointers 16-byte aligned (rows and
- * offsets: 4).  A K of whole blocks that is no multiple of 128, as 2880 is, is padded by the caller, in both factors: columns of
+ * offsets: 4); outputs and workspace overlap neither each other nor an input.  A K of whole blocks that is no multiple of 128, as 2880 is, is padded by the caller, in both factors: columns of
  * zeros, or exponents and codes of 0, behind each row add nothing to the sums; and N with rows of zeros, whose columns of Y are zeros.
  * ------------------------------------------------------------------------- */
 
