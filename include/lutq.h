@@ -465,6 +465,127 @@ lutq_status lutq_mx4_matmul_grouped(const void* X, const void* x_exponents, cons
                                     int64_t experts, int64_t M, int64_t N, int64_t K, lutq_dtype dtype, void* Y,
                                     void* workspace, size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------
+ * 8-bit floating point with a scale for each block of 128, and the gated feed-forward block on it.
+ *
+ * A value is a code of 8 bits times a 32-bit scale.  Codes are E4M3 as the Open Compute formats have it: sign, four bits of exponent,
+ * three of mantissa, 448 the largest magnitude, 0x7f and 0xff not a number.  Three forms share it:
+ *   ROWS     activations [M, K]: codes [M, K] row-major; scales [K / 128, M]: one for each row and 128 neighbouring columns
+ *   WEIGHTS  [N, K]: codes [N, K] row-major; scales [ceil(N / 128), K / 128]: one for each square of 128 x 128 (as checkpoints hold
+ *            them; transposed codes and scales are the transposed matrix's, where N is a multiple of 128 too)
+ *   COLUMNS  X [M, K] transposed, for sums over its rows: codes [K, M'], M' = M rounded up to a multiple of 128, zeros there; scales
+ *            [M' / 128, K], powers of two: one for each column and 128 neighbouring rows
+ *
+ * Quantiser: with a = max |x| over the block, at least 2^-110, the scale is a / 448 and the codes are x * (448 / a), each of the two quotients and
+ * the product one rounding to 32 bits, then to the nearest code, ties to the even one.  By columns the scale is the least power of
+ * two that is at least a / 448.  A block that holds an infinity or a NaN has a scale that is not a number, and codes of 0.
+ *
+ * Products: for each block of 128 columns the sum of the codes' products, as the matrix instruction makes it, times the product of the two scales, one
+ * fp32 number (it loses precision where it is below 2^-126 and is infinite beyond 2^128), added in fp32.  The instruction adds in fp32, but for
+ * eight neighbouring columns at a time it cuts what lies below 2^-13 of the power of two of the largest product: products of at least 2^-7 of that
+ * power are exact.  Anything that is not a number stays in its row or column of the result.
+ *
+ * Domain: N a multiple of 16, up to 2^24; K a multiple of 128, up to 2^22; F (columns of H) a multiple of 128, up to 2^21; rows
+ * 0 <= M < 2^30 with M * K / 128 < 2^30 (no rows: nothing is done and no pointer is looked at; the quantiser of weights takes N as M here); device
+ * pointers 16-byte aligned (rows, offsets and scales: 4); outputs and workspace overlap neither each other nor an input.  A K that
+ * is no multiple of 128 is padded by the caller, in both factors: columns of zero codes behind each row add nothing to the sums.
+ * ------------------------------------------------------------------------- */
+
+/* Quantiser of rows.
+ *   X       device, [source_rows, K] row-major; fp32 if x_is_f32 != 0, else `dtype`
+ *   rows    device, M row numbers (int32), or NULL: output row m is row rows[m] of X, a row of zeros where rows[m] is not
+ *           in 0 .. source_rows - 1.  NULL: row m (source_rows is then M)
+ *   codes_out, scales_out   device, ROWS, fully overwritten
+ * Asynchronous on `stream`.  Errors: NULL, SHAPE, DTYPE, ALIGN, DEVICE. */
+lutq_status lutq_fp8_quantize(const void* X, int x_is_f32, lutq_dtype dtype, int64_t source_rows, const int32_t* rows,
+                              int64_t M, int64_t K, void* codes_out, float* scales_out, void* stream);
+
+/* Quantiser of weights W [N, K].  transposed_codes_out, transposed_scales_out, or NULL: the codes [K, N] and scales
+ * [K / 128, ceil(N / 128)] of W transposed as well.
+ * Asynchronous on `stream`.  Errors: NULL (also for one of these two without the other), SHAPE, DTYPE, ALIGN, DEVICE. */
+lutq_status lutq_fp8_quantize_weights(const void* W, int w_is_f32, lutq_dtype dtype, int64_t N, int64_t K, void* codes_out,
+                                      float* scales_out, void* transposed_codes_out, float* transposed_scales_out, void* stream);
+
+/* Quantiser of columns: codes_out [K, M'] and scales_out [M' / 128, K] of X [M, K], M >= 1.
+ * Asynchronous on `stream`.  Errors: NULL, SHAPE, DTYPE, ALIGN, DEVICE. */
+lutq_status lutq_fp8_quantize_columns(const void* X, int x_is_f32, lutq_dtype dtype, int64_t M, int64_t K, void* codes_out,
+                                      float* scales_out, void* stream);
+
+/* The values back, code times scale in fp32, rounded to the 16-bit `dtype`: [M, K] of ROWS, [N, K] of WEIGHTS.
+ * Asynchronous on `stream`.  Errors: NULL, SHAPE, DTYPE, ALIGN, DEVICE. */
+lutq_status lutq_fp8_dequant(const void* codes, const float* scales, int64_t M, int64_t K, lutq_dtype dtype, void* X_out, void* stream);
+lutq_status lutq_fp8_dequant_weights(const void* codes, const float* scales, int64_t N, int64_t K, lutq_dtype dtype, void* W_out, void* stream);
+
+/* Bytes of device scratch of the products below for up to M rows; experts = 1 for those without.  0 if unsupported. */
+size_t lutq_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t experts);
+size_t lutq_fp8_gated_workspace_bytes(int64_t M, int64_t F, int64_t K, int64_t experts);
+
+/* Y[m, n] = sum_k X[m, k] * W[n, k], rounded once to `dtype`.
+ *   X, x_scales  device: ROWS; or, x_scales NULL, activations [M, K] of `dtype`, which are quantised on the way in, to what
+ *                lutq_fp8_quantize would make of them
+ *   W, w_scales  device: WEIGHTS [N, K]
+ *   Y            device, [M, N] row-major, dtype; fully overwritten
+ *   workspace    device, >= lutq_fp8_workspace_bytes(M, N, K, 1), zero-filled once before its first use, and then as for
+ *                lutq_matmul: its first 64 KiB are left zero, calls that may run concurrently need one each
+ * Asynchronous on `stream`.  Errors: NULL, SHAPE, DTYPE, ALIGN, WORKSPACE, DEVICE; Y untouched on error. */
+lutq_status lutq_fp8_matmul(const void* X, const float* x_scales, const void* W, const float* w_scales, int64_t M, int64_t N, int64_t K,
+                            lutq_dtype dtype, void* Y, void* workspace, size_t workspace_bytes, void* stream);
+
+/* The same by expert: rows offsets[g] .. offsets[g + 1] - 1 of X times the weights of expert g.
+ *   W, w_scales  device: `experts` WEIGHTS [N, K], codes one behind the other and scales one behind the other
+ *   offsets      device, experts + 1 row numbers (int32), not decreasing, within 0 .. M: read on the device, as for lutq_mx4_matmul_grouped
+ *   Y            [M, N]; rows before offsets[0] and from offsets[experts] on stay as they were
+ *   workspace    >= lutq_fp8_workspace_bytes(M, N, K, experts)
+ * 1 <= experts <= 65536.  Everything else as for lutq_fp8_matmul. */
+lutq_status lutq_fp8_matmul_grouped(const void* X, const float* x_scales, const void* W, const float* w_scales, const int32_t* offsets,
+                                    int64_t experts, int64_t M, int64_t N, int64_t K, lutq_dtype dtype, void* Y, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+typedef enum {
+    LUTQ_SILU = 0,             /* g / (1 + exp(-g)) */
+    LUTQ_GELU = 1              /* g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) */
+} lutq_activation;
+
+/* The gated block's projections, activation and product in one kernel: with G and U the two halves of the rows of X W^T,
+ *        H[m, f] = act(G[m, f]) * U[m, f],  G = X W[0 .. F - 1]^T,  U = X W[F .. 2 F - 1]^T
+ *   X, x_scales          as for lutq_fp8_matmul;  W, w_scales  WEIGHTS [2 F, K], the gate's rows first
+ *   H                    device, [M, F], dtype, or NULL
+ *   h_codes, h_scales    device, or NULL: ROWS [M, F], what lutq_fp8_quantize makes of H of `dtype`, ready for the down projection's product.
+ *                        H, these, or all of them
+ *   saved                device, [M, 2 F], dtype, or NULL: G and U side by side, for lutq_fp8_gated_grad
+ *   workspace            >= lutq_fp8_gated_workspace_bytes(M, F, K, 1), as for lutq_fp8_matmul
+ * Errors: those of lutq_fp8_matmul; DTYPE also for an activation that there is not.
+ * By expert (lutq_fp8_gated_grouped; W: `experts` of them) as for lutq_fp8_matmul_grouped: rows outside stay in every output. */
+lutq_status lutq_fp8_gated(const void* X, const float* x_scales, const void* W, const float* w_scales, int64_t M, int64_t F, int64_t K,
+                           lutq_activation activation, lutq_dtype dtype, void* H, void* h_codes, float* h_scales, void* saved,
+                           void* workspace, size_t workspace_bytes, void* stream);
+lutq_status lutq_fp8_gated_grouped(const void* X, const float* x_scales, const void* W, const float* w_scales, const int32_t* offsets,
+                                   int64_t experts, int64_t M, int64_t F, int64_t K, lutq_activation activation, lutq_dtype dtype, void* H,
+                                   void* h_codes, float* h_scales, void* saved, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its backward pass, first part: from dH and the saved G, U the gradients of both,
+ *        dG = dH * U * act'(G),  dU = dH * act(G),
+ * side by side [M, 2 F], in any of three forms (at least one; the others NULL):
+ *   dense_out                       device, [M, 2 F], dtype
+ *   codes_out, scales_out           device, ROWS [M, 2 F]: lutq_fp8_matmul of them and the transposed weights [K, 2 F] is the gradient of X
+ *   columns_out, column_scales_out  device, COLUMNS (codes [2 F, M']): one factor of the gradient of the weights
+ * The quantised forms are made of the 32-bit gradients.  saved may come from any program that has G and U (e.g. from H's rows by expert).
+ * Asynchronous on `stream`.  Errors: NULL (also for scales without codes), SHAPE (also for columns of no rows), DTYPE, ALIGN, DEVICE. */
+lutq_status lutq_fp8_gated_grad(const void* dH, const void* saved, int64_t M, int64_t F, lutq_activation activation, lutq_dtype dtype,
+                                void* dense_out, void* codes_out, float* scales_out, void* columns_out, float* column_scales_out,
+                                void* stream);
+
+/* Second part, the gradient of any product's weights: dW[n, k] = sum_m dY[m, n] * X[m, k], rounded once to `dtype`.
+ *   dY, dy_scales   device, COLUMNS of the gradient of Y: codes [N, M], scales [M / 128, N]
+ *   X, x_scales     device, COLUMNS of X: codes [K, M], scales [M / 128, K]
+ *   M               rows, with those that fill them up: a multiple of 128, at least 128
+ *   dW              device, [N, K], dtype; fully overwritten
+ *   workspace       >= lutq_fp8_workspace_bytes(N, K, M, 1), as for lutq_fp8_matmul
+ * N and K multiples of 16.  The scales have to be powers of two from 2^-126 on (or not a number), as the quantiser of columns makes them: the matrix
+ * instruction takes their exponents.  Errors: those of lutq_fp8_matmul; SHAPE for M = 0, too. */
+lutq_status lutq_fp8_weight_grad(const void* dY, const float* dy_scales, const void* X, const float* x_scales, int64_t N, int64_t K, int64_t M,
+                                 lutq_dtype dtype, void* dW, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,9 @@ EXPORTED_SYMBOLS = (
     "lutq_calib_stream_read", "lutq_calib_copy", "lutq_calib_matmul_trace", "lutq_calib_route", "lutq_calib_plan", "lutq_calib_mx4_launch",
     "lutq_mx4_packed_bytes", "lutq_mx4_pack", "lutq_mx4_unpack", "lutq_mx4_quantize", "lutq_mx4_quantize_packed", "lutq_mx4_dequant",
     "lutq_mx4_dequant_packed", "lutq_mx4_workspace_bytes", "lutq_mx4_matmul", "lutq_mx4_matmul_grouped",
+    "lutq_fp8_quantize", "lutq_fp8_quantize_weights", "lutq_fp8_quantize_columns", "lutq_fp8_dequant", "lutq_fp8_dequant_weights",
+    "lutq_fp8_workspace_bytes", "lutq_fp8_gated_workspace_bytes", "lutq_fp8_matmul", "lutq_fp8_matmul_grouped", "lutq_fp8_gated",
+    "lutq_fp8_gated_grouped", "lutq_fp8_gated_grad", "lutq_fp8_weight_grad", "lutq_calib_fp8_launch",
 )
 
 LUTQ_F16, LUTQ_BF16 = 0, 1
@@ -152,6 +155,23 @@ def load_library():
                        ("matmul", [vp, vp, vp, i64, i64, i64, ci, vp, vp, sz, vp]),
                        ("matmul_grouped", [vp, vp, vp, vp, i64, i64, i64, i64, ci, vp, vp, sz, vp])):
         f = getattr(lib, "lutq_mx4_" + name)
+        f.restype, f.argtypes = ci, args
+    lib.lutq_calib_fp8_launch.restype = ci
+    lib.lutq_calib_fp8_launch.argtypes = [i64, i64, i64, i64, ci, ci, ci, ctypes.POINTER(ctypes.c_int)]
+    for name in ("workspace_bytes", "gated_workspace_bytes"):
+        f = getattr(lib, "lutq_fp8_" + name)
+        f.restype, f.argtypes = sz, [i64, i64, i64, i64]
+    for name, args in (("quantize", [vp, ci, ci, i64, vp, i64, i64, vp, vp, vp]),
+                       ("quantize_weights", [vp, ci, ci, i64, i64, vp, vp, vp, vp, vp]),
+                       ("quantize_columns", [vp, ci, ci, i64, i64, vp, vp, vp]),
+                       ("dequant", [vp, vp, i64, i64, ci, vp, vp]), ("dequant_weights", [vp, vp, i64, i64, ci, vp, vp]),
+                       ("matmul", [vp, vp, vp, vp, i64, i64, i64, ci, vp, vp, sz, vp]),
+                       ("matmul_grouped", [vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, vp, vp, sz, vp]),
+                       ("gated", [vp, vp, vp, vp, i64, i64, i64, ci, ci, vp, vp, vp, vp, vp, sz, vp]),
+                       ("gated_grouped", [vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, ci, vp, vp, vp, vp, vp, sz, vp]),
+                       ("gated_grad", [vp, vp, i64, i64, ci, ci, vp, vp, vp, vp, vp, vp]),
+                       ("weight_grad", [vp, vp, vp, vp, i64, i64, i64, ci, vp, vp, sz, vp])):
+        f = getattr(lib, "lutq_fp8_" + name)
         f.restype, f.argtypes = ci, args
     _LIB = lib
     return lib
@@ -741,6 +761,279 @@ def lutq_mx4_matmul_grouped(X, packed, offsets, Y, workspace, x_scales=None, str
     return _mx4_product("lutq_mx4_matmul_grouped", X, packed, offsets, Y, workspace, x_scales, stream)
 
 
+# ------------------------------------------------------------------ 8-bit floating point, blocks of 128
+LUTQ_SILU, LUTQ_GELU = 0, 1
+_FP8_ACTIVATIONS = {"silu": LUTQ_SILU, "gelu": LUTQ_GELU}
+_FP8_DOMAIN = "N must be a multiple of 16, F and K of 128 (zero codes behind the rows of both factors fill K up)"
+
+
+def lutq_fp8_workspace_bytes(M: int, N: int, K: int, experts: int = 1) -> int:
+    return int(load_library().lutq_fp8_workspace_bytes(M, N, K, experts))
+
+
+def lutq_fp8_gated_workspace_bytes(M: int, F: int, K: int, experts: int = 1) -> int:
+    return int(load_library().lutq_fp8_gated_workspace_bytes(M, F, K, experts))
+
+
+def _fp8_workspace(n, device):
+    if n == 0:
+        raise ValueError(f"unsupported problem: {_FP8_DOMAIN}, M and experts within their limits")
+    return _torch().zeros(n, dtype=_torch().uint8, device=device)
+
+
+def new_fp8_workspace(M: int, N: int, K: int, experts: int = 1, device="cuda"):
+    """A zero-filled device workspace for the products of up to M rows (reusable across calls on one stream)."""
+    return _fp8_workspace(lutq_fp8_workspace_bytes(M, N, K, experts), device)
+
+
+def new_fp8_gated_workspace(M: int, F: int, K: int, experts: int = 1, device="cuda"):
+    """The same for the gated block with F columns of H."""
+    return _fp8_workspace(lutq_fp8_gated_workspace_bytes(M, F, K, experts), device)
+
+
+def _fp8_codes(name, *tensors):
+    torch = _torch()
+    for t in tensors:
+        if t is not None and t.dtype not in (torch.uint8, torch.float8_e4m3fn):
+            raise TypeError(f"{name}: codes must be uint8 or float8_e4m3fn")
+
+
+def _fp8_scales(name, *tensors):
+    for t in tensors:
+        if t is not None and t.dtype != _torch().float32:
+            raise TypeError(f"{name}: scales must be float32")
+
+
+def _fp8_shapes(name, *pairs):
+    """(tensor or None, its shape), each."""
+    for t, shape in pairs:
+        if t is not None and tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name}: inconsistent shapes: {tuple(t.shape)} where {tuple(shape)} is expected")
+
+
+def _fp8_dims(name, *pairs):
+    for t, n in pairs:
+        if t is not None and t.dim() != n:
+            raise ValueError(f"{name}: inconsistent shapes: {tuple(t.shape)} where {n} dimensions are expected")
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _up128(n: int) -> int:
+    return (n + 127) // 128
+
+
+def lutq_fp8_quantize(X, codes_out, scales_out, rows=None, stream=None):
+    """Quantises X [., K] (float32, float16, bfloat16) to codes [M, K] (uint8 or float8_e4m3fn) and scales [K / 128, M] (float32).
+    With rows (int32, [M], on the device) output row m is row rows[m] of X, zeros where that is no row of X."""
+    name = "lutq_fp8_quantize"
+    device, on = _mx4_tensors(name, stream, X, codes_out, scales_out, rows)
+    _fp8_codes(name, codes_out)
+    _fp8_scales(name, scales_out)
+    f32, code = _mx4_source(X, name)
+    if rows is not None and (rows.dtype != _torch().int32 or rows.dim() != 1):
+        raise TypeError(f"{name}: rows must be int32, [M]")
+    _fp8_dims(name, (X, 2))
+    M, K = (X.shape[0] if rows is None else rows.shape[0]), X.shape[1]
+    _fp8_shapes(name, (codes_out, (M, K)), (scales_out, (K // 128, M)))
+    with _torch().cuda.device(device):
+        _check(load_library().lutq_fp8_quantize(X.data_ptr(), f32, code, X.shape[0], _ptr(rows), M, K, codes_out.data_ptr(),
+                                                scales_out.data_ptr(), on), name)
+    return codes_out, scales_out
+
+
+def lutq_fp8_quantize_weights(W, codes_out, scales_out, transposed=None, stream=None):
+    """Quantises W [N, K] (float32, float16, bfloat16) to codes [N, K] and scales [ceil(N / 128), K / 128], one for each square of
+    128 x 128.  transposed=(codes [K, N], scales [K / 128, ceil(N / 128)]) takes those of W transposed as well."""
+    name = "lutq_fp8_quantize_weights"
+    t_codes, t_scales = transposed if transposed is not None else (None, None)
+    device, on = _mx4_tensors(name, stream, W, codes_out, scales_out, t_codes, t_scales)
+    _fp8_codes(name, codes_out, t_codes)
+    _fp8_scales(name, scales_out, t_scales)
+    f32, code = _mx4_source(W, name)
+    _fp8_dims(name, (W, 2))
+    N, K = W.shape
+    _fp8_shapes(name, (codes_out, (N, K)), (scales_out, (_up128(N), K // 128)), (t_codes, (K, N)), (t_scales, (K // 128, _up128(N))))
+    if (t_codes is None) != (t_scales is None):
+        raise TypeError(f"{name}: transposed must be (codes, scales)")
+    torch = _torch()
+    with torch.cuda.device(device):
+        _check(load_library().lutq_fp8_quantize_weights(W.data_ptr(), f32, code, N, K, codes_out.data_ptr(), scales_out.data_ptr(),
+                                                        _ptr(t_codes), _ptr(t_scales), on), name)
+    return codes_out, scales_out
+
+
+def lutq_fp8_quantize_columns(X, codes_out, scales_out, stream=None):
+    """Quantises X [M, K] (float32, float16, bfloat16) by columns: codes [K, M'], M' the next multiple of 128 from M on, and scales
+    [M' / 128, K], powers of two: a factor of lutq_fp8_weight_grad."""
+    name = "lutq_fp8_quantize_columns"
+    device, on = _mx4_tensors(name, stream, X, codes_out, scales_out)
+    _fp8_codes(name, codes_out)
+    _fp8_scales(name, scales_out)
+    f32, code = _mx4_source(X, name)
+    _fp8_dims(name, (X, 2))
+    M, K = X.shape
+    _fp8_shapes(name, (codes_out, (K, 128 * _up128(M))), (scales_out, (_up128(M), K)))
+    with _torch().cuda.device(device):
+        _check(load_library().lutq_fp8_quantize_columns(X.data_ptr(), f32, code, M, K, codes_out.data_ptr(), scales_out.data_ptr(), on), name)
+    return codes_out, scales_out
+
+
+def _fp8_dequantise(name, codes, scales, out, scales_shape, stream):
+    device, on = _mx4_tensors(name, stream, codes, scales, out)
+    _fp8_codes(name, codes)
+    _fp8_scales(name, scales)
+    code = _dtype_code(out)
+    _fp8_dims(name, (out, 2))
+    M, K = out.shape
+    _fp8_shapes(name, (codes, (M, K)), (scales, scales_shape(M, K)))
+    with _torch().cuda.device(device):
+        _check(getattr(load_library(), name)(codes.data_ptr(), scales.data_ptr(), M, K, code, out.data_ptr(), on), name)
+    return out
+
+
+def lutq_fp8_dequant(codes, scales, X_out, stream=None):
+    """X_out [M, K] (float16 or bfloat16) = the values that codes [M, K] and scales [K / 128, M] stand for."""
+    return _fp8_dequantise("lutq_fp8_dequant", codes, scales, X_out, lambda M, K: (K // 128, M), stream)
+
+
+def lutq_fp8_dequant_weights(codes, scales, W_out, stream=None):
+    """W_out [N, K] (float16 or bfloat16) = the values that codes [N, K] and scales [ceil(N / 128), K / 128] stand for."""
+    return _fp8_dequantise("lutq_fp8_dequant_weights", codes, scales, W_out, lambda N, K: (_up128(N), K // 128), stream)
+
+
+def _fp8_product(name, X, x_scales, W, w_scales, offsets, Y, workspace, stream, gated=None):
+    """gated: None, or (activation, H's dtype, codes and scales of H or None, saved or None); Y may be None then."""
+    act, dtype, h_codes, h_scales, saved = gated if gated else (None, Y.dtype, None, None, None)
+    torch = _torch()
+    device, on = _mx4_tensors(name, stream, X, x_scales, W, w_scales, offsets, Y, h_codes, h_scales, saved, workspace)
+    _fp8_codes(name, W, h_codes, *(() if x_scales is None else (X,)))
+    _fp8_scales(name, x_scales, w_scales, h_scales)
+    if workspace.dtype != torch.uint8:
+        raise TypeError(f"{name}: workspace must be uint8")
+    if dtype not in (torch.float16, torch.bfloat16):
+        raise TypeError(f"{name}: dtype must be float16 or bfloat16")
+    code = LUTQ_F16 if dtype == torch.float16 else LUTQ_BF16
+    for t in (Y, saved, X if x_scales is None else None):
+        if t is not None and t.dtype != dtype:
+            raise TypeError(f"{name}: X without x_scales, the outputs and what is saved share one dtype, float16 or bfloat16")
+    experts = 1
+    if offsets is not None:
+        if offsets.dtype != torch.int32 or offsets.dim() != 1:
+            raise TypeError(f"{name}: offsets must be int32, [experts + 1]")
+        experts = offsets.shape[0] - 1
+    out = Y if Y is not None else h_codes
+    _fp8_dims(name, (X, 2), (out, 2), (W, 2 if offsets is None else 3))
+    (M, N), K = out.shape, X.shape[1]
+    rows = 2 * N if gated else N
+    by = () if offsets is None else (experts,)
+    _fp8_shapes(name, (X, (M, K)), (x_scales, (K // 128, M)), (W, (*by, rows, K)), (w_scales, (*by, _up128(rows), K // 128)), (h_codes, (M, N)),
+                (h_scales, (N // 128, M)), (saved, (M, 2 * N)))
+    need = (lutq_fp8_gated_workspace_bytes if gated else lutq_fp8_workspace_bytes)(M, N, K, experts)
+    if need == 0:
+        raise ValueError(f"{name}: unsupported problem: {_FP8_DOMAIN}, M and experts within their limits")
+    head = [X.data_ptr(), _ptr(x_scales), W.data_ptr(), w_scales.data_ptr()]
+    tail = [workspace.data_ptr(), workspace.numel(), on]
+    sizes = [*(() if offsets is None else (offsets.data_ptr(), experts)), M, N, K]
+    with torch.cuda.device(device):
+        if gated:
+            _check(getattr(load_library(), name)(*head, *sizes, act, code, _ptr(Y), _ptr(h_codes), _ptr(h_scales), _ptr(saved), *tail), name)
+        else:
+            _check(getattr(load_library(), name)(*head, *sizes, code, Y.data_ptr(), *tail), name)
+    return out
+
+
+def lutq_fp8_matmul(X, W, w_scales, Y, workspace, x_scales=None, stream=None):
+    """Y [M, N] = X W^T.  X: codes [M, K] with x_scales [K / 128, M], or values [M, K] of Y's dtype, which are quantised on the way
+    in.  W: codes [N, K] with w_scales [ceil(N / 128), K / 128]."""
+    return _fp8_product("lutq_fp8_matmul", X, x_scales, W, w_scales, None, Y, workspace, stream)
+
+
+def lutq_fp8_matmul_grouped(X, W, w_scales, offsets, Y, workspace, x_scales=None, stream=None):
+    """The same by expert: rows offsets[g] .. offsets[g + 1] (int32, on the device) of X times the weights of expert g; W [experts, N, K],
+    w_scales [experts, ceil(N / 128), K / 128].  Rows outside stay as they were."""
+    if offsets is None:
+        raise TypeError("lutq_fp8_matmul_grouped: offsets must be int32, [experts + 1]")
+    return _fp8_product("lutq_fp8_matmul_grouped", X, x_scales, W, w_scales, offsets, Y, workspace, stream)
+
+
+def _fp8_activation(name, activation):
+    if activation not in _FP8_ACTIVATIONS:
+        raise ValueError(f"{name}: activation must be one of {', '.join(_FP8_ACTIVATIONS)}")
+    return _FP8_ACTIVATIONS[activation]
+
+
+def _fp8_gated(name, X, W, w_scales, offsets, H, workspace, x_scales, activation, h_scales, saved, dtype, stream):
+    act = _fp8_activation(name, activation)
+    if h_scales is None:
+        return _fp8_product(name, X, x_scales, W, w_scales, offsets, H, workspace, stream, (act, H.dtype, None, None, saved))
+    if dtype is None:
+        dtype = X.dtype if x_scales is None else None if saved is None else saved.dtype
+        if dtype is None:
+            raise TypeError(f"{name}: dtype, to which H is rounded before it is quantised, has to be given where X is codes")
+    return _fp8_product(name, X, x_scales, W, w_scales, offsets, None, workspace, stream, (act, dtype, H, h_scales, saved))
+
+
+def lutq_fp8_gated(X, W, w_scales, H, workspace, x_scales=None, activation="silu", h_scales=None, saved=None, dtype=None, stream=None):
+    """H [M, F] = act(X G^T) * (X U^T), W [2 F, K] = G over U, X as for lutq_fp8_matmul; activation "silu" or "gelu" (tanh form).
+    H: float16 or bfloat16; or, with h_scales [F / 128, M], codes, quantised from H rounded to `dtype` (that of X where it is no
+    codes).  saved [M, 2 F]: takes the two projections side by side, for lutq_fp8_gated_grad."""
+    return _fp8_gated("lutq_fp8_gated", X, W, w_scales, None, H, workspace, x_scales, activation, h_scales, saved, dtype, stream)
+
+
+def lutq_fp8_gated_grouped(X, W, w_scales, offsets, H, workspace, x_scales=None, activation="silu", h_scales=None, saved=None, dtype=None,
+                           stream=None):
+    """The same by expert, as lutq_fp8_matmul_grouped: W [experts, 2 F, K].  Rows outside stay as they were in every output."""
+    if offsets is None:
+        raise TypeError("lutq_fp8_gated_grouped: offsets must be int32, [experts + 1]")
+    return _fp8_gated("lutq_fp8_gated_grouped", X, W, w_scales, offsets, H, workspace, x_scales, activation, h_scales, saved, dtype, stream)
+
+
+def lutq_fp8_gated_grad(dH, saved, activation="silu", dense=None, rows=None, columns=None, stream=None):
+    """From dH [M, F] and saved [M, 2 F] the gradients of the two projections, side by side, as any of: dense [M, 2 F]; rows=(codes
+    [M, 2 F], scales [2 F / 128, M]), whose product with the transposed weights is the gradient of X; columns=(codes [2 F, M'], scales
+    [M' / 128, 2 F]), a factor of the gradient of the weights."""
+    name = "lutq_fp8_gated_grad"
+    act = _fp8_activation(name, activation)
+    (r_codes, r_scales), (c_codes, c_scales) = (None, None) if rows is None else rows, (None, None) if columns is None else columns
+    device, on = _mx4_tensors(name, stream, dH, saved, dense, r_codes, r_scales, c_codes, c_scales)
+    _fp8_codes(name, r_codes, c_codes)
+    _fp8_scales(name, r_scales, c_scales)
+    code = _dtype_code(dH)
+    if any(t is not None and t.dtype != dH.dtype for t in (saved, dense)):
+        raise TypeError(f"{name}: dH, saved and dense must share one dtype")
+    _fp8_dims(name, (dH, 2))
+    M, F = dH.shape
+    _fp8_shapes(name, (saved, (M, 2 * F)), (dense, (M, 2 * F)), (r_codes, (M, 2 * F)), (r_scales, (2 * F // 128, M)),
+                (c_codes, (2 * F, 128 * _up128(M))), (c_scales, (_up128(M), 2 * F)))
+    if dense is None and rows is None and columns is None:
+        raise ValueError(f"{name}: none of dense, rows, columns is given")
+    with _torch().cuda.device(device):
+        _check(load_library().lutq_fp8_gated_grad(dH.data_ptr(), saved.data_ptr(), M, F, act, code, _ptr(dense), _ptr(r_codes), _ptr(r_scales),
+                                                  _ptr(c_codes), _ptr(c_scales), on), name)
+
+
+def lutq_fp8_weight_grad(dY, dy_scales, X, x_scales, dW, workspace, stream=None):
+    """dW [N, K] (float16 or bfloat16) = the sum over rows of dY times X, both by columns: codes [N, M'] with scales [M' / 128, N], codes
+    [K, M'] with scales [M' / 128, K].  workspace: new_fp8_workspace(N, K, M')."""
+    name = "lutq_fp8_weight_grad"
+    device, on = _mx4_tensors(name, stream, dY, dy_scales, X, x_scales, dW, workspace)
+    _fp8_codes(name, dY, X)
+    _fp8_scales(name, dy_scales, x_scales)
+    if workspace.dtype != _torch().uint8:
+        raise TypeError(f"{name}: workspace must be uint8")
+    code = _dtype_code(dW)
+    _fp8_dims(name, (dY, 2), (dW, 2))
+    (N, K), M = dW.shape, dY.shape[1]
+    _fp8_shapes(name, (dY, (N, M)), (dy_scales, (M // 128, N)), (X, (K, M)), (x_scales, (M // 128, K)))
+    with _torch().cuda.device(device):
+        _check(load_library().lutq_fp8_weight_grad(dY.data_ptr(), dy_scales.data_ptr(), X.data_ptr(), x_scales.data_ptr(), N, K, M, code,
+                                                   dW.data_ptr(), workspace.data_ptr(), workspace.numel(), on), name)
+    return dW
+
+
 # ------------------------------------------------------------------ measurement helpers
 def calib_stream_read(src, grid: int, sink, stream=None):
     _check(load_library().lutq_calib_stream_read(src.data_ptr(), src.numel() * src.element_size(), grid,
@@ -801,6 +1094,15 @@ def calib_mx4_launch(M: int, N: int, K: int, experts: int = 0, codes: bool = Fal
 
 TRACE_STAMPS = ("start", "arguments arrived", "first loads issued", "table built", "first tile multiplied",
                 "K loop done", "waves reduced", "outputs stored")
+
+
+def calib_fp8_launch(M: int, N: int, K: int, experts: int = 0, form: str = "matmul", codes: bool = False, compute_units: int = 256) -> Mx4Launch:
+    """How the library launches lutq_fp8_matmul (form "matmul"), lutq_fp8_gated ("gated", N is F; with experts the ones by expert), or
+    lutq_fp8_weight_grad ("weight_grad"; its N, K, M as M, N, K)."""
+    out = (ctypes.c_int * 8)()
+    _check(load_library().lutq_calib_fp8_launch(M, N, K, experts, ("matmul", "gated", "weight_grad").index(form), int(codes), compute_units, out),
+           "lutq_calib_fp8_launch")
+    return Mx4Launch(bool(out[0]), *out[1:7], bool(out[7]))
 
 
 def calib_matmul_trace(X, packed, scales, lut, bits: int, group_size: int, Y, workspace, trace, stream=None,

@@ -1,0 +1,834 @@
+// Products of the 8-bit form (include/lutq.h): Y = X W^T, the same by expert, the gated block's two projections with its activation and
+// product, and the gradient of weights, on v_mfma_scale_f32_16x16x128_f8f6f4.
+//
+// One instruction sums the products of 128 columns of sixteen rows of either factor, which is one block of the scales: what it returns is multiplied
+// with the two blocks' scales in 32 bits and added to the sums.  The scales of the gradient's factors are powers of two, which the
+// instruction applies itself.
+// Its first operand is the weights, so a lane's four sums are neighbours in a row of Y.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "lutq.h"
+#include "lutq_calib.h"
+#include "lutq_fp8_device.hpp"
+#include "lutq_layout.hpp"
+#include "lutq_product.hpp"
+
+namespace lutq {
+namespace fp8 {
+
+using namespace product;
+
+lutq_status quantize_rows_on(const void* X, int source, int64_t source_rows, const int32_t* rows, const int32_t* offsets, int64_t experts,
+                             int64_t M, int64_t K, void* codes, float* scales, hipStream_t stream);
+
+// kGated: a workgroup's row blocks are half of the gate's weights, half of the others', the same columns of H.  kPowers: both factors'
+// scales are powers of two, one per row and block of 128 columns.
+enum Mode { kPlain = 0, kGated = 1, kPowers = 2 };
+
+struct ProductParams {
+    const char* x;             // codes [M, K]; or 16-bit values
+    const float* xs;           // scales [KT, M]
+    const char* w;             // codes [N, K] (kGated: [2 N, K])
+    const float* ws;           // scales [ceil(N / 128), KT] (kPowers: [KT, N])
+    char* y;                   // [M, N]
+    char* saved;               // kGated: [M, 2 N] or null
+    const int32_t* offsets;    // by expert: experts + 1; else null
+    uint32_t* counters;        // K in slices: how many of a tile's are done, and
+    char* partial;             // their sums
+    int64_t expert, expert_scales;             // bytes of an expert's weights, numbers of its scales
+    int M, N, K, KT, NB;       // blocks of 128 columns, of sixteen columns of Y
+    int experts;
+    int slot0, slots;          // first piece of rows of this launch, and how many
+    int slices;                // of K
+    int bf16;                  // type of Y
+    int act;
+    int once;                  // weights that are read once and do not stay in the caches: past them
+    int place_rows;            // streamed: rows of X that a wavefront's place in LDS holds
+};
+
+// H from sums of the gate's and the other projection.
+__device__ __forceinline__ f32x4 gated(const f32x4& g, const f32x4& u, int act) {
+    f32x4 h;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) h[j] = activated(g[j], act) * u[j];
+    return h;
+}
+
+// Four neighbouring sums of a row, as 16-bit values.
+__device__ __forceinline__ void store_four(char* to, const f32x4& sum, int bf16) {
+    *reinterpret_cast<u32x2*>(to) = u32x2{round_pair(sum[0], sum[1], bf16), round_pair(sum[2], sum[3], bf16)};
+}
+
+// Few rows: a workgroup owns R row blocks of weights (kGated: one of each projection) and sixteen rows of X over all of K; its wavefronts take
+// the quads (four blocks of 128 columns) in turn, and their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the
+// weights, which go from memory into the operand registers as they lie, all of a quad asked for at once.
+// 16-bit values (SRC 1, 2) are quantised on the way, ROWS at a time, by the sixteen lanes that hold a block, and the codes pass through a place of
+// the wavefront's own in LDS.  ROWS says what is likely; any number of rows is right.
+constexpr int kRowPitch = 512 + 16;                    // bytes of a row's codes of a quad; the rest keeps the rows in different banks
+
+template <int SRC, int R, int ROWS, int MODE, bool GROUPED>
+__global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const ProductParams p) {
+    static_assert(MODE != kGated || R == 2, "a row block of each projection");
+    extern __shared__ __align__(16) char smem[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6, i = lane & 15, o = lane >> 4;
+    const int slot = p.slot0 + (int)blockIdx.y;
+    int expert = 0, m0 = slot * 16, m1 = min(p.M, m0 + 16);
+    if constexpr (GROUPED) {
+        Pieces<16> pieces{p.offsets, p.experts, p.M};
+        if (slot >= pieces.count()) return;
+        const auto in = pieces.find(slot);
+        expert = in.expert;
+        m0 = in.first + (slot - in.begin) * 16;
+        m1 = min(in.end, m0 + 16);
+    }
+    constexpr int kBlocks = MODE == kGated ? 1 : R;    // row blocks of Y
+    const int rb0 = (int)blockIdx.x * kBlocks, rows = m1 - m0;
+    const char* w[R];
+    const float* ws[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int64_t row = MODE == kGated ? (int64_t)r * p.N + rb0 * 16 : (int64_t)min(rb0 + r, p.NB - 1) * 16;
+        w[r] = p.w + expert * p.expert + row * p.K;
+        ws[r] = p.ws + expert * p.expert_scales + (row >> 7) * p.KT;
+    }
+    char* const place = smem + wave * (p.place_rows * (kRowPitch + 16));
+    float* const place_scales = reinterpret_cast<float*>(place + p.place_rows * kRowPitch);
+    const uint32_t mine = (uint32_t)i * (uint32_t)p.K + o * 16;
+
+    f32x4 acc[R] = {};
+    const int quads = (p.KT + 3) >> 2;
+    for (int q = wave; q < quads; q += waves) {
+        const int tiles = min(4, p.KT - 4 * q);
+        // X first: loads are waited for in order, and it has further to go.  Rows that do not exist stay unread, and whatever lies in their
+        // operands is multiplied: their sums are not stored.
+        u32x4 xv[4][2] = {};
+        float xs[4] = {};
+        Eight<SRC == kF32 ? kF16 : SRC> few[ROWS];
+        const bool there = o < tiles;
+        auto ask_few = [&](int first) {                // lane 16 block + piece
+            const char* from = p.x + ((int64_t)(m0 + first) * p.K + q * 512 + lane * 8) * 2;
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k)
+                if (first + k < rows && there) few[k].v[0] = *reinterpret_cast<const u32x4*>(from + (int64_t)k * p.K * 2);
+        };
+        if constexpr (SRC == kF32) {
+            const char* from = p.x + (int64_t)(m0 + i) * p.K + q * 512 + o * 16;
+            if (i < rows) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const int at = min(t, tiles - 1);
+                    xv[t][0] = *reinterpret_cast<const u32x4*>(from + at * 128);
+                    xv[t][1] = *reinterpret_cast<const u32x4*>(from + at * 128 + 64);
+                    xs[t] = p.xs[(int64_t)(4 * q + at) * p.M + m0 + i];
+                }
+            }
+        } else {
+            ask_few(0);
+        }
+        u32x4 wv[R][4][2];
+        float sw[R][4];
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) sw[r][t] = ws[r][4 * q + min(t, tiles - 1)];
+        auto ask = [&](auto how) {
+            constexpr int HOW = decltype(how)::value;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    const int at = (4 * q + min(t, tiles - 1)) * 128;
+                    wv[r][t][0] = __builtin_amdgcn_raw_buffer_load_b128(unbounded(w[r]), mine, at, HOW);
+                    wv[r][t][1] = __builtin_amdgcn_raw_buffer_load_b128(unbounded(w[r]), mine, at + 64, HOW);
+                }
+        };
+        if (p.once) ask(std::integral_constant<int, kNonTemporal>());
+        else ask(std::integral_constant<int, 0>());
+        if constexpr (SRC != kF32) {
+            for (int first = 0; first < rows; first += ROWS) {
+                if (first > 0) ask_few(first);
+#pragma unroll
+                for (int k = 0; k < ROWS; ++k) {
+                    if (first + k >= rows || !there) continue;
+                    float v[8];
+                    to_floats<SRC>(few[k], v);
+                    const Scale s = scale_of(largest_of_sixteen(largest(v)));
+                    *reinterpret_cast<u32x2*>(place + (first + k) * kRowPitch + lane * 8) = to_codes(v, s);
+                    if (i == 0) place_scales[(first + k) * 4 + o] = s.scale;
+                }
+            }
+            between_lanes();
+            if (i < rows) {
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    if (t >= tiles) break;
+                    xv[t][0] = *reinterpret_cast<const u32x4*>(place + i * kRowPitch + t * 128 + o * 16);
+                    xv[t][1] = *reinterpret_cast<const u32x4*>(place + i * kRowPitch + t * 128 + o * 16 + 64);
+                    xs[t] = place_scales[i * 4 + t];
+                }
+            }
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            if (t >= tiles) break;
+            const i32x8 x = operand(xv[t][0], xv[t][1]);
+#pragma unroll
+            for (int r = 0; r < R; ++r) acc[r] += product(operand(wv[r][t][0], wv[r][t][1]), x, f32x4{0.f, 0.f, 0.f, 0.f}) * (xs[t] * sw[r][t]);
+        }
+        if constexpr (SRC != kF32) between_lanes();
+    }
+
+    __syncthreads();
+    f32x4* sums = reinterpret_cast<f32x4*>(smem);      // [wave][row block][lane]
+#pragma unroll
+    for (int r = 0; r < R; ++r) sums[(wave * R + r) * 64 + lane] = acc[r];
+    __syncthreads();
+    auto sum_of = [&](int r) {
+        f32x4 sum = sums[r * 64 + lane];
+        for (int v = 1; v < waves; ++v) sum += sums[(v * R + r) * 64 + lane];
+        return sum;
+    };
+    if constexpr (MODE == kGated) {
+        if (wave > 0 || i >= rows) return;
+        const f32x4 g = sum_of(0), u = sum_of(1);
+        const int64_t row = m0 + i;
+        const int column = 16 * rb0 + 4 * o;
+        store_four(p.y + (row * p.N + column) * 2, gated(g, u, p.act), p.bf16);
+        if (p.saved) {
+            store_four(p.saved + (row * 2 * p.N + column) * 2, g, p.bf16);
+            store_four(p.saved + (row * 2 * p.N + p.N + column) * 2, u, p.bf16);
+        }
+    } else {
+        for (int r = wave; r < R; r += waves)
+            if (i < rows && rb0 + r < p.NB) store_four(p.y + ((int64_t)(m0 + i) * p.N + 16 * (rb0 + r) + 4 * o) * 2, sum_of(r), p.bf16);
+    }
+}
+
+// Many rows: a workgroup of GN x GM wavefronts makes tiles of Y, 16 WN GN rows of weights times 16 WM GM rows of X, each wavefront WN x WM
+// blocks of sixteen by sixteen.  K goes by in steps of 128 columns, which are copied from memory into LDS without passing
+// through registers; there is room for DEPTH steps, so DEPTH - 1 are under way while one is multiplied.  A step's scales come the same way.
+//
+// There are at most as many workgroups as run at once, and each takes one tile of Y after the other.  The copies run ahead across the
+// tiles' borders: while one is finished and stored, the first steps of the next are under way.
+//
+// In LDS a piece is sixteen rows of 128 bytes, whole cache lines as they are read; sixteen bytes b of row i lie at 16 (b ^ (i >> 1)), so that the
+// sixteen lanes that are served together hit all banks.  A lane's operand is the sixteens o and o + 4 of its row: both factors' columns are in
+// the same order, which is all that the products need.
+//
+// Where Y has too few tiles for the device, K is cut into slices as well.  Each slice leaves its sums in the
+// workspace, and the last workgroup of a tile to finish adds them in the order of the slices.  No workgroup waits for another: the sums are
+// stored past the caches that the dies do not share (sc1), complete before the workgroup counts itself, and read the same way.
+template <int WN, int WM, int GN, int GM, int DEPTH, int MODE> struct TileShape {
+    static constexpr int kWaves = GN * GM, kThreads = 64 * kWaves;
+    static constexpr int kRB = WN * GN, kMB = WM * GM;                         // pieces of sixteen rows of either factor
+    static constexpr int kBlocks = MODE == kGated ? kRB / 2 : kRB;             // row blocks of Y
+    static constexpr int kStep = (kRB + kMB) * 2048;
+    // Scales of a step, in pieces of 64: of the rows of X, then of the weights (kPowers: of their rows, else of their blocks).
+    static constexpr int kXPieces = kMB / 4, kScalePieces = kXPieces + (MODE == kPowers ? kRB / 4 : 1);
+    static constexpr int kScales = kScalePieces * 256;
+    static constexpr int kLds = DEPTH * (kStep + kScales) + 16;
+    static constexpr bool kSlices = WN * WM <= 8;      // (the join of slices holds four times a tile's sums)
+    static constexpr int kSums = kWaves * WN * WM * 1024;                      // bytes of a tile's sums
+};
+
+template <int WN, int WM, int GN, int GM, int DEPTH, int MODE, bool GROUPED>
+__global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductParams p) {
+    using Shape = TileShape<WN, WM, GN, GM, DEPTH, MODE>;
+    constexpr int kWaves = Shape::kWaves, kRB = Shape::kRB, kMB = Shape::kMB, kStep = Shape::kStep, kBlocks = Shape::kBlocks;
+    // Copies per wavefront and step, eight rows each, and one of scales.
+    constexpr int kWLoads = 2 * kRB / kWaves, kXLoads = 2 * kMB / kWaves, kScaleLoads = (Shape::kScalePieces + kWaves - 1) / kWaves;
+    constexpr int kLoads = kWLoads + kXLoads + kScaleLoads;
+    constexpr int kRing = WN < 4 ? WN : 4;             // row blocks of weights in registers
+    constexpr int kTurn = WN - kRing + 1;              // the row block at which the next step is looked at
+    static_assert(kWLoads * kWaves == 2 * kRB && kXLoads * kWaves == 2 * kMB && kMB % 4 == 0 && kRB % 4 == 0, "whole loads per wavefront");
+    static_assert(MODE != kGated || kWLoads % 2 == 0, "as many of either projection");
+    extern __shared__ __align__(1024) char lds[];      // DEPTH steps, then their scales, then a word
+    char* const scale_places = lds + DEPTH * kStep;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int i = lane & 15, o = lane >> 4;
+
+    const int nx = (p.NB + kBlocks - 1) / kBlocks;
+    Pieces<16 * kMB> pieces{p.offsets, p.experts, p.M};
+    int slots = p.slots;
+    if constexpr (GROUPED) slots = min(slots, pieces.count() - p.slot0);
+    const int total = slots * nx * p.slices;           // tiles of Y, each `slices` times
+
+    struct Item { int expert, m0, m1, rb0, tile, slice, step, steps; };        // step .. steps - 1 of the whole of K
+    // The tiles of an expert (without experts: all) are ordered in bands of at most kBand pieces of rows of X, so that what a die's cache holds
+    // of either factor is used several times; higher ones by expert, whose weights come from memory.
+    auto item = [&](int number) {
+        constexpr int kBand = GROUPED ? 8 : 4;
+        Item it;
+        const int id = by_die(number, total);
+        it.tile = p.slices == 1 ? id : quotient(id, p.slices);
+        it.slice = id - it.tile * p.slices;
+        int inside = it.tile, from = p.slot0, n = slots;                       // the tile's place among those of its expert's pieces
+        typename Pieces<16 * kMB>::Found in{0, 0, p.M, 0, 0};
+        if constexpr (GROUPED) {
+            in = pieces.find(p.slot0 + quotient(it.tile, nx));
+            from = max(in.begin, p.slot0);
+            n = min(in.begin + in.pieces, p.slot0 + slots) - from;
+            inside -= (from - p.slot0) * nx;
+        }
+        const int bands = (n + kBand - 1) / kBand, high = quotient(n + bands - 1, bands);
+        const int band = quotient(inside, high * nx), left = min(high, n - band * high);
+        inside -= band * high * nx;
+        const int nt = quotient(inside, left);
+        it.expert = in.expert;
+        it.m0 = in.first + (from + band * high + inside - nt * left - in.begin) * 16 * kMB;
+        it.m1 = min(in.end, it.m0 + 16 * kMB);
+        it.rb0 = nt * kBlocks;
+        it.step = 0;
+        it.steps = p.KT;
+        if (p.slices > 1) {                            // (up to 2^15 steps and eight slices: the product fits)
+            it.step = quotient(it.slice * p.KT, p.slices);
+            it.steps = quotient((it.slice + 1) * p.KT, p.slices);
+        }
+        return it;
+    };
+
+    // Where the copies are: an item, its next step, the place they go to, and this lane's byte offsets in what the wavefront copies.  Rows
+    // past the end repeat the last.
+    const int block = (lane & 7) ^ (lane >> 4);        // of the row that this lane copies (i >> 1 of row i = 8 c + lane / 8 is 4 (c & 1) + lane / 16)
+    int number = (int)blockIdx.x, step = 0, steps = 0, place = 0;
+    __amdgpu_buffer_rsrc_t wsrc, usrc, xsrc;
+    const char* ssrc[kScaleLoads];                     // scales of step 0, and
+    int64_t sstep[kScaleLoads];                        // bytes from one step to the next
+    uint32_t wfrom[kWLoads], xfrom[kXLoads], sfrom[kScaleLoads];
+    // Eight rows `c` of the weights' list, gate before others: where they lie in LDS (in pieces of eight rows).
+    auto w_place = [&](int c) {
+        if constexpr (MODE != kGated) return c;
+        const int other = c >= kRB, b = (c - other * kRB) >> 1;                // row block of the tile, of either projection
+        return 2 * (b / (WN / 2) * WN + other * (WN / 2) + b % (WN / 2)) + (c & 1);
+    };
+    auto aim = [&](const Item& it) {
+        step = it.step;
+        steps = it.steps;
+        const int last_row = (p.NB - it.rb0) * 16 - 1, rows = it.m1 - it.m0;
+        const char* w = p.w + it.expert * p.expert + (int64_t)it.rb0 * 16 * p.K;
+        wsrc = unbounded(w);
+        if constexpr (MODE == kGated) usrc = unbounded(w + (int64_t)p.N * p.K);
+        xsrc = unbounded(p.x + (int64_t)it.m0 * p.K);
+#pragma unroll
+        for (int j = 0; j < kWLoads; ++j) {
+            int c = wave + kWaves * j;
+            if (MODE == kGated && j >= kWLoads / 2) c -= kRB;
+            wfrom[j] = (uint32_t)min(8 * c + (lane >> 3), last_row) * (uint32_t)p.K + (block ^ (4 * (c & 1))) * 16;
+        }
+#pragma unroll
+        for (int j = 0; j < kXLoads; ++j) {
+            const int c = wave + kWaves * j;
+            xfrom[j] = (uint32_t)min(8 * c + (lane >> 3), rows - 1) * (uint32_t)p.K + (block ^ (4 * (c & 1))) * 16;
+        }
+#pragma unroll
+        for (int j = 0; j < kScaleLoads; ++j) {
+            const int c = (wave + kWaves * j) % Shape::kScalePieces;           // (some are copied twice)
+            if (c < Shape::kXPieces) {
+                ssrc[j] = reinterpret_cast<const char*>(p.xs + it.m0);
+                sstep[j] = (int64_t)p.M * 4;
+                sfrom[j] = min(64 * c + lane, rows - 1) * 4;
+            } else if constexpr (MODE == kPowers) {
+                ssrc[j] = reinterpret_cast<const char*>(p.ws + it.rb0 * 16);
+                sstep[j] = (int64_t)p.N * 4;
+                sfrom[j] = min(64 * (c - Shape::kXPieces) + lane, last_row) * 4;
+            } else {                                   // the first blocks from the tile's on; kGated: one of the gate's and one of the others'
+                ssrc[j] = reinterpret_cast<const char*>(p.ws + it.expert * p.expert_scales + (int64_t)(it.rb0 >> 3) * p.KT);
+                sstep[j] = 4;
+                const int here = MODE == kGated ? min(lane, 1) * (p.N >> 7) : min(lane, min(1, (last_row >> 7)));
+                sfrom[j] = (uint32_t)here * (uint32_t)p.KT * 4;
+            }
+        }
+    };
+    // Copy `j` of this wavefront's kLoads of a step.
+    auto load_part = [&](int j) {
+        char* to = lds + place * kStep;
+        if (j < kWLoads) {
+            const int c = wave + kWaves * j;
+            copy16(MODE == kGated && j >= kWLoads / 2 ? usrc : wsrc, wfrom[j], step * 128, to + w_place(c) * 1024);
+        } else if (j < kWLoads + kXLoads) {
+            const int c = wave + kWaves * (j - kWLoads);
+            copy16(xsrc, xfrom[j - kWLoads], step * 128, to + kRB * 2048 + c * 1024);
+        } else {
+            const int s = j - kWLoads - kXLoads, c = (wave + kWaves * s) % Shape::kScalePieces;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(unbounded(ssrc[s] + step * sstep[s]),
+                (__attribute__((address_space(3))) void*)(scale_places + place * Shape::kScales + c * 256), 4, sfrom[s], 0, 0, 0);
+        }
+    };
+    Item ahead = {};
+    auto next = [&]() {
+        place = (place + 1) % DEPTH;
+        if (++step < steps) return;
+        // (After the last item its last step is copied again and again, to places that nobody reads any more: as many copies are under way
+        // at every step.)
+        if (number + (int)gridDim.x < total) {
+            number += (int)gridDim.x;
+            ahead = item(number);
+            aim(ahead);
+        } else --step;
+    };
+
+    const int wn = wave % GN, wm = wave / GN;
+    i32x8 w[kRing], x[WM];
+    float xs[WM], ws[MODE == kGated ? 2 : 1];          // scales of the step in the registers
+    uint32_t we[kRing];
+    f32x4 acc[WN][WM];
+    int here = 0;                                      // the place of the step being multiplied
+    const char* const wplace = lds + i * 128 + wn * WN * 2048;
+    const char* const xplace = lds + kRB * 2048 + i * 128 + wm * WM * 2048;
+    const int first_half = (o ^ (i >> 1)) * 16, second_half = ((4 + o) ^ (i >> 1)) * 16;
+    auto read = [&](const char* at) {
+        return operand(*reinterpret_cast<const u32x4*>(at + first_half), *reinterpret_cast<const u32x4*>(at + second_half));
+    };
+    auto scale_at = [&](int from, int n) { return *reinterpret_cast<const float*>(scale_places + from * Shape::kScales + n * 4); };
+    auto read_w = [&](int from, int r) {
+        w[r % kRing] = read(wplace + from * kStep + r * 2048);
+        if constexpr (MODE == kPowers) we[r % kRing] = __builtin_bit_cast(uint32_t, scale_at(from, Shape::kXPieces * 64 + 16 * (wn * WN + r) + i)) >> 23;
+    };
+    auto read_x = [&](int from, int b) { x[b] = read(xplace + from * kStep + b * 2048); };
+    auto read_scales = [&](int from) {
+#pragma unroll
+        for (int b = 0; b < WM; ++b) xs[b] = scale_at(from, 16 * (wm * WM + b) + i);
+        if constexpr (MODE == kPlain) ws[0] = scale_at(from, Shape::kXPieces * 64 + wn * WN / 8);
+        if constexpr (MODE == kGated) {
+            ws[0] = scale_at(from, Shape::kXPieces * 64);
+            ws[1] = scale_at(from, Shape::kXPieces * 64 + 1);
+        }
+    };
+
+    // A step: row block by row block of the weights.  Its X and its first kRing - 1 row blocks are in the registers; the others, and at the end
+    // the next step's, are read kRing - 1 row blocks ahead, X as soon as its last product has been started.  What an instruction
+    // returns is added after the next one has been started.
+    f32x4 pending = {};
+    float pending_scale = 0.f;
+    auto one_step = [&](bool stored) {
+        float s[MODE == kGated ? 2 : 1][WM];
+        uint32_t xe[WM];
+#pragma unroll
+        for (int b = 0; b < WM; ++b) {
+            if constexpr (MODE == kPowers) xe[b] = __builtin_bit_cast(uint32_t, xs[b]) >> 23;
+            else {
+#pragma unroll
+                for (int h = 0; h < (MODE == kGated ? 2 : 1); ++h) s[h][b] = xs[b] * ws[h];
+            }
+        }
+        const int from = here;
+#pragma unroll
+        for (int r = 0; r < WN; ++r) {
+            if (r == kTurn) {
+                next();
+                here = (here + 1) % DEPTH;
+                // The next step is there, and nobody needs this one's place any more.
+                constexpr int kStores = MODE == kGated ? 0 : WN / 2 * WM;
+                if (stored) arrive<(DEPTH - 2) * kLoads + kStores>();
+                else arrive<(DEPTH - 2) * kLoads>();
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (r + kRing - 1 < WN) read_w(from, r + kRing - 1);
+            else read_w(here, r + kRing - 1 - WN);
+            if (r == WN - 1) read_scales(here);
+#pragma unroll
+            for (int b = 0; b < WM; ++b) {
+                if constexpr (MODE == kPowers) {
+                    acc[r][b] = scaled_product(w[r % kRing], x[b], acc[r][b], we[r % kRing], xe[b]);
+                } else {
+                    const f32x4 sums = product(w[r % kRing], x[b], f32x4{0.f, 0.f, 0.f, 0.f});
+                    f32x4& last = b ? acc[r][b - 1] : r ? acc[r - 1][WM - 1] : acc[WN - 1][WM - 1];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) last[j] = __builtin_fmaf(pending[j], pending_scale, last[j]);
+                    pending = sums;
+                    pending_scale = s[MODE == kGated && r >= WN / 2][b];
+                }
+                if (r == WN - 1) read_x(here, b);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (r >= kTurn) {
+                constexpr int kRows = WN - kTurn;
+#pragma unroll
+                for (int j = (r - kTurn) * kLoads / kRows; j < (r - kTurn + 1) * kLoads / kRows; ++j) load_part(j);
+            }
+        }
+    };
+
+    // Two wavefronts share a SIMD, and the older one is served first by itself: with the younger ones preferred they drift apart, and one
+    // multiplies while the other waits.
+    if (kWaves == 8 && wave >= 4) __builtin_amdgcn_s_setprio(1);
+    if (number >= total) return;
+    Item it = item(number);
+    aim(it);
+#pragma unroll
+    for (int t = 0; t < DEPTH; ++t) {
+#pragma unroll
+        for (int j = 0; j < kLoads; ++j) load_part(j);
+        if (t < DEPTH - 1) next();
+    }
+    arrive<(DEPTH - 1) * kLoads>();
+#pragma unroll
+    for (int r = 0; r < kRing - 1; ++r) read_w(0, r);
+#pragma unroll
+    for (int b = 0; b < WM; ++b) read_x(0, b);
+    read_scales(0);
+
+    bool stored = false;
+    for (int mine = (int)blockIdx.x;;) {
+#pragma unroll
+        for (int r = 0; r < WN; ++r)
+#pragma unroll
+            for (int b = 0; b < WM; ++b) acc[r][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+        pending = f32x4{0.f, 0.f, 0.f, 0.f};
+        pending_scale = 0.f;
+        mine += (int)gridDim.x;
+        int s = it.step;
+        one_step(stored);
+        for (++s; s < it.steps; ++s) one_step(false);
+        if constexpr (MODE != kPowers) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[WN - 1][WM - 1][j] = __builtin_fmaf(pending[j], pending_scale, acc[WN - 1][WM - 1][j]);
+        }
+
+        bool finished = true;
+        if (Shape::kSlices && p.slices > 1) {          // the other slices of this tile
+            const auto sums = unbounded(p.partial + ((int64_t)it.tile * p.slices) * Shape::kSums);
+            const uint32_t at = wave * (WN * WM * 1024) + lane * 16;
+#pragma unroll
+            for (int r = 0; r < WN; ++r)
+#pragma unroll
+                for (int b = 0; b < WM; ++b) store16_shared(sums, at + (r * WM + b) * 1024, it.slice * Shape::kSums, acc[r][b]);
+            arrive<0>();
+            uint32_t* last = reinterpret_cast<uint32_t*>(lds + Shape::kLds - 16);
+            if (threadIdx.x == 0) {
+                uint32_t* count = p.counters + it.tile;
+                const uint32_t n = __hip_atomic_fetch_add(count, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                *last = n + 1 == (uint32_t)p.slices;
+                if (*last) __hip_atomic_store(count, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            }
+            __syncthreads();
+            finished = __builtin_amdgcn_readfirstlane(*last);
+            __syncthreads();                           // (the word is free for the next item)
+            if (finished) {
+                // In the order of the slices, this one from its registers, the others two ahead.
+                f32x4 sum[WN][WM] = {}, even[WN][WM], odd[WN][WM];
+                auto ask = [&](int z, f32x4(&to)[WN][WM]) {
+                    if (z >= p.slices || z == it.slice) return;
+#pragma unroll
+                    for (int r = 0; r < WN; ++r)
+#pragma unroll
+                        for (int b = 0; b < WM; ++b) to[r][b] = load16_shared(sums, at + (r * WM + b) * 1024, z * Shape::kSums);
+                };
+                auto add = [&](const f32x4(&from)[WN][WM]) {
+#pragma unroll
+                    for (int r = 0; r < WN; ++r)
+#pragma unroll
+                        for (int b = 0; b < WM; ++b) sum[r][b] += from[r][b];
+                };
+                auto take = [&](int z, f32x4(&from)[WN][WM]) {
+                    if (z >= p.slices) return;
+                    if (z == it.slice) add(acc);
+                    else add(from);
+                    ask(z + 2, from);
+                };
+                ask(0, even);
+                ask(1, odd);
+                for (int z = 0; z < p.slices; z += 2) {
+                    take(z, even);
+                    take(z + 1, odd);
+                }
+#pragma unroll
+                for (int r = 0; r < WN; ++r)
+#pragma unroll
+                    for (int b = 0; b < WM; ++b) acc[r][b] = sum[r][b];
+            }
+        }
+        if (finished) {
+#pragma unroll
+            for (int b = 0; b < WM; ++b) {
+                const int m = it.m0 + 16 * (wm * WM + b), rows = it.m1 - m;
+                constexpr int kOut = MODE == kGated ? WN / 2 : WN;             // row blocks of Y
+                const int rb = it.rb0 + wn * kOut, blocks = p.NB - rb;
+                auto store = [&](auto sum, char* y, int width, int column) {
+                    char* to = y + ((int64_t)m * width + column + 16 * rb) * 2;
+                    if constexpr (kOut > 1) store_rows<kOut>(sum, to, rows, blocks, width, p.bf16);
+                    else if (i < rows && blocks > 0) store_four(to + ((int64_t)i * width + 4 * o) * 2, sum(0), p.bf16);
+                };
+                if constexpr (MODE == kGated) {
+                    store([&](int r) { return gated(acc[r][b], acc[r + WN / 2][b], p.act); }, p.y, p.N, 0);
+                    if (p.saved) {
+                        store([&](int r) { return acc[r][b]; }, p.saved, 2 * p.N, 0);
+                        store([&](int r) { return acc[r + WN / 2][b]; }, p.saved, 2 * p.N, p.N);
+                    }
+                } else {
+                    store([&](int r) { return acc[r][b]; }, p.y, p.N, 0);
+                }
+            }
+        }
+        stored = finished;
+        if (mine >= total) break;
+        it = number == mine ? ahead : item(mine);      // (the copies may be further ahead where items have fewer steps than there is room for)
+    }
+    arrive<0>();                                       // (no copy into this workgroup's LDS outlives it)
+}
+
+namespace {
+
+constexpr size_t kCounterBytes = 64 * 1024;
+constexpr int64_t kCounters = kCounterBytes / 4;
+constexpr size_t kPartialBytes = 32 * 1024 * 1024;
+
+int64_t most_pieces(const ProductParams& p, int rows) { return product::most_pieces(p.M, p.offsets ? p.experts : 0, rows); }
+
+template <int SRC, int R, int ROWS, int MODE>
+hipError_t launch_stream(ProductParams p, int waves, hipStream_t s) {
+    constexpr int kBlocks = MODE == kGated ? 1 : R;
+    const int nx = (p.NB + kBlocks - 1) / kBlocks;
+    p.place_rows = SRC == kF32 ? 0 : p.M < 16 ? p.M : 16;
+    const size_t place = (size_t)p.place_rows * (kRowPitch + 16), sums = R * 1024;
+    const size_t lds = waves * (place > sums ? place : sums);
+    // (a launch has fewer than 2^16 workgroups along y and 2^32 threads)
+    int64_t most = (int64_t(1) << 31) / (int64_t(nx) * waves * 64);
+    most = most > 65535 ? 65535 : most;
+    const int64_t slots = most_pieces(p, 16);
+    hipError_t e = hipSuccess;
+    for (int64_t at = 0; at < slots && e == hipSuccess; at += most) {
+        p.slot0 = (int)at;
+        const dim3 grid(nx, (unsigned)(slots - at < most ? slots - at : most));
+        e = p.offsets ? launch<stream_kernel<SRC, R, ROWS, MODE, true>>(grid, waves * 64, lds, p, s)
+                      : launch<stream_kernel<SRC, R, ROWS, MODE, false>>(grid, waves * 64, lds, p, s);
+    }
+    return e;
+}
+
+// Output channels (kGated: of both projections) and rows of a tile, wavefronts, and steps of room, by shape.
+struct TileSize { int channels, rows, waves, room; };
+constexpr TileSize kTiles[] = {{256, 256, 8, 2}, {128, 128, 8, 4}, {128, 64, 8, 4}, {64, 64, 4, 4}};
+
+template <int SHAPE, int WN, int WM, int GN, int GM, int DEPTH, int MODE>
+hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
+    using Shape = TileShape<WN, WM, GN, GM, DEPTH, MODE>;
+    static_assert(kTiles[SHAPE].channels == 16 * Shape::kRB && kTiles[SHAPE].rows == 16 * Shape::kMB && kTiles[SHAPE].waves == Shape::kWaves &&
+                  kTiles[SHAPE].room == DEPTH, "as the choice knows it");
+    constexpr int kAtOnce = 160 * 1024 / Shape::kLds < 8 / Shape::kWaves ? 160 * 1024 / Shape::kLds : 8 / Shape::kWaves;   // per compute unit
+    static_assert(kAtOnce >= 1, "fits a compute unit");
+    const int64_t nx = (p.NB + Shape::kBlocks - 1) / Shape::kBlocks, pieces = most_pieces(p, 16 * Shape::kMB);
+    const int64_t most = (int64_t(1) << 30) / (nx * p.slices);                 // pieces of rows per launch: tiles are counted in 32 bits
+    hipError_t e = hipSuccess;
+    for (int64_t at = 0; at < pieces && e == hipSuccess; at += most) {
+        p.slot0 = (int)at;
+        p.slots = (int)(pieces - at < most ? pieces - at : most);
+        const int64_t items = nx * p.slots * p.slices, grid = items < (int64_t)cus * kAtOnce ? items : (int64_t)cus * kAtOnce;
+        const dim3 g((unsigned)grid);
+        if constexpr (MODE == kPowers) e = launch<tile_kernel<WN, WM, GN, GM, DEPTH, MODE, false>>(g, Shape::kThreads, Shape::kLds, p, s);
+        else e = p.offsets ? launch<tile_kernel<WN, WM, GN, GM, DEPTH, MODE, true>>(g, Shape::kThreads, Shape::kLds, p, s)
+                           : launch<tile_kernel<WN, WM, GN, GM, DEPTH, MODE, false>>(g, Shape::kThreads, Shape::kLds, p, s);
+    }
+    return e;
+}
+
+// Whether the weights are streamed past sixteen rows at a time, or which tile shape, and for the smaller ones how many slices of K: the least
+// of times estimated from the bytes of weights over the pieces of rows (B), or from the number of tiles on the busiest compute unit (n) and of
+// steps (S).  Microseconds.
+struct TileChoice { int shape, slices; };             // shape -1: streamed
+
+// `NB`: row blocks of weights, kGated: of both projections.
+TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, int cus) {
+    const double S = (double)KT;
+    TileChoice best{-1, 1};
+    auto tiles = [&](int64_t rb, int64_t rows) {
+        const int64_t nx = (NB + rb - 1) / rb;
+        if (!experts) return (double)nx * (double)((M + rows - 1) / rows);
+        const double some = (double)(M < experts ? M : experts), filled = (double)M / (double)rows + 0.5 * some;
+        return (double)nx * (filled > some ? filled : some);
+    };
+    if (mode != kPowers && M <= 16 * (experts ? experts : 1)) return best;
+    double least = mode == kPowers ? 1e30 : 2.3 + tiles(1, 16) * (double)KT * 2048.0 / 6.6e6;
+    auto consider = [&](int shape, int slices, double us) {
+        if (us < least) { least = us; best = {shape, slices}; }
+    };
+    auto rounds = [&](double t) { return (double)(int64_t)((t + cus - 1) / cus); };
+    auto pairs = [&](double n, double one, double two) { return two * (double)(int64_t)(n / 2) + ((int64_t)n % 2 ? one : 0.0); };
+    const double t0 = tiles(16, 256), t1 = tiles(8, 128), t2 = tiles(8, 64), t3 = tiles(4, 64);
+    consider(0, 1, 6.0 + rounds(t0) * (1.75 * S + 4.5 * (t0 < cus ? t0 / cus : 1.0)));
+    for (int z = 1; z <= 8; ++z) {
+        if (z > KT) break;
+        const double steps = (double)((int64_t)(S + z - 1) / z);
+        if (z == 1 || t1 * z <= cus) consider(1, z, 3.2 + rounds(t1 * z) * ((t1 > cus ? 0.72 : 0.63) * steps + 1.0) + (z > 1 ? 2.5 + 1.6 * z : 0.0));
+        if (z == 1 || t2 * z <= cus) consider(2, z, 3.2 + rounds(t2 * z) * (0.50 * steps + 0.7) + (z > 1 ? 3.0 + 0.8 * z : 0.0));
+        if (z == 1 || t3 * z <= 2 * cus) consider(3, z, 3.0 + pairs(rounds(t3 * z), 0.37 * steps + 0.9, 0.62 * steps + 0.9) + (z > 1 ? 1.8 + 1.0 * z : 0.0));
+    }
+    if (best.slices > 1) {                             // as many as the workspace has room for
+        const TileSize t = kTiles[best.shape];
+        const int64_t most = (NB * 16 + t.channels - 1) / t.channels * product::most_pieces(M, experts, t.rows);
+        while (best.slices > 1 && (most > kCounters || most * best.slices * t.channels * t.rows * 4 > (int64_t)kPartialBytes)) --best.slices;
+    }
+    return best;
+}
+
+// How a product is launched.
+struct Choice {
+    TileChoice tiles;
+    bool apart;                // X of 16 bits is quantised by a launch of its own
+    bool once;                 // weights past the caches
+    // streamed:
+    int wide;                  // row blocks per workgroup
+    int rows;                  // of X that are quantised at a time, 0: X is codes
+    int waves;                 // per workgroup
+};
+
+// `experts`: 0 without.
+Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool codes, int cus) {
+    Choice c{};
+    const int KQ = (int)((KT + 3) / 4);
+    c.tiles = choose_tiles(M, NB, KT, experts, mode, cus);
+    const int64_t pieces = experts ? (M < experts ? M : experts) : (M + 15) / 16, mean = (M + pieces - 1) / pieces;
+    c.apart = !codes && (c.tiles.shape >= 0 || mean > 4);
+    if (c.apart) codes = true;
+    c.wide = mode == kGated ? 2 : NB * pieces > 1024 && mean > 2 ? 2 : 1;
+    const int64_t groups = (NB + c.wide - 1) / c.wide * pieces;
+    const int64_t shared = c.tiles.shape >= 0 ? 0 : experts ? 4 : 16;
+    c.once = (experts ? mean : M) <= shared && NB * (experts ? pieces : 1) * KT * 2048 > (int64_t(128) << 20);
+    const int most = groups > 4096 ? 4 : c.wide > 1 || groups > 512 ? 8 : 16;
+    c.waves = KQ < most ? KQ : most;
+    c.rows = codes ? 0 : mean > 1 ? 4 : 1;
+    return c;
+}
+
+template <int R, int MODE> hipError_t launch_stream_of(int src, int rows, const ProductParams& p, int waves, hipStream_t s) {
+    if (rows == 0) return launch_stream<kF32, R, 1, MODE>(p, waves, s);
+    if (rows == 1) return src == kF16 ? launch_stream<kF16, R, 1, MODE>(p, waves, s) : launch_stream<kBF16, R, 1, MODE>(p, waves, s);
+    return src == kF16 ? launch_stream<kF16, R, 4, MODE>(p, waves, s) : launch_stream<kBF16, R, 4, MODE>(p, waves, s);
+}
+
+template <int MODE> hipError_t launch_of(const Choice& c, int src, const ProductParams& p, int cus, hipStream_t s) {
+    switch (c.tiles.shape) {
+        case 0: return launch_tiles<0, 8, 4, 2, 4, 2, MODE>(p, cus, s);
+        case 1: return launch_tiles<1, 4, 2, 2, 4, 4, MODE>(p, cus, s);
+        case 2: return launch_tiles<2, 2, 2, 4, 2, 4, MODE>(p, cus, s);
+        case 3: return launch_tiles<3, 2, 2, 2, 2, 4, MODE>(p, cus, s);
+    }
+    if constexpr (MODE == kGated) return launch_stream_of<2, MODE>(src, c.rows, p, c.waves, s);
+    else if constexpr (MODE == kPlain)
+        return c.wide == 1 ? launch_stream_of<1, MODE>(src, c.rows, p, c.waves, s) : launch_stream_of<2, MODE>(src, c.rows, p, c.waves, s);
+    return hipErrorInvalidValue;
+}
+
+// Bytes of the products' scratch before what a gated call adds; 0 if unsupported.
+size_t scratch_bytes(int64_t M, int64_t K) { return kCounterBytes + kPartialBytes + up256((size_t)M * (size_t)K) + up256((size_t)M * (size_t)(K / 128) * 4); }
+
+// What the entry points have in common.  N: columns of Y.
+struct Call {
+    const void* x; const float* xs; const void* w; const float* ws; const int32_t* offsets; int64_t experts;
+    int64_t M, N, K; lutq_dtype dtype; void* y; void* saved; void* h_codes; float* h_scales; int mode, act;
+    void* workspace; size_t workspace_bytes, needed;
+    bool by_expert;
+};
+
+lutq_status product_on(const Call& a, hipStream_t s) {
+    if (a.needed == 0) return LUTQ_ERR_SHAPE;
+    if ((a.dtype != LUTQ_F16 && a.dtype != LUTQ_BF16) || (a.mode == kGated && a.act != LUTQ_SILU && a.act != LUTQ_GELU)) return LUTQ_ERR_DTYPE;
+    if (a.M == 0) return LUTQ_OK;
+    if (!a.x || !a.w || !a.ws || (!a.y && !a.h_codes) || !a.h_codes != !a.h_scales || (a.by_expert && !a.offsets)) return LUTQ_ERR_NULL;
+    if (!aligned(a.x, 16) || !aligned(a.xs, 4) || !aligned(a.w, 16) || !aligned(a.ws, 4) || !aligned(a.y, 16) || !aligned(a.saved, 16) ||
+        !aligned(a.h_codes, 16) || !aligned(a.h_scales, 4) || !aligned(a.workspace, 16) || !aligned(a.offsets, 4))
+        return LUTQ_ERR_ALIGN;
+    if (!a.workspace || a.workspace_bytes < a.needed) return LUTQ_ERR_WORKSPACE;
+
+    ProductParams p{};
+    const int64_t w_rows = a.mode == kGated ? 2 * a.N : a.N;
+    p.x = static_cast<const char*>(a.x); p.xs = a.xs;
+    p.w = static_cast<const char*>(a.w); p.ws = a.ws;
+    p.offsets = a.by_expert ? a.offsets : nullptr; p.experts = (int)a.experts;
+    p.expert = w_rows * a.K; p.expert_scales = (w_rows + 127) / 128 * (a.K / 128);
+    p.M = (int)a.M; p.N = (int)a.N; p.K = (int)a.K; p.KT = (int)(a.K / 128); p.NB = (int)(a.N / 16);
+    p.bf16 = a.dtype == LUTQ_BF16; p.act = a.act;
+    p.counters = static_cast<uint32_t*>(a.workspace);
+    p.partial = static_cast<char*>(a.workspace) + kCounterBytes;
+    char* const codes = p.partial + kPartialBytes;
+    float* const scales = reinterpret_cast<float*>(codes + up256((size_t)a.M * a.K));
+    char* const dense = reinterpret_cast<char*>(scales) + up256((size_t)a.M * (a.K / 128) * 4);
+    p.y = a.y ? static_cast<char*>(a.y) : dense; p.saved = static_cast<char*>(a.saved);
+    const int src = a.xs ? kF32 : a.dtype == LUTQ_F16 ? kF16 : kBF16;
+    const int cus = compute_units();
+    if (cus < 1) return LUTQ_ERR_DEVICE;
+    const Choice c = choose(a.M, w_rows / 16, p.KT, p.offsets ? a.experts : 0, a.mode, a.xs != nullptr, cus);
+    if (c.apart) {
+        const lutq_status st = quantize_rows_on(a.x, src, a.M, nullptr, nullptr, 0, a.M, a.K, codes, scales, s);
+        if (st != LUTQ_OK) return st;
+        p.x = codes; p.xs = scales;
+    }
+    p.once = c.once;
+    p.slices = c.tiles.slices;
+    const hipError_t e = a.mode == kGated ? launch_of<kGated>(c, src, p, cus, s) : a.mode == kPowers ? launch_of<kPowers>(c, src, p, cus, s)
+                                                                                                   : launch_of<kPlain>(c, src, p, cus, s);
+    if (e != hipSuccess) return LUTQ_ERR_DEVICE;
+    if (!a.h_codes) return LUTQ_OK;
+    return quantize_rows_on(p.y, a.dtype == LUTQ_F16 ? kF16 : kBF16, a.M, nullptr, p.offsets, a.experts, a.M, a.N, a.h_codes, a.h_scales, s);
+}
+
+bool experts_ok(int64_t experts) { return experts >= 1 && experts <= 65536; }
+
+}  // namespace
+
+}  // namespace fp8
+}  // namespace lutq
+
+using namespace lutq::fp8;
+
+extern "C" size_t lutq_fp8_workspace_bytes(int64_t M, int64_t N, int64_t K, int64_t experts) {
+    if (!shape_ok(N, K) || !rows_ok(M, K) || !experts_ok(experts)) return 0;
+    return scratch_bytes(M, K);
+}
+
+extern "C" size_t lutq_fp8_gated_workspace_bytes(int64_t M, int64_t F, int64_t K, int64_t experts) {
+    if (F < 1 || F % 128 != 0 || F > kMostColumns / 2 || !shape_ok(2 * F, K) || !rows_ok(M, K) || !rows_ok(M, 2 * F) || !experts_ok(experts)) return 0;
+    return scratch_bytes(M, K) + lutq::product::up256((size_t)M * (size_t)F * 2);
+}
+
+extern "C" lutq_status lutq_fp8_matmul(const void* X, const float* x_scales, const void* W, const float* w_scales, int64_t M, int64_t N, int64_t K,
+                                       lutq_dtype dtype, void* Y, void* workspace, size_t workspace_bytes, void* stream) {
+    return product_on({X, x_scales, W, w_scales, nullptr, 1, M, N, K, dtype, Y, nullptr, nullptr, nullptr, kPlain, 0, workspace, workspace_bytes,
+                       lutq_fp8_workspace_bytes(M, N, K, 1), false}, static_cast<hipStream_t>(stream));
+}
+
+extern "C" lutq_status lutq_fp8_matmul_grouped(const void* X, const float* x_scales, const void* W, const float* w_scales, const int32_t* offsets,
+                                               int64_t experts, int64_t M, int64_t N, int64_t K, lutq_dtype dtype, void* Y, void* workspace,
+                                               size_t workspace_bytes, void* stream) {
+    return product_on({X, x_scales, W, w_scales, offsets, experts, M, N, K, dtype, Y, nullptr, nullptr, nullptr, kPlain, 0, workspace, workspace_bytes,
+                       lutq_fp8_workspace_bytes(M, N, K, experts), true}, static_cast<hipStream_t>(stream));
+}
+
+extern "C" lutq_status lutq_fp8_gated(const void* X, const float* x_scales, const void* W, const float* w_scales, int64_t M, int64_t F, int64_t K,
+                                      lutq_activation activation, lutq_dtype dtype, void* H, void* h_codes, float* h_scales, void* saved,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+    return product_on({X, x_scales, W, w_scales, nullptr, 1, M, F, K, dtype, H, saved, h_codes, h_scales, kGated, activation, workspace, workspace_bytes,
+                       lutq_fp8_gated_workspace_bytes(M, F, K, 1), false}, static_cast<hipStream_t>(stream));
+}
+
+extern "C" lutq_status lutq_fp8_gated_grouped(const void* X, const float* x_scales, const void* W, const float* w_scales, const int32_t* offsets,
+                                              int64_t experts, int64_t M, int64_t F, int64_t K, lutq_activation activation, lutq_dtype dtype, void* H,
+                                              void* h_codes, float* h_scales, void* saved, void* workspace, size_t workspace_bytes, void* stream) {
+    return product_on({X, x_scales, W, w_scales, offsets, experts, M, F, K, dtype, H, saved, h_codes, h_scales, kGated, activation, workspace,
+                       workspace_bytes, lutq_fp8_gated_workspace_bytes(M, F, K, experts), true}, static_cast<hipStream_t>(stream));
+}
+
+extern "C" lutq_status lutq_fp8_weight_grad(const void* dY, const float* dy_scales, const void* X, const float* x_scales, int64_t N, int64_t K, int64_t M,
+                                            lutq_dtype dtype, void* dW, void* workspace, size_t workspace_bytes, void* stream) {
+    if (M < 1 || M % 128 != 0 || N < 1 || N % 16 != 0) return LUTQ_ERR_SHAPE;
+    if (!dy_scales) return LUTQ_ERR_NULL;
+    return product_on({dY, dy_scales, X, x_scales, nullptr, 1, N, K, M, dtype, dW, nullptr, nullptr, nullptr, kPowers, 0, workspace, workspace_bytes,
+                       lutq_fp8_workspace_bytes(N, K, M, 1), false}, static_cast<hipStream_t>(stream));
+}
+
+extern "C" int lutq_calib_fp8_launch(int64_t M, int64_t N, int64_t K, int64_t experts, int form, int x_is_codes, int compute_units, int* launch) {
+    if (!launch) return LUTQ_ERR_NULL;
+    if (form < 0 || form > 2 || experts < 0 || M < 1 || compute_units < 1 || compute_units > 4096 || (form == kPowers && (experts || !x_is_codes)) ||
+        (form == kGated ? lutq_fp8_gated_workspace_bytes(M, N, K, experts ? experts : 1) : lutq_fp8_workspace_bytes(M, N, K, experts ? experts : 1)) == 0)
+        return LUTQ_ERR_SHAPE;
+    const Choice c = choose(M, N / 16 * (form == kGated ? 2 : 1), K / 128, experts, form, x_is_codes != 0, compute_units);
+    const bool streamed = c.tiles.shape < 0;
+    const TileSize t = streamed ? TileSize{16 * c.wide, 16, c.waves, 0} : kTiles[c.tiles.shape];
+    const int out[8] = {c.apart, t.channels, t.rows, t.waves, t.room, c.tiles.slices, streamed ? c.rows : 0, c.once};
+    for (int i = 0; i < 8; ++i) launch[i] = out[i];
+    return LUTQ_OK;
+}

@@ -42,6 +42,19 @@ inline bool rows_ok(int64_t M, int64_t K) {
 
 }  // namespace mx4
 
+// The 8-bit form (include/lutq.h).
+namespace fp8 {
+
+constexpr int64_t kMostColumns = int64_t(1) << 22;     // (256 rows of codes are 1 GiB at most: offsets inside a tile fit 32 bits)
+inline bool shape_ok(int64_t N, int64_t K) {
+    return N > 0 && K > 0 && N <= (1 << 24) && K <= kMostColumns && N % 16 == 0 && K % 128 == 0;
+}
+inline bool rows_ok(int64_t M, int64_t K) {
+    return M >= 0 && K > 0 && K <= kMostColumns && K % 128 == 0 && M < (int64_t(1) << 30) && M * (K / 128) < (int64_t(1) << 30);
+}
+
+}  // namespace fp8
+
 // Compute units of the current device, 0 if it cannot be asked (lutq_api.hip).
 int compute_units();
 
