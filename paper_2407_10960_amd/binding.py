@@ -180,6 +180,7 @@ def load_library():
 class _NoNative:
     """In place of the native part where it cannot be loaded: takes no call."""
     mm = quantize = dequant = mx4_quantize = mx4_dequant = mx4_mm = staticmethod(lambda *args: -1)
+    fp8_quantize = fp8_dequant = fp8_mm = fp8_grad = fp8_weight_grad = staticmethod(lambda *args: -1)
 
 
 def _native():
@@ -198,7 +199,9 @@ def _native():
                       ("lutq_packed_bytes", "lutq_matmul", "lutq_matmul_static", "lutq_matmul_channel", "lutq_matmul_pairs",
                        "lutq_matmul_quads", "lutq_quantize", "lutq_dequant", "lutq_mx4_packed_bytes", "lutq_mx4_quantize",
                        "lutq_mx4_quantize_packed", "lutq_mx4_dequant", "lutq_mx4_dequant_packed", "lutq_mx4_matmul",
-                       "lutq_mx4_matmul_grouped")))
+                       "lutq_mx4_matmul_grouped", "lutq_fp8_quantize", "lutq_fp8_quantize_weights", "lutq_fp8_quantize_columns",
+                       "lutq_fp8_dequant", "lutq_fp8_dequant_weights", "lutq_fp8_matmul", "lutq_fp8_matmul_grouped", "lutq_fp8_gated",
+                       "lutq_fp8_gated_grouped", "lutq_fp8_gated_grad", "lutq_fp8_weight_grad")))
     except ImportError as e:
         warnings.warn(f"calls take about 6 us more host time each: the binding's native part is not loaded ({e}); "
                       "`python -m paper_2407_10960_amd.build` builds it", RuntimeWarning, stacklevel=3)
@@ -829,6 +832,8 @@ def lutq_fp8_quantize(X, codes_out, scales_out, rows=None, stream=None):
     """Quantises X [., K] (float32, float16, bfloat16) to codes [M, K] (uint8 or float8_e4m3fn) and scales [K / 128, M] (float32).
     With rows (int32, [M], on the device) output row m is row rows[m] of X, zeros where that is no row of X."""
     name = "lutq_fp8_quantize"
+    if stream is None and _done(_native().fp8_quantize(0, X, codes_out, scales_out, rows, None, None), name):
+        return codes_out, scales_out
     device, on = _mx4_tensors(name, stream, X, codes_out, scales_out, rows)
     _fp8_codes(name, codes_out)
     _fp8_scales(name, scales_out)
@@ -849,6 +854,8 @@ def lutq_fp8_quantize_weights(W, codes_out, scales_out, transposed=None, stream=
     128 x 128.  transposed=(codes [K, N], scales [K / 128, ceil(N / 128)]) takes those of W transposed as well."""
     name = "lutq_fp8_quantize_weights"
     t_codes, t_scales = transposed if transposed is not None else (None, None)
+    if stream is None and _done(_native().fp8_quantize(1, W, codes_out, scales_out, None, t_codes, t_scales), name):
+        return codes_out, scales_out
     device, on = _mx4_tensors(name, stream, W, codes_out, scales_out, t_codes, t_scales)
     _fp8_codes(name, codes_out, t_codes)
     _fp8_scales(name, scales_out, t_scales)
@@ -869,6 +876,8 @@ def lutq_fp8_quantize_columns(X, codes_out, scales_out, stream=None):
     """Quantises X [M, K] (float32, float16, bfloat16) by columns: codes [K, M'], M' the next multiple of 128 from M on, and scales
     [M' / 128, K], powers of two: a factor of lutq_fp8_weight_grad."""
     name = "lutq_fp8_quantize_columns"
+    if stream is None and _done(_native().fp8_quantize(2, X, codes_out, scales_out, None, None, None), name):
+        return codes_out, scales_out
     device, on = _mx4_tensors(name, stream, X, codes_out, scales_out)
     _fp8_codes(name, codes_out)
     _fp8_scales(name, scales_out)
@@ -881,7 +890,9 @@ def lutq_fp8_quantize_columns(X, codes_out, scales_out, stream=None):
     return codes_out, scales_out
 
 
-def _fp8_dequantise(name, codes, scales, out, scales_shape, stream):
+def _fp8_dequantise(name, kind, codes, scales, out, scales_shape, stream):
+    if stream is None and _done(_native().fp8_dequant(kind, codes, scales, out), name):
+        return out
     device, on = _mx4_tensors(name, stream, codes, scales, out)
     _fp8_codes(name, codes)
     _fp8_scales(name, scales)
@@ -896,18 +907,21 @@ def _fp8_dequantise(name, codes, scales, out, scales_shape, stream):
 
 def lutq_fp8_dequant(codes, scales, X_out, stream=None):
     """X_out [M, K] (float16 or bfloat16) = the values that codes [M, K] and scales [K / 128, M] stand for."""
-    return _fp8_dequantise("lutq_fp8_dequant", codes, scales, X_out, lambda M, K: (K // 128, M), stream)
+    return _fp8_dequantise("lutq_fp8_dequant", 0, codes, scales, X_out, lambda M, K: (K // 128, M), stream)
 
 
 def lutq_fp8_dequant_weights(codes, scales, W_out, stream=None):
     """W_out [N, K] (float16 or bfloat16) = the values that codes [N, K] and scales [ceil(N / 128), K / 128] stand for."""
-    return _fp8_dequantise("lutq_fp8_dequant_weights", codes, scales, W_out, lambda N, K: (_up128(N), K // 128), stream)
+    return _fp8_dequantise("lutq_fp8_dequant_weights", 1, codes, scales, W_out, lambda N, K: (_up128(N), K // 128), stream)
 
 
 def _fp8_product(name, X, x_scales, W, w_scales, offsets, Y, workspace, stream, gated=None):
     """gated: None, or (activation, H's dtype, codes and scales of H or None, saved or None); Y may be None then."""
-    act, dtype, h_codes, h_scales, saved = gated if gated else (None, Y.dtype, None, None, None)
     torch = _torch()
+    act, dtype, h_codes, h_scales, saved = gated if gated else (-1, Y.dtype, None, None, None)
+    if stream is None and _done(_native().fp8_mm(X, x_scales, W, w_scales, offsets, act, {torch.float16: 0, torch.bfloat16: 1}.get(dtype, -1), Y, h_codes, h_scales, saved,
+                                                 workspace), name):
+        return Y if Y is not None else h_codes
     device, on = _mx4_tensors(name, stream, X, x_scales, W, w_scales, offsets, Y, h_codes, h_scales, saved, workspace)
     _fp8_codes(name, W, h_codes, *(() if x_scales is None else (X,)))
     _fp8_scales(name, x_scales, w_scales, h_scales)
@@ -998,6 +1012,8 @@ def lutq_fp8_gated_grad(dH, saved, activation="silu", dense=None, rows=None, col
     name = "lutq_fp8_gated_grad"
     act = _fp8_activation(name, activation)
     (r_codes, r_scales), (c_codes, c_scales) = (None, None) if rows is None else rows, (None, None) if columns is None else columns
+    if stream is None and _done(_native().fp8_grad(dH, saved, act, dense, r_codes, r_scales, c_codes, c_scales), name):
+        return
     device, on = _mx4_tensors(name, stream, dH, saved, dense, r_codes, r_scales, c_codes, c_scales)
     _fp8_codes(name, r_codes, c_codes)
     _fp8_scales(name, r_scales, c_scales)
@@ -1019,6 +1035,8 @@ def lutq_fp8_weight_grad(dY, dy_scales, X, x_scales, dW, workspace, stream=None)
     """dW [N, K] (float16 or bfloat16) = the sum over rows of dY times X, both by columns: codes [N, M'] with scales [M' / 128, N], codes
     [K, M'] with scales [M' / 128, K].  workspace: new_fp8_workspace(N, K, M')."""
     name = "lutq_fp8_weight_grad"
+    if stream is None and _done(_native().fp8_weight_grad(dY, dy_scales, X, x_scales, dW, workspace), name):
+        return dW
     device, on = _mx4_tensors(name, stream, dY, dy_scales, X, x_scales, dW, workspace)
     _fp8_codes(name, dY, X)
     _fp8_scales(name, dy_scales, x_scales)

@@ -32,12 +32,24 @@ decltype(&lutq_mx4_dequant) mx4_dequant = nullptr;
 decltype(&lutq_mx4_dequant_packed) mx4_dequant_packed = nullptr;
 decltype(&lutq_mx4_matmul) mx4_matmul = nullptr;
 decltype(&lutq_mx4_matmul_grouped) mx4_matmul_grouped = nullptr;
+decltype(&lutq_fp8_quantize) fp8_quantize = nullptr;
+decltype(&lutq_fp8_quantize_weights) fp8_quantize_weights = nullptr;
+decltype(&lutq_fp8_quantize_columns) fp8_quantize_columns = nullptr;
+decltype(&lutq_fp8_dequant) fp8_dequant = nullptr;
+decltype(&lutq_fp8_dequant_weights) fp8_dequant_weights = nullptr;
+decltype(&lutq_fp8_matmul) fp8_matmul = nullptr;
+decltype(&lutq_fp8_matmul_grouped) fp8_matmul_grouped = nullptr;
+decltype(&lutq_fp8_gated) fp8_gated = nullptr;
+decltype(&lutq_fp8_gated_grouped) fp8_gated_grouped = nullptr;
+decltype(&lutq_fp8_gated_grad) fp8_gated_grad = nullptr;
+decltype(&lutq_fp8_weight_grad) fp8_weight_grad = nullptr;
 
 // the functions of liblutq.so by address, in the order of the declarations above
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    void* p[15];
-    if (n != 15) { PyErr_SetString(PyExc_TypeError, "fifteen addresses"); return nullptr; }
-    for (int i = 0; i < 15; ++i) {
+    constexpr Py_ssize_t kCount = 26;
+    void* p[kCount];
+    if (n != kCount) { PyErr_SetString(PyExc_TypeError, "twenty-six addresses"); return nullptr; }
+    for (int i = 0; i < kCount; ++i) {
         p[i] = PyLong_AsVoidPtr(args[i]);
         if (!p[i]) { if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address"); return nullptr; }
     }
@@ -56,6 +68,17 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     mx4_dequant_packed = reinterpret_cast<decltype(mx4_dequant_packed)>(p[12]);
     mx4_matmul = reinterpret_cast<decltype(mx4_matmul)>(p[13]);
     mx4_matmul_grouped = reinterpret_cast<decltype(mx4_matmul_grouped)>(p[14]);
+    fp8_quantize = reinterpret_cast<decltype(fp8_quantize)>(p[15]);
+    fp8_quantize_weights = reinterpret_cast<decltype(fp8_quantize_weights)>(p[16]);
+    fp8_quantize_columns = reinterpret_cast<decltype(fp8_quantize_columns)>(p[17]);
+    fp8_dequant = reinterpret_cast<decltype(fp8_dequant)>(p[18]);
+    fp8_dequant_weights = reinterpret_cast<decltype(fp8_dequant_weights)>(p[19]);
+    fp8_matmul = reinterpret_cast<decltype(fp8_matmul)>(p[20]);
+    fp8_matmul_grouped = reinterpret_cast<decltype(fp8_matmul_grouped)>(p[21]);
+    fp8_gated = reinterpret_cast<decltype(fp8_gated)>(p[22]);
+    fp8_gated_grouped = reinterpret_cast<decltype(fp8_gated_grouped)>(p[23]);
+    fp8_gated_grad = reinterpret_cast<decltype(fp8_gated_grad)>(p[24]);
+    fp8_weight_grad = reinterpret_cast<decltype(fp8_weight_grad)>(p[25]);
     Py_RETURN_NONE;
 }
 
@@ -271,6 +294,154 @@ PyObject* mx4_mm(PyObject*, PyObject* const* args, Py_ssize_t n) { return answer
     return PyLong_FromLong((long)st);
 }); }
 
+// ---- 8-bit floating point, blocks of 128
+bool is_codes(const at::Tensor* t) { return !t || t->scalar_type() == at::kByte || t->scalar_type() == at::kFloat8_e4m3fn; }
+bool is_scales(const at::Tensor* t) { return !t || t->scalar_type() == at::kFloat; }
+bool fits(const at::Tensor* t, int64_t a, int64_t b) { return !t || shape_is(*t, a, b); }
+int64_t up128(int64_t n) { return (n + 127) / 128; }
+void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+float* floats(const at::Tensor* t) { return static_cast<float*>(data(t)); }
+
+enum QuantiseKind { kRows = 0, kWeights = 1, kColumns = 2 };
+
+// (kind, X, codes, scales, rows or None, transposed codes or None, transposed scales or None) -> status, or -1
+PyObject* fp8_quant(PyObject*, PyObject* const* args, Py_ssize_t n) { return answer([&]() -> PyObject* {
+    int kind;
+    if (!fp8_quantize || n != 7 || !small_int(args[0], 0, 2, &kind)) return PyLong_FromLong(-1);
+    const at::Tensor *X = plain(args[1]), *codes = plain(args[2]), *scales = plain(args[3]), *rows = nullptr, *t = nullptr, *ts = nullptr;
+    if (!X || !codes || !scales || !plain_or_none(args[4], &rows) || !plain_or_none(args[5], &t) || !plain_or_none(args[6], &ts) || X->dim() != 2 ||
+        !on_current_device(X, codes, scales, rows, t, ts) || !is_codes(codes) || !is_codes(t) || !is_scales(scales) || !is_scales(ts) || !is_numbers(rows) || !t != !ts)
+        return PyLong_FromLong(-1);
+    const bool f32 = X->scalar_type() == at::kFloat;
+    const int code = f32 ? LUTQ_F16 : dtype_code(*X);
+    const int64_t from = X->size(0), K = X->size(1), M = rows ? rows->size(0) : from;
+    if (code < 0 || (kind == kRows      ? !shape_is(*codes, M, K) || !shape_is(*scales, K / 128, M)
+                     : kind == kWeights ? !shape_is(*codes, M, K) || !shape_is(*scales, up128(M), K / 128) || !fits(t, K, M) || !fits(ts, K / 128, up128(M))
+                                        : !shape_is(*codes, K, 128 * up128(M)) || !shape_is(*scales, up128(M), K)))
+        return PyLong_FromLong(-1);
+    const void *x = data(X), *r = data(rows);
+    void *c = data(codes), *tc = data(t), *stream = current_stream();
+    float *s = floats(scales), *tcs = floats(ts);
+    const lutq_dtype dt = (lutq_dtype)code;
+    lutq_status st;
+    {
+        WithoutGil released;
+        st = kind == kRows      ? fp8_quantize(x, f32, dt, from, static_cast<const int32_t*>(r), M, K, c, s, stream)
+             : kind == kWeights ? fp8_quantize_weights(x, f32, dt, M, K, c, s, tc, tcs, stream)
+                                : fp8_quantize_columns(x, f32, dt, M, K, c, s, stream);
+    }
+    return PyLong_FromLong((long)st);
+}); }
+
+// (kind, codes, scales, out) -> status, or -1
+PyObject* fp8_dequantise(PyObject*, PyObject* const* args, Py_ssize_t n) { return answer([&]() -> PyObject* {
+    int kind;
+    if (!fp8_dequant || n != 4 || !small_int(args[0], 0, 1, &kind)) return PyLong_FromLong(-1);
+    const at::Tensor *codes = plain(args[1]), *scales = plain(args[2]), *out = plain(args[3]);
+    if (!codes || !scales || !out || out->dim() != 2 || !on_current_device(codes, scales, out) || !is_codes(codes) || !is_scales(scales)) return PyLong_FromLong(-1);
+    const int code = dtype_code(*out);
+    const int64_t M = out->size(0), K = out->size(1);
+    if (code < 0 || !shape_is(*codes, M, K) || !(kind == kRows ? shape_is(*scales, K / 128, M) : shape_is(*scales, up128(M), K / 128))) return PyLong_FromLong(-1);
+    const void* c = data(codes);
+    const float* s = floats(scales);
+    void *w = data(out), *stream = current_stream();
+    lutq_status st;
+    {
+        WithoutGil released;
+        st = (kind == kRows ? fp8_dequant : fp8_dequant_weights)(c, s, M, K, (lutq_dtype)code, w, stream);
+    }
+    return PyLong_FromLong((long)st);
+}); }
+
+bool is_weights(const at::Tensor& W, const at::Tensor& ws, int64_t experts, int64_t N, int64_t K) {
+    if (experts < 0) return shape_is(W, N, K) && shape_is(ws, up128(N), K / 128);
+    return W.dim() == 3 && ws.dim() == 3 && W.size(0) == experts && W.size(1) == N && W.size(2) == K && ws.size(0) == experts && ws.size(1) == up128(N) && ws.size(2) == K / 128;
+}
+
+// (X, scales or None, W, scales, offsets or None, activation or -1 for the plain product, 0 or 1 for H's dtype, Y or None, codes of H or None, their
+// scales or None, saved or None, workspace) -> status, or -1
+PyObject* fp8_mm(PyObject*, PyObject* const* args, Py_ssize_t n) { return answer([&]() -> PyObject* {
+    int act, code;
+    if (!fp8_matmul || n != 12 || !small_int(args[5], -1, 1, &act) || !small_int(args[6], 0, 1, &code)) return PyLong_FromLong(-1);
+    const at::Tensor *X = plain(args[0]), *xs = nullptr, *W = plain(args[2]), *ws = plain(args[3]), *offsets = nullptr, *Y = nullptr, *hc = nullptr,
+                     *hs = nullptr, *saved = nullptr, *work = plain(args[11]);
+    if (!X || !plain_or_none(args[1], &xs) || !W || !ws || !plain_or_none(args[4], &offsets) || !plain_or_none(args[7], &Y) || !plain_or_none(args[8], &hc) ||
+        !plain_or_none(args[9], &hs) || !plain_or_none(args[10], &saved) || !work || (!Y && !hc) || !hc != !hs || X->dim() != 2 ||
+        !on_current_device(X, xs, W, ws, offsets, Y, hc, hs, saved, work))
+        return PyLong_FromLong(-1);
+    const at::Tensor& out = Y ? *Y : *hc;
+    if (out.dim() != 2 || (xs && !is_codes(X)) || (!xs && dtype_code(*X) != code) || !is_codes(W) || !is_codes(hc) || !is_scales(xs) || !is_scales(ws) || !is_scales(hs) ||
+        !is_bytes(work) || !is_numbers(offsets) || (Y && dtype_code(*Y) != code) || (saved && dtype_code(*saved) != code))
+        return PyLong_FromLong(-1);
+    const int64_t M = out.size(0), N = out.size(1), K = X->size(1), rows = act < 0 ? N : 2 * N, experts = offsets ? offsets->size(0) - 1 : -1;
+    if ((act < 0 && (hc || saved)) || (offsets && experts < 1) || X->size(0) != M || !fits(xs, K / 128, M) || !is_weights(*W, *ws, experts, rows, K) ||
+        !fits(hc, M, N) || !fits(hs, N / 128, M) || !fits(saved, M, 2 * N))
+        return PyLong_FromLong(-1);
+    const void *x = data(X), *w = data(W);
+    const float *xf = floats(xs), *wf = floats(ws);
+    const int32_t* at = static_cast<const int32_t*>(data(offsets));
+    void *y = data(Y), *h = data(hc), *sv = data(saved), *scratch = data(work), *stream = current_stream();
+    float* hf = floats(hs);
+    const size_t bytes = (size_t)work->numel();
+    const lutq_dtype dt = (lutq_dtype)code;
+    lutq_status st;
+    {
+        WithoutGil released;
+        st = act < 0 ? (at ? fp8_matmul_grouped(x, xf, w, wf, at, experts, M, N, K, dt, y, scratch, bytes, stream)
+                           : fp8_matmul(x, xf, w, wf, M, N, K, dt, y, scratch, bytes, stream))
+                     : (at ? fp8_gated_grouped(x, xf, w, wf, at, experts, M, N, K, (lutq_activation)act, dt, y, h, hf, sv, scratch, bytes, stream)
+                           : fp8_gated(x, xf, w, wf, M, N, K, (lutq_activation)act, dt, y, h, hf, sv, scratch, bytes, stream));
+    }
+    return PyLong_FromLong((long)st);
+}); }
+
+// (dH, saved, activation, dense or None, row codes or None, their scales or None, column codes or None, their scales or None) -> status, or -1
+PyObject* fp8_grad(PyObject*, PyObject* const* args, Py_ssize_t n) { return answer([&]() -> PyObject* {
+    int act;
+    if (!fp8_gated_grad || n != 8 || !small_int(args[2], 0, 1, &act)) return PyLong_FromLong(-1);
+    const at::Tensor *dh = plain(args[0]), *saved = plain(args[1]), *dense = nullptr, *rc = nullptr, *rs = nullptr, *cc = nullptr, *cs = nullptr;
+    if (!dh || !saved || !plain_or_none(args[3], &dense) || !plain_or_none(args[4], &rc) || !plain_or_none(args[5], &rs) || !plain_or_none(args[6], &cc) ||
+        !plain_or_none(args[7], &cs) || dh->dim() != 2 || !on_current_device(dh, saved, dense, rc, rs, cc, cs))
+        return PyLong_FromLong(-1);
+    const int code = dtype_code(*dh);
+    const int64_t M = dh->size(0), F = dh->size(1);
+    if (code < 0 || dtype_code(*saved) != code || (dense && dtype_code(*dense) != code) || !is_codes(rc) || !is_codes(cc) || !is_scales(rs) || !is_scales(cs) ||
+        (!dense && !rc && !cc) || !rc != !rs || !cc != !cs || !shape_is(*saved, M, 2 * F) || !fits(dense, M, 2 * F) || !fits(rc, M, 2 * F) || !fits(rs, 2 * F / 128, M) ||
+        !fits(cc, 2 * F, 128 * up128(M)) || !fits(cs, up128(M), 2 * F))
+        return PyLong_FromLong(-1);
+    const void *d = data(dh), *s = data(saved);
+    void *out = data(dense), *r = data(rc), *c = data(cc), *stream = current_stream();
+    float *rf = floats(rs), *cf = floats(cs);
+    lutq_status st;
+    {
+        WithoutGil released;
+        st = fp8_gated_grad(d, s, M, F, (lutq_activation)act, (lutq_dtype)code, out, r, rf, c, cf, stream);
+    }
+    return PyLong_FromLong((long)st);
+}); }
+
+// (dY, scales, X, scales, dW, workspace) -> status, or -1
+PyObject* fp8_wgrad(PyObject*, PyObject* const* args, Py_ssize_t n) { return answer([&]() -> PyObject* {
+    if (!fp8_weight_grad || n != 6) return PyLong_FromLong(-1);
+    const at::Tensor *dy = plain(args[0]), *ds = plain(args[1]), *X = plain(args[2]), *xs = plain(args[3]), *dw = plain(args[4]), *work = plain(args[5]);
+    if (!dy || !ds || !X || !xs || !dw || !work || dy->dim() != 2 || dw->dim() != 2 || !on_current_device(dy, ds, X, xs, dw, work) || !is_codes(dy) || !is_codes(X) ||
+        !is_scales(ds) || !is_scales(xs) || !is_bytes(work))
+        return PyLong_FromLong(-1);
+    const int code = dtype_code(*dw);
+    const int64_t N = dw->size(0), K = dw->size(1), M = dy->size(1);
+    if (code < 0 || !shape_is(*dy, N, M) || !shape_is(*ds, M / 128, N) || !shape_is(*X, K, M) || !shape_is(*xs, M / 128, K)) return PyLong_FromLong(-1);
+    const void *d = data(dy), *x = data(X);
+    const float *df = floats(ds), *xf = floats(xs);
+    void *w = data(dw), *scratch = data(work), *stream = current_stream();
+    const size_t bytes = (size_t)work->numel();
+    lutq_status st;
+    {
+        WithoutGil released;
+        st = fp8_weight_grad(d, df, x, xf, N, K, M, (lutq_dtype)code, w, scratch, bytes, stream);
+    }
+    return PyLong_FromLong((long)st);
+}); }
+
 PyMethodDef methods[] = {
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
     {"mm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mm)), METH_FASTCALL, nullptr},
@@ -279,6 +450,11 @@ PyMethodDef methods[] = {
     {"mx4_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx4_quant)), METH_FASTCALL, nullptr},
     {"mx4_dequant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx4_dequantise)), METH_FASTCALL, nullptr},
     {"mx4_mm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(mx4_mm)), METH_FASTCALL, nullptr},
+    {"fp8_quantize", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp8_quant)), METH_FASTCALL, nullptr},
+    {"fp8_dequant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp8_dequantise)), METH_FASTCALL, nullptr},
+    {"fp8_mm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp8_mm)), METH_FASTCALL, nullptr},
+    {"fp8_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp8_grad)), METH_FASTCALL, nullptr},
+    {"fp8_weight_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(fp8_wgrad)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_lutq_torch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

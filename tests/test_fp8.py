@@ -222,6 +222,10 @@ def test_binding_refuses_host_tensors(lutq):
         lutq.lutq_fp8_gated(x, u, s, x, u, activation="relu")
     with pytest.raises(TypeError, match="offsets"):
         lutq.lutq_fp8_gated_grouped(x, u, s, None, x, u)
+    nat = lutq.binding._native()
+    assert nat.fp8_quantize(0, x, u, s, None, None, None) == nat.fp8_quantize(x) == nat.fp8_dequant(0, u, s, x) == nat.fp8_grad(x, x, 0, x, None, None, None, None) == -1
+    assert nat.fp8_mm(u, s, u, s, None, -1, 0, x, None, None, None, u) == nat.fp8_mm(u, s, u, s, "o", 2, 0, x, None, None, None, u) == -1
+    assert nat.fp8_weight_grad(u, s, u, s, x, u) == -1
 
 
 # ---------------------------------------------------------------------------------------------------- device: quantisers
