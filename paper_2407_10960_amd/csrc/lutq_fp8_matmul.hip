@@ -434,11 +434,14 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             for (int b = 0; b < WM; ++b) {
                 if constexpr (MODE == kPowers) {
                     acc[r][b] = scaled_product(w[r % kRing], x[b], acc[r][b], we[r % kRing], xe[b]);
+                    asm volatile("" : "+v"(acc[r][b])::"memory");
                 } else {
-                    const f32x4 sums = product(w[r % kRing], x[b], f32x4{0.f, 0.f, 0.f, 0.f});
+                    f32x4 sums = product(w[r % kRing], x[b], f32x4{0.f, 0.f, 0.f, 0.f});
+                    asm volatile("" : "+v"(sums)::"memory");
                     f32x4& last = b ? acc[r][b - 1] : r ? acc[r - 1][WM - 1] : acc[WN - 1][WM - 1];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) last[j] = __builtin_fmaf(pending[j], pending_scale, last[j]);
+                    asm volatile("" : "+v"(last)::"memory");
                     pending = sums;
                     pending_scale = s[MODE == kGated && r >= WN / 2][b];
                 }
