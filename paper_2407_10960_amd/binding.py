@@ -1115,10 +1115,10 @@ TRACE_STAMPS = ("start", "arguments arrived", "first loads issued", "table built
 
 
 def calib_fp8_launch(M: int, N: int, K: int, experts: int = 0, form: str = "matmul", codes: bool = False, compute_units: int = 256) -> Mx4Launch:
-    """How the library launches lutq_fp8_matmul (form "matmul"), lutq_fp8_gated ("gated", N is F; with experts the ones by expert), or
+    """How the library launches lutq_fp8_matmul (form "matmul"), lutq_fp8_gated ("gated", N is F, "gated_saved"; with experts the ones by expert), or
     lutq_fp8_weight_grad ("weight_grad"; its N, K, M as M, N, K)."""
     out = (ctypes.c_int * 8)()
-    _check(load_library().lutq_calib_fp8_launch(M, N, K, experts, ("matmul", "gated", "weight_grad").index(form), int(codes), compute_units, out),
+    _check(load_library().lutq_calib_fp8_launch(M, N, K, experts, ("matmul", "gated", "weight_grad", "gated_saved").index(form), int(codes), compute_units, out),
            "lutq_calib_fp8_launch")
     return Mx4Launch(bool(out[0]), *out[1:7], bool(out[7]))
 

@@ -98,6 +98,30 @@ __device__ __forceinline__ f32x4 product(const i32x8& w, const i32x8& x, const f
 __device__ __forceinline__ f32x4 scaled_product(const i32x8& w, const i32x8& x, const f32x4& acc, uint32_t we, uint32_t xe) {
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, acc, 0, 0, 0, (int)we, 0, (int)xe);
 }
+// It adds eight neighbours' products (of a lane's columns) in fewer bits than fp32 has: what lies below 2^-13 of the power of two of the largest
+// is cut off, 2^-18 of the sum of magnitudes on random codes.  The 16-bit instruction does not (2^-30), at half the rate: the same sums of
+// the codes as 16-bit numbers, which hold them exactly.
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+struct Wide { f16x8 v[4]; };
+__device__ __forceinline__ Wide widen(const i32x8& c) {
+    Wide r;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        f16x2 h[4];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            h[2 * j] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)c[2 * q + j], 1.0f, false);
+            h[2 * j + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)c[2 * q + j], 1.0f, true);
+        }
+        r.v[q] = f16x8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
+    }
+    return r;
+}
+__device__ __forceinline__ f32x4 product(const Wide& w, const Wide& x, f32x4 acc) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[q], x.v[q], acc, 0, 0, 0);
+    return acc;
+}
 __device__ __forceinline__ i32x8 operand(u32x4 a, u32x4 b) {
     return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b[0], (int)b[1], (int)b[2], (int)b[3]};
 }

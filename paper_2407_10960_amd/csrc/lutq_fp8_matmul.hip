@@ -57,22 +57,46 @@ __device__ __forceinline__ f32x4 gated(const f32x4& g, const f32x4& u, int act) 
     return h;
 }
 
+// Where something in LDS lies, as its instructions take it.
+__device__ __forceinline__ uint32_t lds_offset(const void* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void*)p;
+}
+
+// Quotient of a lane's numbers.
+__device__ __forceinline__ int quotient_of_lane(int a, int b) { return b == 1 ? a : (int)((uint32_t)a / (uint32_t)b); }
+
 // Four neighbouring sums of a row, as 16-bit values.
 __device__ __forceinline__ void store_four(char* to, const f32x4& sum, int bf16) {
     *reinterpret_cast<u32x2*>(to) = u32x2{round_pair(sum[0], sum[1], bf16), round_pair(sum[2], sum[3], bf16)};
 }
 
-// Few rows: a workgroup owns R row blocks of weights (kGated: one of each projection) and sixteen rows of X over all of K; its wavefronts take
-// the quads (four blocks of 128 columns) in turn, and their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the
-// weights, which go from memory into the operand registers as they lie, all of a quad asked for at once.
-// 16-bit values (SRC 1, 2) are quantised on the way, ROWS at a time, by the sixteen lanes that hold a block, and the codes pass through a place of
-// the wavefront's own in LDS.  ROWS says what is likely; any number of rows is right.
-constexpr int kRowPitch = 512 + 16;                    // bytes of a row's codes of a quad; the rest keeps the rows in different banks
+// Few rows: a workgroup owns a row block of weights (kGated: one of each projection) and sixteen rows of X over all of K; its wavefronts have a
+// part of K each, and their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the weights.  They are copied from memory
+// to LDS in whole cache lines, DEPTH blocks of 128 columns ahead, without passing through registers.
+// X is staged, all of it by all wavefronts before the first product (SRC 1, 2: quantised by sixteen lanes per block); or (XP > 0), where that would take
+// too much LDS, its codes come block by block with the weights, XP pieces of eight rows.
+// The sums of the codes are exact (Wide): the 16-bit instruction's half rate is far above what the reads leave to do.
+constexpr int kAhead = 4;                              // blocks of X per sixteen lanes that are asked for before the weights are
 
-template <int SRC, int R, int ROWS, int MODE, bool GROUPED>
-__global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const ProductParams p) {
-    static_assert(MODE != kGated || R == 2, "a row block of each projection");
-    extern __shared__ __align__(16) char smem[];
+// Waits until at most BLOCKS times N of this wavefront's global loads are under way.
+template <int N> __device__ __forceinline__ void wait_blocks(int blocks) {
+    if (blocks >= 3) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * N) : "memory");
+    else if (blocks == 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * N) : "memory");
+    else if (blocks == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+constexpr int stream_depth(int mode) { return mode == kGated ? 2 : 4; }
+// Bytes of LDS of a wavefront's places.
+constexpr int stream_place(int mode, int xp) { return stream_depth(mode) * ((mode == kGated ? 2 : 1) * 2048 + xp * 1024 + (xp ? 256 : 0)); }
+
+template <int SRC, int XP, int MODE, bool GROUPED, bool ONCE>
+__global__ __launch_bounds__(1024) void stream_kernel(const ProductParams p) {
+    constexpr int R = MODE == kGated ? 2 : 1, DEPTH = stream_depth(MODE);
+    static_assert(DEPTH <= 4, "as wait_blocks knows");
+    static_assert(SRC == kF32 || XP == 0, "16-bit values are staged");
+    constexpr int kSlot = R * 2048 + XP * 1024 + (XP ? 256 : 0), kCopies = 2 * R + (XP ? XP + 1 : 0);
+    extern __shared__ __align__(1024) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int waves = blockDim.x >> 6, i = lane & 15, o = lane >> 4;
     const int slot = p.slot0 + (int)blockIdx.y;
@@ -85,104 +109,145 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
         m0 = in.first + (slot - in.begin) * 16;
         m1 = min(in.end, m0 + 16);
     }
-    constexpr int kBlocks = MODE == kGated ? 1 : R;    // row blocks of Y
-    const int rb0 = (int)blockIdx.x * kBlocks, rows = m1 - m0;
+    const int rb0 = (int)blockIdx.x, rows = m1 - m0;
     const char* w[R];
     const float* ws[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int64_t row = MODE == kGated ? (int64_t)r * p.N + rb0 * 16 : (int64_t)min(rb0 + r, p.NB - 1) * 16;
+        const int64_t row = (int64_t)r * p.N + rb0 * 16;
         w[r] = p.w + expert * p.expert + row * p.K;
         ws[r] = p.ws + expert * p.expert_scales + (row >> 7) * p.KT;
     }
-    char* const place = smem + wave * (p.place_rows * (kRowPitch + 16));
-    float* const place_scales = reinterpret_cast<float*>(place + p.place_rows * kRowPitch);
-    const uint32_t mine = (uint32_t)i * (uint32_t)p.K + o * 16;
+    char* const place = smem + wave * (DEPTH * kSlot);
+    char* const staged = smem + waves * (DEPTH * kSlot);
+    const int pitch = p.K + 16;
+    float* const staged_scales = reinterpret_cast<float*>(staged + p.place_rows * pitch);              // [block][row]
 
-    f32x4 acc[R] = {};
-    const int quads = (p.KT + 3) >> 2;
-    for (int q = wave; q < quads; q += waves) {
-        const int tiles = min(4, p.KT - 4 * q);
-        // X first: loads are waited for in order, and it has further to go.  Rows that do not exist stay unread, and whatever lies in their
-        // operands is multiplied: their sums are not stored.
-        u32x4 xv[4][2] = {};
-        float xs[4] = {};
-        Eight<SRC == kF32 ? kF16 : SRC> few[ROWS];
-        const bool there = o < tiles;
-        auto ask_few = [&](int first) {                // lane 16 block + piece
-            const char* from = p.x + ((int64_t)(m0 + first) * p.K + q * 512 + lane * 8) * 2;
+    // This wavefront's blocks (up to 2^15 of them, and sixteen wavefronts: the product fits).
+    const int kb0 = quotient(wave * p.KT, waves), kb1 = quotient((wave + 1) * p.KT, waves);
+    // Scales of the weights: 64 blocks ahead, one per lane.
+    float sw[R];
+    auto ask_scales = [&](int kb) {
 #pragma unroll
-            for (int k = 0; k < ROWS; ++k)
-                if (first + k < rows && there) few[k].v[0] = *reinterpret_cast<const u32x4*>(from + (int64_t)k * p.K * 2);
-        };
+        for (int r = 0; r < R; ++r) sw[r] = ws[r][min(kb + lane, p.KT - 1)];
+    };
+    ask_scales(kb0);
+    // What is staged: unit u is block u / rows of row u % rows.
+    const int units = XP ? 0 : rows * p.KT, teams = (int)blockDim.x >> 4, team = (int)threadIdx.x >> 4;
+    Eight<SRC == kF32 ? kF16 : SRC> ahead[kAhead];
+    u32x2 ahead_codes[kAhead];
+    float ahead_scale[kAhead];
+    auto ask = [&](int u, int t) {
+        if (u >= units) return;
+        const int kb = quotient_of_lane(u, rows), row = m0 + u - kb * rows;
+        const int64_t at = (int64_t)row * p.K + kb * 128 + 8 * i;
         if constexpr (SRC == kF32) {
-            const char* from = p.x + (int64_t)(m0 + i) * p.K + q * 512 + o * 16;
-            if (i < rows) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    const int at = min(t, tiles - 1);
-                    xv[t][0] = *reinterpret_cast<const u32x4*>(from + at * 128);
-                    xv[t][1] = *reinterpret_cast<const u32x4*>(from + at * 128 + 64);
-                    xs[t] = p.xs[(int64_t)(4 * q + at) * p.M + m0 + i];
-                }
-            }
+            ahead_codes[t] = *reinterpret_cast<const u32x2*>(p.x + at);
+            ahead_scale[t] = p.xs[(int64_t)kb * p.M + row];
         } else {
-            ask_few(0);
+            ahead[t].v[0] = *reinterpret_cast<const u32x4*>(p.x + at * 2);
         }
-        u32x4 wv[R][4][2];
-        float sw[R][4];
+    };
+    auto stage = [&](int u, int t) {
+        if (u >= units) return;
+        const int kb = quotient_of_lane(u, rows), row = u - kb * rows;
+        float scale;
+        u32x2 codes;
+        if constexpr (SRC == kF32) {
+            codes = ahead_codes[t];
+            scale = ahead_scale[t];
+        } else {
+            float v[8];
+            to_floats<SRC>(ahead[t], v);
+            const Scale s = scale_of(largest_of_sixteen(largest(v)));
+            codes = to_codes(v, s);
+            scale = s.scale;
+        }
+        // (written so, as the compiler would have every copy to LDS that is under way arrive before it lets anything else write there)
+        const uint32_t to = lds_offset(staged + row * pitch + kb * 128 + 8 * i), scale_to = lds_offset(staged_scales + kb * rows + row);
+        asm volatile("ds_write_b64 %0, %1" ::"v"(to), "v"(codes) : "memory");
+        if (i == 0) asm volatile("ds_write_b32 %0, %1" ::"v"(scale_to), "v"(scale) : "memory");
+    };
+    if constexpr (XP == 0) {
+#pragma unroll
+        for (int t = 0; t < kAhead; ++t) ask(team + t * teams, t);
+    }
+
+    const int block = (lane & 7) ^ (lane >> 4);        // of the row that this lane copies, as in the tiles
+    uint32_t from[2], xfrom[XP ? XP : 1];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) from[c] = (uint32_t)(8 * c + (lane >> 3)) * (uint32_t)p.K + (block ^ (4 * c)) * 16;
+#pragma unroll
+    for (int c = 0; c < XP; ++c) xfrom[c] = (uint32_t)min(8 * c + (lane >> 3), rows - 1) * (uint32_t)p.K + (block ^ (4 * c)) * 16;
+    auto issue = [&](int kb, int d) {
+        char* to = place + d * kSlot;
+        if constexpr (XP > 0) {
+#pragma unroll
+            for (int c = 0; c < XP; ++c) copy16(unbounded(p.x + (int64_t)m0 * p.K), xfrom[c], kb * 128, to + R * 2048 + c * 1024);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(unbounded(reinterpret_cast<const char*>(p.xs + (int64_t)kb * p.M + m0)),
+                (__attribute__((address_space(3))) void*)(to + R * 2048 + XP * 1024), 4, min(i, rows - 1) * 4, 0, 0, 0);
+        }
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int t = 0; t < 4; ++t) sw[r][t] = ws[r][4 * q + min(t, tiles - 1)];
-        auto ask = [&](auto how) {
-            constexpr int HOW = decltype(how)::value;
+            for (int c = 0; c < 2; ++c) copy16<ONCE ? kNonTemporal : 0>(unbounded(w[r]), from[c], kb * 128, to + r * 2048 + c * 1024);
+    };
 #pragma unroll
-            for (int t = 0; t < 4; ++t)
+    for (int d = 0; d < DEPTH; ++d) issue(min(kb0 + d, max(kb1 - 1, kb0)), d);     // (fewer blocks than there is room for: the last again)
+    if constexpr (XP == 0) {
 #pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    const int at = (4 * q + min(t, tiles - 1)) * 128;
-                    wv[r][t][0] = __builtin_amdgcn_raw_buffer_load_b128(unbounded(w[r]), mine, at, HOW);
-                    wv[r][t][1] = __builtin_amdgcn_raw_buffer_load_b128(unbounded(w[r]), mine, at + 64, HOW);
-                }
-        };
-        if (p.once) ask(std::integral_constant<int, kNonTemporal>());
-        else ask(std::integral_constant<int, 0>());
-        if constexpr (SRC != kF32) {
-            for (int first = 0; first < rows; first += ROWS) {
-                if (first > 0) ask_few(first);
-#pragma unroll
-                for (int k = 0; k < ROWS; ++k) {
-                    if (first + k >= rows || !there) continue;
-                    float v[8];
-                    to_floats<SRC>(few[k], v);
-                    const Scale s = scale_of(largest_of_sixteen(largest(v)));
-                    *reinterpret_cast<u32x2*>(place + (first + k) * kRowPitch + lane * 8) = to_codes(v, s);
-                    if (i == 0) place_scales[(first + k) * 4 + o] = s.scale;
-                }
-            }
-            between_lanes();
-            if (i < rows) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    if (t >= tiles) break;
-                    xv[t][0] = *reinterpret_cast<const u32x4*>(place + i * kRowPitch + t * 128 + o * 16);
-                    xv[t][1] = *reinterpret_cast<const u32x4*>(place + i * kRowPitch + t * 128 + o * 16 + 64);
-                    xs[t] = place_scales[i * 4 + t];
-                }
-            }
+        for (int t = 0; t < kAhead; ++t) stage(team + t * teams, t);
+        for (int u = team + kAhead * teams; u < units; u += teams) {
+            ask(u, 0);
+            stage(u, 0);
         }
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-            if (t >= tiles) break;
-            const i32x8 x = operand(xv[t][0], xv[t][1]);
-#pragma unroll
-            for (int r = 0; r < R; ++r) acc[r] += product(operand(wv[r][t][0], wv[r][t][1]), x, f32x4{0.f, 0.f, 0.f, 0.f}) * (xs[t] * sw[r][t]);
-        }
-        if constexpr (SRC != kF32) between_lanes();
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
 
-    __syncthreads();
+    f32x4 acc[R] = {};
+    const int first_half = (o ^ (i >> 1)) * 16, second_half = ((4 + o) ^ (i >> 1)) * 16, xrow = min(i, rows - 1);
+    int d = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+        const int mine = kb - kb0;
+        if (mine > 0 && (mine & 63) == 0) {            // (waited for here: a wait where they are used would be one for every copy under way)
+            ask_scales(kb);
+#pragma unroll
+            for (int r = 0; r < R; ++r) asm volatile("s_waitcnt vmcnt(0)" : "+v"(sw[r])::"memory");
+        }
+        const char* at = place + d * kSlot;
+        wait_blocks<kCopies>(min(kb1 - kb, DEPTH) - 1);
+        i32x8 wv[R], xv;
+        float xs;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const char* a = at + r * 2048 + i * 128;
+            wv[r] = operand(*reinterpret_cast<const u32x4*>(a + first_half), *reinterpret_cast<const u32x4*>(a + second_half));
+        }
+        if constexpr (XP > 0) {
+            const int row = XP == 1 ? i & 7 : i;
+            const char* a = at + R * 2048 + row * 128;
+            xv = operand(*reinterpret_cast<const u32x4*>(a + ((o ^ (row >> 1)) * 16)), *reinterpret_cast<const u32x4*>(a + (((4 + o) ^ (row >> 1)) * 16)));
+            xs = *reinterpret_cast<const float*>(at + R * 2048 + XP * 1024 + i * 4);
+        } else {
+            const char* a = staged + xrow * pitch + kb * 128 + o * 16;
+            xv = operand(*reinterpret_cast<const u32x4*>(a), *reinterpret_cast<const u32x4*>(a + 64));
+            xs = staged_scales[kb * rows + xrow];
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                     // (the place is free)
+        if (kb + DEPTH < kb1) issue(kb + DEPTH, d);
+        d = d == DEPTH - 1 ? 0 : d + 1;
+        const Wide x = widen(xv);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float s = xs * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sw[r]), mine & 63));
+            const f32x4 sums = product(widen(wv[r]), x, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[r][j] = __builtin_fmaf(sums[j], s, acc[r][j]);
+        }
+    }
+
+    // (no copy is under way; the places and what is staged are free when all are here)
+    arrive<0>();
     f32x4* sums = reinterpret_cast<f32x4*>(smem);      // [wave][row block][lane]
 #pragma unroll
     for (int r = 0; r < R; ++r) sums[(wave * R + r) * 64 + lane] = acc[r];
@@ -203,8 +268,7 @@ __global__ __launch_bounds__(R == 1 ? 1024 : 512) void stream_kernel(const Produ
             store_four(p.saved + (row * 2 * p.N + p.N + column) * 2, u, p.bf16);
         }
     } else {
-        for (int r = wave; r < R; r += waves)
-            if (i < rows && rb0 + r < p.NB) store_four(p.y + ((int64_t)(m0 + i) * p.N + 16 * (rb0 + r) + 4 * o) * 2, sum_of(r), p.bf16);
+        if (wave == 0 && i < rows) store_four(p.y + ((int64_t)(m0 + i) * p.N + 16 * rb0 + 4 * o) * 2, sum_of(0), p.bf16);
     }
 }
 
@@ -235,7 +299,7 @@ template <int WN, int WM, int GN, int GM, int DEPTH, int MODE> struct TileShape 
     static constexpr int kSums = kWaves * WN * WM * 1024;                      // bytes of a tile's sums
 };
 
-template <int WN, int WM, int GN, int GM, int DEPTH, int MODE, bool GROUPED>
+template <int WN, int WM, int GN, int GM, int DEPTH, int MODE, bool GROUPED, bool EXACT>
 __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductParams p) {
     using Shape = TileShape<WN, WM, GN, GM, DEPTH, MODE>;
     constexpr int kWaves = Shape::kWaves, kRB = Shape::kRB, kMB = Shape::kMB, kStep = Shape::kStep, kBlocks = Shape::kBlocks;
@@ -415,6 +479,11 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
                 for (int h = 0; h < (MODE == kGated ? 2 : 1); ++h) s[h][b] = xs[b] * ws[h];
             }
         }
+        Wide wide[EXACT ? WM : 1];
+        if constexpr (EXACT) {
+#pragma unroll
+            for (int b = 0; b < WM; ++b) wide[b] = widen(x[b]);
+        }
         const int from = here;
 #pragma unroll
         for (int r = 0; r < WN; ++r) {
@@ -430,13 +499,17 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             if (r + kRing - 1 < WN) read_w(from, r + kRing - 1);
             else read_w(here, r + kRing - 1 - WN);
             if (r == WN - 1) read_scales(here);
+            Wide wide_w;
+            if constexpr (EXACT) wide_w = widen(w[r % kRing]);
 #pragma unroll
             for (int b = 0; b < WM; ++b) {
                 if constexpr (MODE == kPowers) {
                     acc[r][b] = scaled_product(w[r % kRing], x[b], acc[r][b], we[r % kRing], xe[b]);
                     asm volatile("" : "+v"(acc[r][b])::"memory");
                 } else {
-                    f32x4 sums = product(w[r % kRing], x[b], f32x4{0.f, 0.f, 0.f, 0.f});
+                    f32x4 sums = {0.f, 0.f, 0.f, 0.f};
+                    if constexpr (EXACT) sums = product(wide_w, wide[b], sums);
+                    else sums = product(w[r % kRing], x[b], sums);
                     asm volatile("" : "+v"(sums)::"memory");
                     f32x4& last = b ? acc[r][b - 1] : r ? acc[r - 1][WM - 1] : acc[WN - 1][WM - 1];
 #pragma unroll
@@ -580,25 +653,29 @@ constexpr size_t kCounterBytes = 64 * 1024;
 constexpr int64_t kCounters = kCounterBytes / 4;
 constexpr size_t kPartialBytes = 32 * 1024 * 1024;
 
+// Bytes of LDS of X that is staged, with its scales.
+constexpr int64_t staged_bytes(int64_t rows, int64_t K) { return rows * (K + 16) + rows * (K / 128) * 4; }
+
 int64_t most_pieces(const ProductParams& p, int rows) { return product::most_pieces(p.M, p.offsets ? p.experts : 0, rows); }
 
-template <int SRC, int R, int ROWS, int MODE>
+template <int SRC, int XP, int MODE>
 hipError_t launch_stream(ProductParams p, int waves, hipStream_t s) {
-    constexpr int kBlocks = MODE == kGated ? 1 : R;
-    const int nx = (p.NB + kBlocks - 1) / kBlocks;
-    p.place_rows = SRC == kF32 ? 0 : p.M < 16 ? p.M : 16;
-    const size_t place = (size_t)p.place_rows * (kRowPitch + 16), sums = R * 1024;
-    const size_t lds = waves * (place > sums ? place : sums);
+    p.place_rows = XP ? 0 : p.M < 16 ? p.M : 16;
+    const size_t lds = (size_t)waves * stream_place(MODE, XP) + staged_bytes(p.place_rows, p.K);
     // (a launch has fewer than 2^16 workgroups along y and 2^32 threads)
-    int64_t most = (int64_t(1) << 31) / (int64_t(nx) * waves * 64);
+    int64_t most = (int64_t(1) << 31) / (int64_t(p.NB) * waves * 64);
     most = most > 65535 ? 65535 : most;
     const int64_t slots = most_pieces(p, 16);
     hipError_t e = hipSuccess;
     for (int64_t at = 0; at < slots && e == hipSuccess; at += most) {
         p.slot0 = (int)at;
-        const dim3 grid(nx, (unsigned)(slots - at < most ? slots - at : most));
-        e = p.offsets ? launch<stream_kernel<SRC, R, ROWS, MODE, true>>(grid, waves * 64, lds, p, s)
-                      : launch<stream_kernel<SRC, R, ROWS, MODE, false>>(grid, waves * 64, lds, p, s);
+        const dim3 grid(p.NB, (unsigned)(slots - at < most ? slots - at : most));
+        auto run = [&](auto once) {
+            constexpr bool ONCE = decltype(once)::value;
+            return p.offsets ? launch<stream_kernel<SRC, XP, MODE, true, ONCE>>(grid, waves * 64, lds, p, s)
+                             : launch<stream_kernel<SRC, XP, MODE, false, ONCE>>(grid, waves * 64, lds, p, s);
+        };
+        e = p.once ? run(std::true_type()) : run(std::false_type());
     }
     return e;
 }
@@ -607,7 +684,7 @@ hipError_t launch_stream(ProductParams p, int waves, hipStream_t s) {
 struct TileSize { int channels, rows, waves, room; };
 constexpr TileSize kTiles[] = {{256, 256, 8, 2}, {128, 128, 8, 4}, {128, 64, 8, 4}, {64, 64, 4, 4}};
 
-template <int SHAPE, int WN, int WM, int GN, int GM, int DEPTH, int MODE>
+template <int SHAPE, int WN, int WM, int GN, int GM, int DEPTH, int MODE, bool EXACT>
 hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
     using Shape = TileShape<WN, WM, GN, GM, DEPTH, MODE>;
     static_assert(kTiles[SHAPE].channels == 16 * Shape::kRB && kTiles[SHAPE].rows == 16 * Shape::kMB && kTiles[SHAPE].waves == Shape::kWaves &&
@@ -622,9 +699,9 @@ hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
         p.slots = (int)(pieces - at < most ? pieces - at : most);
         const int64_t items = nx * p.slots * p.slices, grid = items < (int64_t)cus * kAtOnce ? items : (int64_t)cus * kAtOnce;
         const dim3 g((unsigned)grid);
-        if constexpr (MODE == kPowers) e = launch<tile_kernel<WN, WM, GN, GM, DEPTH, MODE, false>>(g, Shape::kThreads, Shape::kLds, p, s);
-        else e = p.offsets ? launch<tile_kernel<WN, WM, GN, GM, DEPTH, MODE, true>>(g, Shape::kThreads, Shape::kLds, p, s)
-                           : launch<tile_kernel<WN, WM, GN, GM, DEPTH, MODE, false>>(g, Shape::kThreads, Shape::kLds, p, s);
+        if constexpr (MODE == kPowers) e = launch<tile_kernel<WN, WM, GN, GM, DEPTH, MODE, false, EXACT>>(g, Shape::kThreads, Shape::kLds, p, s);
+        else e = p.offsets ? launch<tile_kernel<WN, WM, GN, GM, DEPTH, MODE, true, EXACT>>(g, Shape::kThreads, Shape::kLds, p, s)
+                           : launch<tile_kernel<WN, WM, GN, GM, DEPTH, MODE, false, EXACT>>(g, Shape::kThreads, Shape::kLds, p, s);
     }
     return e;
 }
@@ -635,8 +712,8 @@ hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
 struct TileChoice { int shape, slices; };             // shape -1: streamed
 
 // `NB`: row blocks of weights, kGated: of both projections.
-TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, int cus) {
-    const double S = (double)KT;
+TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool exact, int cus) {
+    const double S = (double)KT * (exact ? 1.6 : 1.0);
     TileChoice best{-1, 1};
     auto tiles = [&](int64_t rb, int64_t rows) {
         const int64_t nx = (NB + rb - 1) / rb;
@@ -652,7 +729,7 @@ TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int 
     auto rounds = [&](double t) { return (double)(int64_t)((t + cus - 1) / cus); };
     auto pairs = [&](double n, double one, double two) { return two * (double)(int64_t)(n / 2) + ((int64_t)n % 2 ? one : 0.0); };
     const double t0 = tiles(16, 256), t1 = tiles(8, 128), t2 = tiles(8, 64), t3 = tiles(4, 64);
-    consider(0, 1, 6.0 + rounds(t0) * (1.75 * S + 4.5 * (t0 < cus ? t0 / cus : 1.0)));
+    if (!exact) consider(0, 1, 6.0 + rounds(t0) * (1.75 * S + 4.5 * (t0 < cus ? t0 / cus : 1.0)));
     for (int z = 1; z <= 8; ++z) {
         if (z > KT) break;
         const double steps = (double)((int64_t)(S + z - 1) / z);
@@ -674,45 +751,50 @@ struct Choice {
     bool apart;                // X of 16 bits is quantised by a launch of its own
     bool once;                 // weights past the caches
     // streamed:
-    int wide;                  // row blocks per workgroup
-    int rows;                  // of X that are quantised at a time, 0: X is codes
+    int pieces;                // of eight rows of X that come with them, 0: X is staged
     int waves;                 // per workgroup
 };
 
 // `experts`: 0 without.
-Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool codes, int cus) {
+Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool exact, bool codes, int cus) {
     Choice c{};
     const int KQ = (int)((KT + 3) / 4);
-    c.tiles = choose_tiles(M, NB, KT, experts, mode, cus);
+    c.tiles = choose_tiles(M, NB, KT, experts, mode, exact, cus);
     const int64_t pieces = experts ? (M < experts ? M : experts) : (M + 15) / 16, mean = (M + pieces - 1) / pieces;
-    c.apart = !codes && (c.tiles.shape >= 0 || mean > 4);
-    if (c.apart) codes = true;
-    c.wide = mode == kGated ? 2 : NB * pieces > 1024 && mean > 2 ? 2 : 1;
-    const int64_t groups = (NB + c.wide - 1) / c.wide * pieces;
-    const int64_t shared = c.tiles.shape >= 0 ? 0 : experts ? 4 : 16;
-    c.once = (experts ? mean : M) <= shared && NB * (experts ? pieces : 1) * KT * 2048 > (int64_t(128) << 20);
-    const int most = groups > 4096 ? 4 : c.wide > 1 || groups > 512 ? 8 : 16;
-    c.waves = KQ < most ? KQ : most;
-    c.rows = codes ? 0 : mean > 1 ? 4 : 1;
+    const int64_t groups = (mode == kGated ? NB / 2 : NB) * pieces, most_rows = M < 16 ? M : 16;
+    constexpr int64_t kStagedMost = 32 * 1024;
+    const bool staged = staged_bytes(most_rows, KT * 128) <= kStagedMost;
+    c.apart = !codes && (c.tiles.shape >= 0 || mean > 4 || !staged);
+    c.once = c.tiles.shape < 0 && (experts ? mean <= 4 : M <= 16) && NB * (experts ? pieces : 1) * KT * 2048 > (int64_t(128) << 20);
+    c.pieces = (c.apart || codes) && !(staged && mean <= 4) ? (most_rows > 8 ? 2 : 1) : 0;
+    const int depth = stream_depth(mode), per_wave = stream_place(mode, c.pieces);
+    const int64_t room = 160 * 1024 - (c.pieces ? 0 : staged_bytes(most_rows, KT * 128));
+    int64_t waves = KT / depth < 1 ? 1 : KT / depth;
+    if (waves > 16) waves = 16;
+    if (waves > 8 && groups > 512) waves = 8;
+    while (waves > 1 && waves * per_wave > (groups > cus ? room / 2 : room)) --waves;
+    c.waves = (int)waves;
     return c;
 }
 
-template <int R, int MODE> hipError_t launch_stream_of(int src, int rows, const ProductParams& p, int waves, hipStream_t s) {
-    if (rows == 0) return launch_stream<kF32, R, 1, MODE>(p, waves, s);
-    if (rows == 1) return src == kF16 ? launch_stream<kF16, R, 1, MODE>(p, waves, s) : launch_stream<kBF16, R, 1, MODE>(p, waves, s);
-    return src == kF16 ? launch_stream<kF16, R, 4, MODE>(p, waves, s) : launch_stream<kBF16, R, 4, MODE>(p, waves, s);
+template <int MODE> hipError_t launch_stream_of(int src, int pieces, const ProductParams& p, int waves, hipStream_t s) {
+    if (pieces == 1) return launch_stream<kF32, 1, MODE>(p, waves, s);
+    if (pieces == 2) return launch_stream<kF32, 2, MODE>(p, waves, s);
+    return src == kF32   ? launch_stream<kF32, 0, MODE>(p, waves, s)
+           : src == kF16 ? launch_stream<kF16, 0, MODE>(p, waves, s)
+                         : launch_stream<kBF16, 0, MODE>(p, waves, s);
 }
 
-template <int MODE> hipError_t launch_of(const Choice& c, int src, const ProductParams& p, int cus, hipStream_t s) {
+template <int MODE, bool EXACT = false> hipError_t launch_of(const Choice& c, int src, const ProductParams& p, int cus, hipStream_t s) {
     switch (c.tiles.shape) {
-        case 0: return launch_tiles<0, 8, 4, 2, 4, 2, MODE>(p, cus, s);
-        case 1: return launch_tiles<1, 4, 2, 2, 4, 4, MODE>(p, cus, s);
-        case 2: return launch_tiles<2, 2, 2, 4, 2, 4, MODE>(p, cus, s);
-        case 3: return launch_tiles<3, 2, 2, 2, 2, 4, MODE>(p, cus, s);
+        case 0:
+            if constexpr (!EXACT) return launch_tiles<0, 8, 4, 2, 4, 2, MODE, EXACT>(p, cus, s);
+            return hipErrorInvalidValue;
+        case 1: return launch_tiles<1, 4, 2, 2, 4, 4, MODE, EXACT>(p, cus, s);
+        case 2: return launch_tiles<2, 2, 2, 4, 2, 4, MODE, EXACT>(p, cus, s);
+        case 3: return launch_tiles<3, 2, 2, 2, 2, 4, MODE, EXACT>(p, cus, s);
     }
-    if constexpr (MODE == kGated) return launch_stream_of<2, MODE>(src, c.rows, p, c.waves, s);
-    else if constexpr (MODE == kPlain)
-        return c.wide == 1 ? launch_stream_of<1, MODE>(src, c.rows, p, c.waves, s) : launch_stream_of<2, MODE>(src, c.rows, p, c.waves, s);
+    if constexpr (MODE != kPowers) return launch_stream_of<MODE>(src, c.pieces, p, c.waves, s);
     return hipErrorInvalidValue;
 }
 
@@ -751,18 +833,19 @@ lutq_status product_on(const Call& a, hipStream_t s) {
     float* const scales = reinterpret_cast<float*>(codes + up256((size_t)a.M * a.K));
     char* const dense = reinterpret_cast<char*>(scales) + up256((size_t)a.M * (a.K / 128) * 4);
     p.y = a.y ? static_cast<char*>(a.y) : dense; p.saved = static_cast<char*>(a.saved);
-    const int src = a.xs ? kF32 : a.dtype == LUTQ_F16 ? kF16 : kBF16;
+    int src = a.xs ? kF32 : a.dtype == LUTQ_F16 ? kF16 : kBF16;
     const int cus = compute_units();
     if (cus < 1) return LUTQ_ERR_DEVICE;
-    const Choice c = choose(a.M, w_rows / 16, p.KT, p.offsets ? a.experts : 0, a.mode, a.xs != nullptr, cus);
+    const Choice c = choose(a.M, w_rows / 16, p.KT, p.offsets ? a.experts : 0, a.mode, a.saved != nullptr, a.xs != nullptr, cus);
     if (c.apart) {
         const lutq_status st = quantize_rows_on(a.x, src, a.M, nullptr, nullptr, 0, a.M, a.K, codes, scales, s);
         if (st != LUTQ_OK) return st;
         p.x = codes; p.xs = scales;
+        src = kF32;
     }
     p.once = c.once;
     p.slices = c.tiles.slices;
-    const hipError_t e = a.mode == kGated ? launch_of<kGated>(c, src, p, cus, s) : a.mode == kPowers ? launch_of<kPowers>(c, src, p, cus, s)
+    const hipError_t e = a.mode == kGated ? (a.saved ? launch_of<kGated, true>(c, src, p, cus, s) : launch_of<kGated>(c, src, p, cus, s)) : a.mode == kPowers ? launch_of<kPowers>(c, src, p, cus, s)
                                                                                                    : launch_of<kPlain>(c, src, p, cus, s);
     if (e != hipSuccess) return LUTQ_ERR_DEVICE;
     if (!a.h_codes) return LUTQ_OK;
@@ -825,13 +908,15 @@ extern "C" lutq_status lutq_fp8_weight_grad(const void* dY, const float* dy_scal
 
 extern "C" int lutq_calib_fp8_launch(int64_t M, int64_t N, int64_t K, int64_t experts, int form, int x_is_codes, int compute_units, int* launch) {
     if (!launch) return LUTQ_ERR_NULL;
-    if (form < 0 || form > 2 || experts < 0 || M < 1 || compute_units < 1 || compute_units > 4096 || (form == kPowers && (experts || !x_is_codes)) ||
-        (form == kGated ? lutq_fp8_gated_workspace_bytes(M, N, K, experts ? experts : 1) : lutq_fp8_workspace_bytes(M, N, K, experts ? experts : 1)) == 0)
+    constexpr int kSaved = 3;
+    const bool gate = form == kGated || form == kSaved;
+    if (form < 0 || form > 3 || experts < 0 || M < 1 || compute_units < 1 || compute_units > 4096 || (form == kPowers && (experts || !x_is_codes)) ||
+        (gate ? lutq_fp8_gated_workspace_bytes(M, N, K, experts ? experts : 1) : lutq_fp8_workspace_bytes(M, N, K, experts ? experts : 1)) == 0)
         return LUTQ_ERR_SHAPE;
-    const Choice c = choose(M, N / 16 * (form == kGated ? 2 : 1), K / 128, experts, form, x_is_codes != 0, compute_units);
+    const Choice c = choose(M, N / 16 * (gate ? 2 : 1), K / 128, experts, form == kSaved ? kGated : form, form == kSaved, x_is_codes != 0, compute_units);
     const bool streamed = c.tiles.shape < 0;
-    const TileSize t = streamed ? TileSize{16 * c.wide, 16, c.waves, 0} : kTiles[c.tiles.shape];
-    const int out[8] = {c.apart, t.channels, t.rows, t.waves, t.room, c.tiles.slices, streamed ? c.rows : 0, c.once};
+    const TileSize t = streamed ? TileSize{gate ? 32 : 16, 16, c.waves, stream_depth(gate ? kGated : kPlain)} : kTiles[c.tiles.shape];
+    const int out[8] = {c.apart, t.channels, t.rows, t.waves, t.room, c.tiles.slices, streamed ? 1 + c.pieces : 0, c.once};
     for (int i = 0; i < 8; ++i) launch[i] = out[i];
     return LUTQ_OK;
 }
