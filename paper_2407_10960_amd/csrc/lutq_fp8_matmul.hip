@@ -70,13 +70,14 @@ __device__ __forceinline__ void store_four(char* to, const f32x4& sum, int bf16)
     *reinterpret_cast<u32x2*>(to) = u32x2{round_pair(sum[0], sum[1], bf16), round_pair(sum[2], sum[3], bf16)};
 }
 
-// Few rows: a workgroup owns a row block of weights (kGated: one of each projection) and sixteen rows of X over all of K; its wavefronts have a
-// part of K each, and their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the weights.  They are copied from memory
-// to LDS in whole cache lines, DEPTH blocks of 128 columns ahead, without passing through registers.
+// Few rows: a workgroup has up to sixteen rows of X and a run of row blocks of weights (kGated: of both projections), one after the other over all of K;
+// its wavefronts have a part of K each, and their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the weights: they
+// are copied from memory to LDS in whole cache lines, DEPTH blocks of 128 columns ahead, without passing through registers, and
+// from one row block to the next without a pause.
 // X is staged, all of it by all wavefronts before the first product (SRC 1, 2: quantised by sixteen lanes per block); or (XP > 0), where that would take
 // too much LDS, its codes come block by block with the weights, XP pieces of eight rows.
 // The sums of the codes are exact (Wide): the 16-bit instruction's half rate is far above what the reads leave to do.
-constexpr int kAhead = 4;                              // blocks of X per sixteen lanes that are asked for before the weights are
+constexpr int kAhead = 8;                              // blocks of X per sixteen lanes that are asked for at a time
 
 // Waits until at most BLOCKS times N of this wavefront's global loads are under way.
 template <int N> __device__ __forceinline__ void wait_blocks(int blocks) {
@@ -87,8 +88,12 @@ template <int N> __device__ __forceinline__ void wait_blocks(int blocks) {
 }
 
 constexpr int stream_depth(int mode) { return mode == kGated ? 2 : 4; }
-// Bytes of LDS of a wavefront's places.
+// Bytes of LDS of a wavefront's places, and of its sums, two sets of them in turn.
 constexpr int stream_place(int mode, int xp) { return stream_depth(mode) * ((mode == kGated ? 2 : 1) * 2048 + xp * 1024 + (xp ? 256 : 0)); }
+constexpr int stream_sums(int mode) { return 2 * (mode == kGated ? 2 : 1) * 1024; }
+
+// A number that every lane has, and that nothing in the launch writes.
+__device__ __forceinline__ float scalar_at(const float* p) { return *(const __attribute__((address_space(4))) float*)(uintptr_t)p; }
 
 template <int SRC, int XP, int MODE, bool GROUPED, bool ONCE>
 __global__ __launch_bounds__(1024) void stream_kernel(const ProductParams p) {
@@ -109,29 +114,19 @@ __global__ __launch_bounds__(1024) void stream_kernel(const ProductParams p) {
         m0 = in.first + (slot - in.begin) * 16;
         m1 = min(in.end, m0 + 16);
     }
-    const int rb0 = (int)blockIdx.x, rows = m1 - m0;
-    const char* w[R];
-    const float* ws[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int64_t row = (int64_t)r * p.N + rb0 * 16;
-        w[r] = p.w + expert * p.expert + row * p.K;
-        ws[r] = p.ws + expert * p.expert_scales + (row >> 7) * p.KT;
-    }
+    const int rows = m1 - m0;
+    // This workgroup's row blocks and this wavefront's part of K (up to 2^15 blocks over sixteen wavefronts: the products fit).
+    const int run = (int)blockIdx.x, each = quotient(p.NB, (int)gridDim.x), more = p.NB - each * (int)gridDim.x;
+    const int rb0 = run * each + min(run, more), rb1 = rb0 + each + (run < more ? 1 : 0);
+    const int kb0 = quotient(wave * p.KT, waves), kb1 = quotient((wave + 1) * p.KT, waves);
+    const char* const w = p.w + expert * p.expert;
+    const float* const ws = p.ws + expert * p.expert_scales;
     char* const place = smem + wave * (DEPTH * kSlot);
-    char* const staged = smem + waves * (DEPTH * kSlot);
-    const int pitch = p.K + 16;
+    f32x4* const sums = reinterpret_cast<f32x4*>(smem + waves * (DEPTH * kSlot));      // [in turn][wave][row block][lane]
+    char* const staged = smem + waves * (DEPTH * kSlot + stream_sums(MODE));
+    const int pitch = p.K + 16;                        // (rows sixteen bytes apart: no two in the same banks)
     float* const staged_scales = reinterpret_cast<float*>(staged + p.place_rows * pitch);              // [block][row]
 
-    // This wavefront's blocks (up to 2^15 of them, and sixteen wavefronts: the product fits).
-    const int kb0 = quotient(wave * p.KT, waves), kb1 = quotient((wave + 1) * p.KT, waves);
-    // Scales of the weights: 64 blocks ahead, one per lane.
-    float sw[R];
-    auto ask_scales = [&](int kb) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) sw[r] = ws[r][min(kb + lane, p.KT - 1)];
-    };
-    ask_scales(kb0);
     // What is staged: unit u is block u / rows of row u % rows.
     const int units = XP ? 0 : rows * p.KT, teams = (int)blockDim.x >> 4, team = (int)threadIdx.x >> 4;
     Eight<SRC == kF32 ? kF16 : SRC> ahead[kAhead];
@@ -179,8 +174,10 @@ __global__ __launch_bounds__(1024) void stream_kernel(const ProductParams p) {
     for (int c = 0; c < 2; ++c) from[c] = (uint32_t)(8 * c + (lane >> 3)) * (uint32_t)p.K + (block ^ (4 * c)) * 16;
 #pragma unroll
     for (int c = 0; c < XP; ++c) xfrom[c] = (uint32_t)min(8 * c + (lane >> 3), rows - 1) * (uint32_t)p.K + (block ^ (4 * c)) * 16;
-    auto issue = [&](int kb, int d) {
-        char* to = place + d * kSlot;
+    int rb_ahead = rb0, kb_ahead = kb0, d_ahead = 0;   // of the next copies
+    auto issue = [&]() {                               // (at the end the last block stays next)
+        char* to = place + d_ahead * kSlot;
+        const int kb = kb_ahead;
         if constexpr (XP > 0) {
 #pragma unroll
             for (int c = 0; c < XP; ++c) copy16(unbounded(p.x + (int64_t)m0 * p.K), xfrom[c], kb * 128, to + R * 2048 + c * 1024);
@@ -190,85 +187,98 @@ __global__ __launch_bounds__(1024) void stream_kernel(const ProductParams p) {
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) copy16<ONCE ? kNonTemporal : 0>(unbounded(w[r]), from[c], kb * 128, to + r * 2048 + c * 1024);
+            for (int c = 0; c < 2; ++c)
+                copy16<ONCE ? kNonTemporal : 0>(unbounded(w + ((int64_t)r * p.N + rb_ahead * 16) * p.K), from[c], kb * 128, to + r * 2048 + c * 1024);
+        d_ahead = d_ahead == DEPTH - 1 ? 0 : d_ahead + 1;
+        if (kb_ahead + 1 < kb1) ++kb_ahead;
+        else if (rb_ahead + 1 < rb1) {
+            kb_ahead = kb0;
+            ++rb_ahead;
+        }
     };
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) issue(min(kb0 + d, max(kb1 - 1, kb0)), d);     // (fewer blocks than there is room for: the last again)
+    for (int d = 0; d < DEPTH; ++d) issue();           // (fewer blocks than there is room for: the last again)
     if constexpr (XP == 0) {
 #pragma unroll
         for (int t = 0; t < kAhead; ++t) stage(team + t * teams, t);
-        for (int u = team + kAhead * teams; u < units; u += teams) {
-            ask(u, 0);
-            stage(u, 0);
+        for (int u = team + kAhead * teams; u < units; u += kAhead * teams) {
+#pragma unroll
+            for (int t = 0; t < kAhead; ++t) ask(u + t * teams, t);
+#pragma unroll
+            for (int t = 0; t < kAhead; ++t) stage(u + t * teams, t);
         }
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
 
-    f32x4 acc[R] = {};
     const int first_half = (o ^ (i >> 1)) * 16, second_half = ((4 + o) ^ (i >> 1)) * 16, xrow = min(i, rows - 1);
-    int d = 0;
-    for (int kb = kb0; kb < kb1; ++kb) {
-        const int mine = kb - kb0;
-        if (mine > 0 && (mine & 63) == 0) {            // (waited for here: a wait where they are used would be one for every copy under way)
-            ask_scales(kb);
+    int d = 0, turn = 0, left = (rb1 - rb0) * (kb1 - kb0);                     // blocks that are still to be multiplied
+    for (int rb = rb0; rb < rb1; ++rb) {
+        const float* const scales = ws + (int64_t)(rb >> 3) * p.KT;
+        f32x4 acc[R] = {};
+        for (int kb = kb0; kb < kb1; ++kb, --left) {
+            float sw[R];
 #pragma unroll
-            for (int r = 0; r < R; ++r) asm volatile("s_waitcnt vmcnt(0)" : "+v"(sw[r])::"memory");
-        }
-        const char* at = place + d * kSlot;
-        wait_blocks<kCopies>(min(kb1 - kb, DEPTH) - 1);
-        i32x8 wv[R], xv;
-        float xs;
+            for (int r = 0; r < R; ++r) sw[r] = scalar_at(scales + (int64_t)r * (p.N >> 7) * p.KT + kb);
+            const char* at = place + d * kSlot;
+            wait_blocks<kCopies>(min(left, DEPTH) - 1);
+            i32x8 wv[R], xv;
+            float xs;
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const char* a = at + r * 2048 + i * 128;
-            wv[r] = operand(*reinterpret_cast<const u32x4*>(a + first_half), *reinterpret_cast<const u32x4*>(a + second_half));
-        }
-        if constexpr (XP > 0) {
-            const int row = XP == 1 ? i & 7 : i;
-            const char* a = at + R * 2048 + row * 128;
-            xv = operand(*reinterpret_cast<const u32x4*>(a + ((o ^ (row >> 1)) * 16)), *reinterpret_cast<const u32x4*>(a + (((4 + o) ^ (row >> 1)) * 16)));
-            xs = *reinterpret_cast<const float*>(at + R * 2048 + XP * 1024 + i * 4);
-        } else {
-            const char* a = staged + xrow * pitch + kb * 128 + o * 16;
-            xv = operand(*reinterpret_cast<const u32x4*>(a), *reinterpret_cast<const u32x4*>(a + 64));
-            xs = staged_scales[kb * rows + xrow];
-        }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                     // (the place is free)
-        if (kb + DEPTH < kb1) issue(kb + DEPTH, d);
-        d = d == DEPTH - 1 ? 0 : d + 1;
-        const Wide x = widen(xv);
+            for (int r = 0; r < R; ++r) {
+                const char* a = at + r * 2048 + i * 128;
+                wv[r] = operand(*reinterpret_cast<const u32x4*>(a + first_half), *reinterpret_cast<const u32x4*>(a + second_half));
+            }
+            if constexpr (XP > 0) {
+                const int row = XP == 1 ? i & 7 : i;
+                const char* a = at + R * 2048 + row * 128;
+                xv = operand(*reinterpret_cast<const u32x4*>(a + ((o ^ (row >> 1)) * 16)), *reinterpret_cast<const u32x4*>(a + (((4 + o) ^ (row >> 1)) * 16)));
+                xs = *reinterpret_cast<const float*>(at + R * 2048 + XP * 1024 + i * 4);
+            } else {
+                const char* a = staged + xrow * pitch + kb * 128 + o * 16;
+                xv = operand(*reinterpret_cast<const u32x4*>(a), *reinterpret_cast<const u32x4*>(a + 64));
+                xs = staged_scales[kb * rows + xrow];
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");                 // (the place is free)
+            if (left > DEPTH) issue();
+            d = d == DEPTH - 1 ? 0 : d + 1;
+            const Wide x = widen(xv);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float s = xs * __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sw[r]), mine & 63));
-            const f32x4 sums = product(widen(wv[r]), x, f32x4{0.f, 0.f, 0.f, 0.f});
+            for (int r = 0; r < R; ++r) {
+                const float s = xs * sw[r];
+                const f32x4 codes = product(widen(wv[r]), x, f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[r][j] = __builtin_fmaf(sums[j], s, acc[r][j]);
+                for (int j = 0; j < 4; ++j) acc[r][j] = __builtin_fmaf(codes[j], s, acc[r][j]);
+            }
         }
-    }
 
-    // (no copy is under way; the places and what is staged are free when all are here)
-    arrive<0>();
-    f32x4* sums = reinterpret_cast<f32x4*>(smem);      // [wave][row block][lane]
+        // The wavefronts add up and store in turn.  (A set of sums is written again two row blocks later: behind a barrier that whoever reads
+        // it now reaches after that.)
+        f32x4* const set = sums + (rb & 1) * (waves * R * 64);
 #pragma unroll
-    for (int r = 0; r < R; ++r) sums[(wave * R + r) * 64 + lane] = acc[r];
-    __syncthreads();
-    auto sum_of = [&](int r) {
-        f32x4 sum = sums[r * 64 + lane];
-        for (int v = 1; v < waves; ++v) sum += sums[(v * R + r) * 64 + lane];
-        return sum;
-    };
-    if constexpr (MODE == kGated) {
-        if (wave > 0 || i >= rows) return;
-        const f32x4 g = sum_of(0), u = sum_of(1);
-        const int64_t row = m0 + i;
-        const int column = 16 * rb0 + 4 * o;
-        store_four(p.y + (row * p.N + column) * 2, gated(g, u, p.act), p.bf16);
-        if (p.saved) {
-            store_four(p.saved + (row * 2 * p.N + column) * 2, g, p.bf16);
-            store_four(p.saved + (row * 2 * p.N + p.N + column) * 2, u, p.bf16);
+        for (int r = 0; r < R; ++r) {
+            const uint32_t to = lds_offset(set + (wave * R + r) * 64 + lane);
+            asm volatile("ds_write_b128 %0, %1" ::"v"(to), "v"(acc[r]) : "memory");
         }
-    } else {
-        if (wave == 0 && i < rows) store_four(p.y + ((int64_t)(m0 + i) * p.N + 16 * rb0 + 4 * o) * 2, sum_of(0), p.bf16);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const bool my_turn = turn == wave;
+        turn = turn == waves - 1 ? 0 : turn + 1;
+        if (!my_turn) continue;
+        f32x4 sum[R] = {};
+        for (int v = 0; v < waves; ++v)
+#pragma unroll
+            for (int r = 0; r < R; ++r) sum[r] += set[(v * R + r) * 64 + lane];
+        if (i >= rows) continue;
+        const int64_t row = m0 + i;
+        const int column = 16 * rb + 4 * o;
+        if constexpr (MODE == kGated) {
+            store_four(p.y + (row * p.N + column) * 2, gated(sum[0], sum[1], p.act), p.bf16);
+            if (p.saved) {
+                store_four(p.saved + (row * 2 * p.N + column) * 2, sum[0], p.bf16);
+                store_four(p.saved + (row * 2 * p.N + p.N + column) * 2, sum[1], p.bf16);
+            }
+        } else {
+            store_four(p.y + (row * p.N + column) * 2, sum[0], p.bf16);
+        }
     }
 }
 
@@ -308,6 +318,8 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
     constexpr int kLoads = kWLoads + kXLoads + kScaleLoads;
     constexpr int kRing = WN < 4 ? WN : 4;             // row blocks of weights in registers
     constexpr int kTurn = WN - kRing + 1;              // the row block at which the next step is looked at
+    constexpr int kXRing = EXACT && WM > 2 ? 2 : WM;   // of X (EXACT: until it is widened)
+    constexpr int kDelay = EXACT ? 1 : kWaves * WN * WM >= 256 ? 1 : 2;
     static_assert(kWLoads * kWaves == 2 * kRB && kXLoads * kWaves == 2 * kMB && kMB % 4 == 0 && kRB % 4 == 0, "whole loads per wavefront");
     static_assert(MODE != kGated || kWLoads % 2 == 0, "as many of either projection");
     extern __shared__ __align__(1024) char lds[];      // DEPTH steps, then their scales, then a word
@@ -436,7 +448,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
     };
 
     const int wn = wave % GN, wm = wave / GN;
-    i32x8 w[kRing], x[WM];
+    i32x8 w[kRing], x[kXRing];
     float xs[WM], ws[MODE == kGated ? 2 : 1];          // scales of the step in the registers
     uint32_t we[kRing];
     f32x4 acc[WN][WM];
@@ -452,7 +464,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         w[r % kRing] = read(wplace + from * kStep + r * 2048);
         if constexpr (MODE == kPowers) we[r % kRing] = __builtin_bit_cast(uint32_t, scale_at(from, Shape::kXPieces * 64 + 16 * (wn * WN + r) + i)) >> 23;
     };
-    auto read_x = [&](int from, int b) { x[b] = read(xplace + from * kStep + b * 2048); };
+    auto read_x = [&](int from, int b) { x[b % kXRing] = read(xplace + from * kStep + b * 2048); };
     auto read_scales = [&](int from) {
 #pragma unroll
         for (int b = 0; b < WM; ++b) xs[b] = scale_at(from, 16 * (wm * WM + b) + i);
@@ -465,9 +477,20 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
 
     // A step: row block by row block of the weights.  Its X and its first kRing - 1 row blocks are in the registers; the others, and at the end
     // the next step's, are read kRing - 1 row blocks ahead, X as soon as its last product has been started.  What an instruction
-    // returns is added after the next one has been started.
-    f32x4 pending = {};
-    float pending_scale = 0.f;
+    // returns is added after kDelay more have been started.  Copies of a later step are asked for one at a time between the products.
+    // (The empty statements keep the compiler from moving products and additions past each other and past what is read.)
+    constexpr int kProducts = WN * WM;
+    static_assert(kProducts % kDelay == 0, "a product's place is the same in every step");
+    f32x4 pending[kDelay] = {};
+    float pending_scale[kDelay] = {};
+    auto retire = [&](int n) {                         // product n of this step, or, below 0, of the one before
+        f32x4& sum = acc[(n + kProducts) % kProducts / WM][(n + kProducts) % WM];
+        const int at = (n + kProducts) % kDelay;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum[j] = __builtin_fmaf(pending[at][j], pending_scale[at], sum[j]);
+        asm volatile("" : "+v"(sum)::"memory");
+    };
+    Wide wide[EXACT ? WM : 1];
     auto one_step = [&](bool stored) {
         float s[MODE == kGated ? 2 : 1][WM];
         uint32_t xe[WM];
@@ -478,11 +501,6 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
 #pragma unroll
                 for (int h = 0; h < (MODE == kGated ? 2 : 1); ++h) s[h][b] = xs[b] * ws[h];
             }
-        }
-        Wide wide[EXACT ? WM : 1];
-        if constexpr (EXACT) {
-#pragma unroll
-            for (int b = 0; b < WM; ++b) wide[b] = widen(x[b]);
         }
         const int from = here;
 #pragma unroll
@@ -499,10 +517,15 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             if (r + kRing - 1 < WN) read_w(from, r + kRing - 1);
             else read_w(here, r + kRing - 1 - WN);
             if (r == WN - 1) read_scales(here);
+            auto copies = [&](int at, int places) {    // of the places after the turn's, those of one
+#pragma unroll
+                for (int j = at * kLoads / places; j < (at + 1) * kLoads / places; ++j) load_part(j);
+            };
             Wide wide_w;
             if constexpr (EXACT) wide_w = widen(w[r % kRing]);
 #pragma unroll
             for (int b = 0; b < WM; ++b) {
+                const int n = r * WM + b;
                 if constexpr (MODE == kPowers) {
                     acc[r][b] = scaled_product(w[r % kRing], x[b], acc[r][b], we[r % kRing], xe[b]);
                     asm volatile("" : "+v"(acc[r][b])::"memory");
@@ -511,20 +534,19 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
                     if constexpr (EXACT) sums = product(wide_w, wide[b], sums);
                     else sums = product(w[r % kRing], x[b], sums);
                     asm volatile("" : "+v"(sums)::"memory");
-                    f32x4& last = b ? acc[r][b - 1] : r ? acc[r - 1][WM - 1] : acc[WN - 1][WM - 1];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) last[j] = __builtin_fmaf(pending[j], pending_scale, last[j]);
-                    asm volatile("" : "+v"(last)::"memory");
-                    pending = sums;
-                    pending_scale = s[MODE == kGated && r >= WN / 2][b];
+                    retire(n - kDelay);
+                    pending[n % kDelay] = sums;
+                    pending_scale[n % kDelay] = s[MODE == kGated && r >= WN / 2][b];
                 }
-                if (r == WN - 1) read_x(here, b);
+                if (r == WN - 1) {
+                    read_x(here, b);
+                    if constexpr (EXACT) {
+                        if (b > 0) wide[b - 1] = widen(x[(b - 1) % kXRing]);
+                        if (b == WM - 1) wide[b] = widen(x[b % kXRing]);
+                    }
+                }
                 __builtin_amdgcn_sched_barrier(0);
-            }
-            if (r >= kTurn) {
-                constexpr int kRows = WN - kTurn;
-#pragma unroll
-                for (int j = (r - kTurn) * kLoads / kRows; j < (r - kTurn + 1) * kLoads / kRows; ++j) load_part(j);
+                if (r >= kTurn) copies(n - kTurn * WM, (WN - kTurn) * WM);
             }
         }
     };
@@ -545,7 +567,10 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
 #pragma unroll
     for (int r = 0; r < kRing - 1; ++r) read_w(0, r);
 #pragma unroll
-    for (int b = 0; b < WM; ++b) read_x(0, b);
+    for (int b = 0; b < WM; ++b) {
+        read_x(0, b);
+        if constexpr (EXACT) wide[b] = widen(x[b % kXRing]);
+    }
     read_scales(0);
 
     bool stored = false;
@@ -554,19 +579,22 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         for (int r = 0; r < WN; ++r)
 #pragma unroll
             for (int b = 0; b < WM; ++b) acc[r][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-        pending = f32x4{0.f, 0.f, 0.f, 0.f};
-        pending_scale = 0.f;
+#pragma unroll
+        for (int d = 0; d < kDelay; ++d) {
+            pending[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+            pending_scale[d] = 0.f;
+        }
         mine += (int)gridDim.x;
         int s = it.step;
         one_step(stored);
         for (++s; s < it.steps; ++s) one_step(false);
         if constexpr (MODE != kPowers) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) acc[WN - 1][WM - 1][j] = __builtin_fmaf(pending[j], pending_scale, acc[WN - 1][WM - 1][j]);
+            for (int n = kProducts - kDelay; n < kProducts; ++n) retire(n);
         }
 
         bool finished = true;
-        if (Shape::kSlices && p.slices > 1) {          // the other slices of this tile
+        if constexpr (Shape::kSlices) if (p.slices > 1) {                      // the other slices of this tile
             const auto sums = unbounded(p.partial + ((int64_t)it.tile * p.slices) * Shape::kSums);
             const uint32_t at = wave * (WN * WM * 1024) + lane * 16;
 #pragma unroll
@@ -585,32 +613,26 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
             finished = __builtin_amdgcn_readfirstlane(*last);
             __syncthreads();                           // (the word is free for the next item)
             if (finished) {
-                // In the order of the slices, this one from its registers, the others two ahead.
-                f32x4 sum[WN][WM] = {}, even[WN][WM], odd[WN][WM];
-                auto ask = [&](int z, f32x4(&to)[WN][WM]) {
-                    if (z >= p.slices || z == it.slice) return;
+                // In the order of the slices, this one from its registers, of the others as many at a time as there are registers for.
+                constexpr int kAtATime = 24 / (WN * WM);
+                f32x4 sum[WN][WM] = {}, other[kAtATime][WN][WM];
+                for (int z0 = 0; z0 < p.slices; z0 += kAtATime) {
 #pragma unroll
-                    for (int r = 0; r < WN; ++r)
+                    for (int z = 0; z < kAtATime; ++z) {
+                        if (z0 + z >= p.slices) continue;
 #pragma unroll
-                        for (int b = 0; b < WM; ++b) to[r][b] = load16_shared(sums, at + (r * WM + b) * 1024, z * Shape::kSums);
-                };
-                auto add = [&](const f32x4(&from)[WN][WM]) {
+                        for (int r = 0; r < WN; ++r)
 #pragma unroll
-                    for (int r = 0; r < WN; ++r)
+                            for (int b = 0; b < WM; ++b) other[z][r][b] = load16_shared(sums, at + (r * WM + b) * 1024, (z0 + z) * Shape::kSums);
+                    }
 #pragma unroll
-                        for (int b = 0; b < WM; ++b) sum[r][b] += from[r][b];
-                };
-                auto take = [&](int z, f32x4(&from)[WN][WM]) {
-                    if (z >= p.slices) return;
-                    if (z == it.slice) add(acc);
-                    else add(from);
-                    ask(z + 2, from);
-                };
-                ask(0, even);
-                ask(1, odd);
-                for (int z = 0; z < p.slices; z += 2) {
-                    take(z, even);
-                    take(z + 1, odd);
+                    for (int z = 0; z < kAtATime; ++z) {
+                        if (z0 + z >= p.slices) continue;
+#pragma unroll
+                        for (int r = 0; r < WN; ++r)
+#pragma unroll
+                            for (int b = 0; b < WM; ++b) sum[r][b] += z0 + z == it.slice ? acc[r][b] : other[z][r][b];
+                    }
                 }
 #pragma unroll
                 for (int r = 0; r < WN; ++r)
@@ -659,17 +681,17 @@ constexpr int64_t staged_bytes(int64_t rows, int64_t K) { return rows * (K + 16)
 int64_t most_pieces(const ProductParams& p, int rows) { return product::most_pieces(p.M, p.offsets ? p.experts : 0, rows); }
 
 template <int SRC, int XP, int MODE>
-hipError_t launch_stream(ProductParams p, int waves, hipStream_t s) {
+hipError_t launch_stream(ProductParams p, int waves, int runs, hipStream_t s) {
     p.place_rows = XP ? 0 : p.M < 16 ? p.M : 16;
-    const size_t lds = (size_t)waves * stream_place(MODE, XP) + staged_bytes(p.place_rows, p.K);
+    const size_t lds = (size_t)waves * (stream_place(MODE, XP) + stream_sums(MODE)) + staged_bytes(p.place_rows, p.K);
     // (a launch has fewer than 2^16 workgroups along y and 2^32 threads)
-    int64_t most = (int64_t(1) << 31) / (int64_t(p.NB) * waves * 64);
+    int64_t most = (int64_t(1) << 31) / (int64_t(runs) * waves * 64);
     most = most > 65535 ? 65535 : most;
     const int64_t slots = most_pieces(p, 16);
     hipError_t e = hipSuccess;
     for (int64_t at = 0; at < slots && e == hipSuccess; at += most) {
         p.slot0 = (int)at;
-        const dim3 grid(p.NB, (unsigned)(slots - at < most ? slots - at : most));
+        const dim3 grid(runs, (unsigned)(slots - at < most ? slots - at : most));
         auto run = [&](auto once) {
             constexpr bool ONCE = decltype(once)::value;
             return p.offsets ? launch<stream_kernel<SRC, XP, MODE, true, ONCE>>(grid, waves * 64, lds, p, s)
@@ -682,7 +704,7 @@ hipError_t launch_stream(ProductParams p, int waves, hipStream_t s) {
 
 // Output channels (kGated: of both projections) and rows of a tile, wavefronts, and steps of room, by shape.
 struct TileSize { int channels, rows, waves, room; };
-constexpr TileSize kTiles[] = {{256, 256, 8, 2}, {128, 128, 8, 4}, {128, 64, 8, 4}, {64, 64, 4, 4}};
+constexpr TileSize kTiles[] = {{256, 256, 8, 2}, {128, 128, 8, 4}, {128, 64, 8, 4}, {64, 64, 4, 4}, {256, 128, 8, 3}};
 
 template <int SHAPE, int WN, int WM, int GN, int GM, int DEPTH, int MODE, bool EXACT>
 hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
@@ -713,7 +735,7 @@ struct TileChoice { int shape, slices; };             // shape -1: streamed
 
 // `NB`: row blocks of weights, kGated: of both projections.
 TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool exact, int cus) {
-    const double S = (double)KT * (exact ? 1.6 : 1.0);
+    const double S = (double)KT * (exact ? 1.8 : 1.0);
     TileChoice best{-1, 1};
     auto tiles = [&](int64_t rb, int64_t rows) {
         const int64_t nx = (NB + rb - 1) / rb;
@@ -722,20 +744,21 @@ TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int 
         return (double)nx * (filled > some ? filled : some);
     };
     if (mode != kPowers && M <= 16 * (experts ? experts : 1)) return best;
-    double least = mode == kPowers ? 1e30 : 2.3 + tiles(1, 16) * (double)KT * 2048.0 / 6.6e6;
+    double least = mode == kPowers ? 1e30 : 4.0 + tiles(1, 16) * (double)KT * 2048.0 / 3.3e6;
     auto consider = [&](int shape, int slices, double us) {
         if (us < least) { least = us; best = {shape, slices}; }
     };
     auto rounds = [&](double t) { return (double)(int64_t)((t + cus - 1) / cus); };
     auto pairs = [&](double n, double one, double two) { return two * (double)(int64_t)(n / 2) + ((int64_t)n % 2 ? one : 0.0); };
-    const double t0 = tiles(16, 256), t1 = tiles(8, 128), t2 = tiles(8, 64), t3 = tiles(4, 64);
-    if (!exact) consider(0, 1, 6.0 + rounds(t0) * (1.75 * S + 4.5 * (t0 < cus ? t0 / cus : 1.0)));
+    const double t0 = tiles(16, 256), t1 = tiles(8, 128), t2 = tiles(8, 64), t3 = tiles(4, 64), t4 = tiles(16, 128);
+    if (!exact) consider(0, 1, 3.8 + rounds(t0) * (1.64 * S + 4.5 * (t0 < cus ? t0 / cus : 1.0)));
+    consider(4, 1, 2.8 + rounds(t4) * (0.95 * S + 1.5));
     for (int z = 1; z <= 8; ++z) {
         if (z > KT) break;
-        const double steps = (double)((int64_t)(S + z - 1) / z);
-        if (z == 1 || t1 * z <= cus) consider(1, z, 3.2 + rounds(t1 * z) * ((t1 > cus ? 0.72 : 0.63) * steps + 1.0) + (z > 1 ? 2.5 + 1.6 * z : 0.0));
-        if (z == 1 || t2 * z <= cus) consider(2, z, 3.2 + rounds(t2 * z) * (0.50 * steps + 0.7) + (z > 1 ? 3.0 + 0.8 * z : 0.0));
-        if (z == 1 || t3 * z <= 2 * cus) consider(3, z, 3.0 + pairs(rounds(t3 * z), 0.37 * steps + 0.9, 0.62 * steps + 0.9) + (z > 1 ? 1.8 + 1.0 * z : 0.0));
+        const double steps = z > 1 ? (double)((int64_t)((S + z - 1) / z)) : S;
+        if (z == 1 || t1 * z <= cus) consider(1, z, 2.7 + rounds(t1 * z) * (0.68 * steps + 1.1) + (z > 1 ? 4.0 + 0.65 * z : 0.0));
+        if (z == 1 || t2 * z <= cus) consider(2, z, 3.2 + rounds(t2 * z) * (0.467 * steps + 0.7) + (z > 1 ? 3.1 + 0.63 * z : 0.0));
+        if (z == 1 || t3 * z <= 2 * cus) consider(3, z, 2.5 + pairs(rounds(t3 * z), 0.325 * steps + 1.0, 0.555 * steps + 1.0) + (z > 1 ? 3.0 + 0.23 * z : 0.0));
     }
     if (best.slices > 1) {                             // as many as the workspace has room for
         const TileSize t = kTiles[best.shape];
@@ -753,6 +776,7 @@ struct Choice {
     // streamed:
     int pieces;                // of eight rows of X that come with them, 0: X is staged
     int waves;                 // per workgroup
+    int runs;                  // of row blocks, one per workgroup
 };
 
 // `experts`: 0 without.
@@ -761,28 +785,30 @@ Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool
     const int KQ = (int)((KT + 3) / 4);
     c.tiles = choose_tiles(M, NB, KT, experts, mode, exact, cus);
     const int64_t pieces = experts ? (M < experts ? M : experts) : (M + 15) / 16, mean = (M + pieces - 1) / pieces;
-    const int64_t groups = (mode == kGated ? NB / 2 : NB) * pieces, most_rows = M < 16 ? M : 16;
-    constexpr int64_t kStagedMost = 32 * 1024;
-    const bool staged = staged_bytes(most_rows, KT * 128) <= kStagedMost;
-    c.apart = !codes && (c.tiles.shape >= 0 || mean > 4 || !staged);
+    const int64_t blocks = mode == kGated ? NB / 2 : NB, most_rows = M < 16 ? M : 16, staged = staged_bytes(most_rows, KT * 128);
+    constexpr int64_t kLds = 160 * 1024, kStagedMost = 72 * 1024;
+    const bool stage = staged <= kStagedMost;
+    c.apart = !codes && (c.tiles.shape >= 0 || mean > 4 || !stage);
     c.once = c.tiles.shape < 0 && (experts ? mean <= 4 : M <= 16) && NB * (experts ? pieces : 1) * KT * 2048 > (int64_t(128) << 20);
-    c.pieces = (c.apart || codes) && !(staged && mean <= 4) ? (most_rows > 8 ? 2 : 1) : 0;
-    const int depth = stream_depth(mode), per_wave = stream_place(mode, c.pieces);
-    const int64_t room = 160 * 1024 - (c.pieces ? 0 : staged_bytes(most_rows, KT * 128));
-    int64_t waves = KT / depth < 1 ? 1 : KT / depth;
-    if (waves > 16) waves = 16;
-    if (waves > 8 && groups > 512) waves = 8;
-    while (waves > 1 && waves * per_wave > (groups > cus ? room / 2 : room)) --waves;
+    c.pieces = stage ? 0 : most_rows > 8 ? 2 : 1;
+    const int64_t per_wave = stream_place(mode, c.pieces) + stream_sums(mode), shared = c.pieces ? 0 : staged;
+    const int64_t most_waves = KT <= 32 && most_rows <= 8 ? 4 : 8;
+    int64_t waves = KT < most_waves ? KT : most_waves;
+    while (waves > 1 && waves * per_wave + shared > kLds) --waves;
+    int64_t at_once = kLds / (waves * per_wave + shared);                      // workgroups per compute unit
+    if (at_once > 32 / waves) at_once = 32 / waves;
+    const int64_t runs = (cus * at_once + pieces - 1) / pieces;
+    c.runs = (int)(runs < blocks ? runs : blocks);
     c.waves = (int)waves;
     return c;
 }
 
-template <int MODE> hipError_t launch_stream_of(int src, int pieces, const ProductParams& p, int waves, hipStream_t s) {
-    if (pieces == 1) return launch_stream<kF32, 1, MODE>(p, waves, s);
-    if (pieces == 2) return launch_stream<kF32, 2, MODE>(p, waves, s);
-    return src == kF32   ? launch_stream<kF32, 0, MODE>(p, waves, s)
-           : src == kF16 ? launch_stream<kF16, 0, MODE>(p, waves, s)
-                         : launch_stream<kBF16, 0, MODE>(p, waves, s);
+template <int MODE> hipError_t launch_stream_of(int src, const Choice& c, const ProductParams& p, hipStream_t s) {
+    if (c.pieces == 1) return launch_stream<kF32, 1, MODE>(p, c.waves, c.runs, s);
+    if (c.pieces == 2) return launch_stream<kF32, 2, MODE>(p, c.waves, c.runs, s);
+    return src == kF32   ? launch_stream<kF32, 0, MODE>(p, c.waves, c.runs, s)
+           : src == kF16 ? launch_stream<kF16, 0, MODE>(p, c.waves, c.runs, s)
+                         : launch_stream<kBF16, 0, MODE>(p, c.waves, c.runs, s);
 }
 
 template <int MODE, bool EXACT = false> hipError_t launch_of(const Choice& c, int src, const ProductParams& p, int cus, hipStream_t s) {
@@ -793,8 +819,9 @@ template <int MODE, bool EXACT = false> hipError_t launch_of(const Choice& c, in
         case 1: return launch_tiles<1, 4, 2, 2, 4, 4, MODE, EXACT>(p, cus, s);
         case 2: return launch_tiles<2, 2, 2, 4, 2, 4, MODE, EXACT>(p, cus, s);
         case 3: return launch_tiles<3, 2, 2, 2, 2, 4, MODE, EXACT>(p, cus, s);
+        case 4: return launch_tiles<4, 4, 4, 4, 2, 3, MODE, EXACT>(p, cus, s);
     }
-    if constexpr (MODE != kPowers) return launch_stream_of<MODE>(src, c.pieces, p, c.waves, s);
+    if constexpr (MODE != kPowers) return launch_stream_of<MODE>(src, c, p, s);
     return hipErrorInvalidValue;
 }
 
