@@ -133,9 +133,9 @@ __device__ __forceinline__ float sigma(float z) { return __builtin_amdgcn_rcpf(1
 __device__ __forceinline__ float argument(float g, int act) { return act == kSilu ? g : 1.5957691216057308f * (g + 0.044715f * g * g * g); }
 __device__ __forceinline__ float activated(float g, int act) { return g * sigma(argument(g, act)); }
 __device__ __forceinline__ void activated(float g, int act, float& f, float& slope) {
-    const float s = sigma(argument(g, act));
+    const float s = sigma(argument(g, act)), rest = 1.0f - s;
     f = g * s;
-    slope = s + f * (1.0f - s) * (act == kSilu ? 1.0f : 1.5957691216057308f * (1.0f + 0.134145f * g * g));
+    slope = act == kSilu ? s + f * rest : s + f * rest * (1.5957691216057308f * (1.0f + 0.134145f * g * g));
 }
 
 }  // namespace fp8

@@ -744,21 +744,31 @@ TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int 
         return (double)nx * (filled > some ? filled : some);
     };
     if (mode != kPowers && M <= 16 * (experts ? experts : 1)) return best;
-    double least = mode == kPowers ? 1e30 : 4.0 + tiles(1, 16) * (double)KT * 2048.0 / 3.3e6;
+    double least = mode == kPowers ? 1e30 : 4.2 + tiles(1, 16) * (double)KT * 2048.0 / 3.0e6;
     auto consider = [&](int shape, int slices, double us) {
         if (us < least) { least = us; best = {shape, slices}; }
     };
-    auto rounds = [&](double t) { return (double)(int64_t)((t + cus - 1) / cus); };
+    // Rounds of tiles: by expert, where they may be more or fewer than is estimated, on average; else rounded up, but for a part: the units that have
+    // a tile in an uneven last round have more of the memory and of the power to themselves.
+    auto rounds = [&](double t) {
+        const double exact_rounds = t / cus, up = (double)(int64_t)((t + cus - 1) / cus);
+        if (experts) return exact_rounds < 0.6 ? 1.0 : exact_rounds + 0.4;
+        return up < 2.0 ? up : 0.8 * up + 0.2 * exact_rounds;
+    };
     auto pairs = [&](double n, double one, double two) { return two * (double)(int64_t)(n / 2) + ((int64_t)n % 2 ? one : 0.0); };
     const double t0 = tiles(16, 256), t1 = tiles(8, 128), t2 = tiles(8, 64), t3 = tiles(4, 64), t4 = tiles(16, 128);
-    if (!exact) consider(0, 1, 3.8 + rounds(t0) * (1.64 * S + 4.5 * (t0 < cus ? t0 / cus : 1.0)));
-    consider(4, 1, 2.8 + rounds(t4) * (0.95 * S + 1.5));
+    if (!exact) consider(0, 1, 4.8 + rounds(t0) * (1.52 * S + 5.6 * (t0 < cus ? t0 / cus : 1.0)));
+    consider(4, 1, 2.8 + rounds(t4) * (0.88 * S + 2.9));
+    const double most = (experts ? 0.7 : 1.0) * cus;   // slices that run at once
     for (int z = 1; z <= 8; ++z) {
         if (z > KT) break;
         const double steps = z > 1 ? (double)((int64_t)((S + z - 1) / z)) : S;
-        if (z == 1 || t1 * z <= cus) consider(1, z, 2.7 + rounds(t1 * z) * (0.68 * steps + 1.1) + (z > 1 ? 4.0 + 0.65 * z : 0.0));
-        if (z == 1 || t2 * z <= cus) consider(2, z, 3.2 + rounds(t2 * z) * (0.467 * steps + 0.7) + (z > 1 ? 3.1 + 0.63 * z : 0.0));
-        if (z == 1 || t3 * z <= 2 * cus) consider(3, z, 2.5 + pairs(rounds(t3 * z), 0.325 * steps + 1.0, 0.555 * steps + 1.0) + (z > 1 ? 3.0 + 0.23 * z : 0.0));
+        if (z == 1 || t1 * z <= most) consider(1, z, 3.9 + rounds(t1 * z) * (0.57 * steps + 1.4) + (z > 1 ? 4.4 + 0.53 * z : 0.0));
+        if (z == 1 || t2 * z <= most) consider(2, z, 3.25 + rounds(t2 * z) * (0.428 * steps + 0.7) + (z > 1 ? 3.6 + 0.75 * z : 0.0));
+        if (z == 1 || t3 * z <= 2 * most) {
+            const double n = (double)(int64_t)((t3 * z + cus - 1) / cus);
+            consider(3, z, 2.25 + pairs(n, 0.374 * steps + 0.9, 0.673 * steps + 0.9) + (z > 1 ? 3.0 + 0.28 * z : 0.0));
+        }
     }
     if (best.slices > 1) {                             // as many as the workspace has room for
         const TileSize t = kTiles[best.shape];

@@ -2,7 +2,7 @@
 //
 // All are bound by memory traffic.  Sixteen lanes ("team") hold 128 columns, eight values each, so every load is 16 (fp32: 32)
 // consecutive bytes per lane and whole cache lines per wavefront.  Where a square of 128 x 128 is looked at as one (weights, columns,
-// gradients), a workgroup holds it in registers, an 8 x 8 block per lane: its rows' and columns' codes both leave from there.
+// gradients), a workgroup holds it in registers, a 4 x 8 block per lane: its rows' and columns' codes both leave from there.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -79,14 +79,13 @@ __global__ __launch_bounds__(kThreads) void quantize_rows(const QuantizeParams p
 }
 
 // ---------------------------------------------------------------------------------------------------- squares of 128 x 128
-// Lane 16 team + j of a workgroup of sixteen teams holds rows 8 team .. 8 team + 7, columns 8 j .. 8 j + 7 of the square.
-struct Block { float v[8][8]; };
+// Lane 16 team + j of a workgroup of 32 teams holds rows 4 team .. 4 team + 3, columns 8 j .. 8 j + 7 of the square.
+constexpr int kSquare = 512, kEach = 4;
+struct Block { float v[kEach][8]; };
 
-constexpr int kPitch = 128 + 16;                       // bytes of a column's codes in LDS
-
-template <int SRC> __device__ __forceinline__ void load_block(const void* x, int64_t row0, int64_t rows, int64_t K, int64_t column, Eight<SRC> (&raw)[8]) {
+template <int SRC> __device__ __forceinline__ void load_block(const void* x, int64_t row0, int64_t rows, int64_t K, int64_t column, Eight<SRC> (&raw)[kEach]) {
 #pragma unroll
-    for (int r = 0; r < 8; ++r) raw[r] = row0 + r < rows ? load_eight<SRC>(x, (row0 + r) * K + column) : no_values<SRC>();
+    for (int r = 0; r < kEach; ++r) raw[r] = row0 + r < rows ? load_eight<SRC>(x, (row0 + r) * K + column) : no_values<SRC>();
 }
 
 // 4 x 4 bytes: word r of `m` is a row, then a column.
@@ -99,23 +98,32 @@ __device__ __forceinline__ void transpose_four(uint32_t (&m)[4]) {
     m[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
+// The largest over the four teams of a wavefront.
+__device__ __forceinline__ uint32_t largest_of_teams(uint32_t a) {
+    const auto near = __builtin_amdgcn_permlane16_swap(a, a, false, false);
+    a = max(near[0], near[1]);
+    const auto far = __builtin_amdgcn_permlane32_swap(a, a, false, false);
+    return max(far[0], far[1]);
+}
+
 // The codes of the lane's rows to those of its columns, by way of LDS to memory: column c of the square at `to` + c * pitch, 128 bytes, of which those
-// of `bytes` rows are written (a multiple of sixteen).  All threads call it; `tile` is kPitch * 128 bytes, free before and after.
-__device__ __forceinline__ void store_columns(const u32x2 (&codes)[8], char* tile, char* to, int64_t pitch, int bytes) {
+// of `bytes` rows are written (a multiple of sixteen); `keep` is zero for columns of no codes.  All threads call it; `tile` is 16 KiB, free before and after.
+// Sixteen rows q of column c lie at 16 (q ^ ((c >> 3) & 7)): lanes that write, or read, together do not meet in a bank more than twice.
+__device__ __forceinline__ void store_columns(const u32x2 (&codes)[kEach], const uint32_t (&keep)[8], char* tile, char* to, int64_t pitch, int bytes) {
     const uint32_t j = threadIdx.x & 15u, team = threadIdx.x >> 4;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {                      // columns 4 h .. 4 h + 3
-        uint32_t low[4] = {codes[0][h], codes[1][h], codes[2][h], codes[3][h]}, high[4] = {codes[4][h], codes[5][h], codes[6][h], codes[7][h]};
-        transpose_four(low);
-        transpose_four(high);
+        uint32_t m[4] = {codes[0][h], codes[1][h], codes[2][h], codes[3][h]};
+        transpose_four(m);
 #pragma unroll
-        for (int c = 0; c < 4; ++c) *reinterpret_cast<u32x2*>(tile + (8 * j + 4 * h + c) * kPitch + 8 * team) = u32x2{low[c], high[c]};
+        for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<uint32_t*>(tile + (8 * j + 4 * h + c) * 128 + ((team >> 2) ^ (j & 7u)) * 16 + (team & 3u) * 4) = m[c] & keep[4 * h + c];
     }
     __syncthreads();
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int c = t * 32 + (int)(threadIdx.x >> 3), at = 16 * (int)(threadIdx.x & 7u);
-        if (at < bytes) *reinterpret_cast<u32x4*>(to + c * pitch + at) = *reinterpret_cast<const u32x4*>(tile + c * kPitch + at);
+    for (int t = 0; t < 2; ++t) {
+        const int c = t * 64 + (int)(threadIdx.x >> 3), q = (int)(threadIdx.x & 7u);
+        if (16 * q < bytes) *reinterpret_cast<u32x4*>(to + c * pitch + 16 * q) = *reinterpret_cast<const u32x4*>(tile + c * 128 + ((q ^ (c >> 3)) & 7) * 16);
     }
     __syncthreads();
 }
@@ -124,7 +132,7 @@ __device__ __forceinline__ void store_columns(const u32x2 (&codes)[8], char* til
 __device__ __forceinline__ void rows_out(const Block& b, int64_t row0, int64_t rows, char* codes, int64_t pitch, float* scales) {
     const uint32_t j = threadIdx.x & 15u;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
+    for (int r = 0; r < kEach; ++r) {
         const Scale s = scale_of(largest_of_sixteen(largest(b.v[r])));
         if (row0 + r >= rows) continue;
         *reinterpret_cast<u32x2*>(codes + (row0 + r) * pitch) = to_codes(b.v[r], s);
@@ -132,73 +140,81 @@ __device__ __forceinline__ void rows_out(const Block& b, int64_t row0, int64_t r
     }
 }
 
-// Codes of its columns: a power of two per column, and the codes as rows of the transposed matrix.  `most` is 16 * 128 words.
+// Codes of its columns: a power of two per column, and the codes as rows of the transposed matrix.  `most` is 8 * 128 words.
 __device__ __forceinline__ void columns_out(const Block& b, char* tile, uint32_t* most, char* to, int64_t pitch, float* scales) {
-    const uint32_t j = threadIdx.x & 15u, team = threadIdx.x >> 4;
+    const uint32_t j = threadIdx.x & 15u;
     uint32_t a[8];
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
         a[c] = 0;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) a[c] = max(a[c], magnitude(b.v[r][c]));
+        for (int r = 0; r < kEach; ++r) a[c] = max(a[c], magnitude(b.v[r][c]));
+        a[c] = largest_of_teams(a[c]);
     }
-    *reinterpret_cast<u32x4*>(most + team * 128 + 8 * j) = u32x4{a[0], a[1], a[2], a[3]};
-    *reinterpret_cast<u32x4*>(most + team * 128 + 8 * j + 4) = u32x4{a[4], a[5], a[6], a[7]};
+    if ((threadIdx.x & 48u) == 0) {
+        uint32_t* mine = most + (threadIdx.x >> 6) * 128 + 8 * j;
+        *reinterpret_cast<u32x4*>(mine) = u32x4{a[0], a[1], a[2], a[3]};
+        *reinterpret_cast<u32x4*>(mine + 4) = u32x4{a[4], a[5], a[6], a[7]};
+    }
     __syncthreads();
     if (threadIdx.x < 128) {
         uint32_t all = 0;
 #pragma unroll
-        for (int t = 0; t < 16; ++t) all = max(all, most[t * 128 + threadIdx.x]);
+        for (int t = 0; t < kSquare / 64; ++t) all = max(all, most[t * 128 + threadIdx.x]);
         most[threadIdx.x] = all;                       // (this thread alone reads its column)
         scales[threadIdx.x] = power_of_two_scale_of(all).scale;
     }
     __syncthreads();
-    Scale s[8];
+    float inverse[8];
+    uint32_t keep[8];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) s[c] = power_of_two_scale_of(most[8 * j + c]);
-    u32x2 codes[8];
+    for (int c = 0; c < 8; ++c) {
+        const Scale s = power_of_two_scale_of(most[8 * j + c]);
+        inverse[c] = s.inverse;
+        keep[c] = s.bad ? 0u : 0xffffffffu;
+    }
+    u32x2 codes[kEach];
 #pragma unroll
-    for (int r = 0; r < 8; ++r)
+    for (int r = 0; r < kEach; ++r)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            float u[4];
-#pragma unroll
-            for (int c = 0; c < 4; ++c) u[c] = s[4 * h + c].bad ? 0.0f : b.v[r][4 * h + c] * s[4 * h + c].inverse;
-            int w = __builtin_amdgcn_cvt_pk_fp8_f32(u[0], u[1], 0, false);
-            codes[r][h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(u[2], u[3], w, true);
+            const float* v = b.v[r] + 4 * h;
+            int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0] * inverse[4 * h], v[1] * inverse[4 * h + 1], 0, false);
+            codes[r][h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2] * inverse[4 * h + 2], v[3] * inverse[4 * h + 3], w, true);
         }
-    store_columns(codes, tile, to, pitch, 128);
+    store_columns(codes, keep, tile, to, pitch, 128);
 }
 
 template <int SRC>
-__global__ __launch_bounds__(kThreads) void quantize_weights(const QuantizeParams p) {
-    __shared__ __align__(16) char tile[kPitch * 128];
-    __shared__ uint32_t most[4];
+__global__ __launch_bounds__(kSquare) void quantize_weights(const QuantizeParams p) {
+    __shared__ __align__(16) char tile[16 * 1024];
+    __shared__ uint32_t most[kSquare / 64];
     const uint32_t j = threadIdx.x & 15u, team = threadIdx.x >> 4;
     const uint32_t id = p.block0 + (uint32_t)blockIdx.x, nb = (uint32_t)(((uint64_t)id * p.magic) >> p.shift), kb = id - nb * p.groups;
-    const int64_t row0 = (int64_t)nb * 128 + 8 * team, column = (int64_t)kb * 128 + 8 * j;
-    Eight<SRC> raw[8];
+    const int64_t row0 = (int64_t)nb * 128 + kEach * team, column = (int64_t)kb * 128 + 8 * j;
+    Eight<SRC> raw[kEach];
     load_block<SRC>(p.x, row0, p.M, p.K, column, raw);
     uint32_t a = 0;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
+    for (int r = 0; r < kEach; ++r) {
         float v[8];
         to_floats<SRC>(raw[r], v);
         a = max(a, largest(v));
     }
-    a = largest_of_sixteen(a);
-    a = max(a, (uint32_t)__shfl_xor((int)a, 16));
-    a = max(a, (uint32_t)__shfl_xor((int)a, 32));
+    a = largest_of_teams(largest_of_sixteen(a));
     if ((threadIdx.x & 63u) == 0) most[threadIdx.x >> 6] = a;
     __syncthreads();
-    const Scale s = scale_of(max(max(most[0], most[1]), max(most[2], most[3])));
+    a = 0;
+#pragma unroll
+    for (int t = 0; t < kSquare / 64; ++t) a = max(a, most[t]);
+    const Scale s = scale_of(a);
     if (threadIdx.x == 0) {
         p.scales[(int64_t)nb * p.ku + kb] = s.scale;
         if (p.transposed) p.transposed_scales[(int64_t)kb * ((p.M + 127) >> 7) + nb] = s.scale;
     }
-    u32x2 codes[8];
+    u32x2 codes[kEach];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
+    for (int r = 0; r < kEach; ++r) {
         float v[8];
         to_floats<SRC>(raw[r], v);
         codes[r] = to_codes(v, s);
@@ -206,21 +222,22 @@ __global__ __launch_bounds__(kThreads) void quantize_weights(const QuantizeParam
     }
     if (p.transposed) {
         const int64_t left = p.M - (int64_t)nb * 128;
-        store_columns(codes, tile, p.transposed + (int64_t)kb * 128 * p.M + (int64_t)nb * 128, p.M, left < 128 ? (int)left : 128);
+        const uint32_t all[8] = {~0u, ~0u, ~0u, ~0u, ~0u, ~0u, ~0u, ~0u};
+        store_columns(codes, all, tile, p.transposed + (int64_t)kb * 128 * p.M + (int64_t)nb * 128, p.M, left < 128 ? (int)left : 128);
     }
 }
 
 template <int SRC>
-__global__ __launch_bounds__(kThreads) void quantize_columns(const QuantizeParams p) {
-    __shared__ __align__(16) char tile[kPitch * 128];
-    __shared__ __align__(16) uint32_t most[16 * 128];
+__global__ __launch_bounds__(kSquare) void quantize_columns(const QuantizeParams p) {
+    __shared__ __align__(16) char tile[16 * 1024];
+    __shared__ __align__(16) uint32_t most[8 * 128];
     const uint32_t j = threadIdx.x & 15u, team = threadIdx.x >> 4;
     const uint32_t id = p.block0 + (uint32_t)blockIdx.x, mb = (uint32_t)(((uint64_t)id * p.magic) >> p.shift), kb = id - mb * p.groups;
-    Eight<SRC> raw[8];
-    load_block<SRC>(p.x, (int64_t)mb * 128 + 8 * team, p.M, p.K, (int64_t)kb * 128 + 8 * j, raw);
+    Eight<SRC> raw[kEach];
+    load_block<SRC>(p.x, (int64_t)mb * 128 + kEach * team, p.M, p.K, (int64_t)kb * 128 + 8 * j, raw);
     Block b;
 #pragma unroll
-    for (int r = 0; r < 8; ++r) to_floats<SRC>(raw[r], b.v[r]);
+    for (int r = 0; r < kEach; ++r) to_floats<SRC>(raw[r], b.v[r]);
     columns_out(b, tile, most, p.codes + (int64_t)kb * 128 * p.padded + (int64_t)mb * 128, p.padded, p.scales + (int64_t)mb * p.K + (int64_t)kb * 128);
 }
 
@@ -238,46 +255,52 @@ struct GradParams {
     uint32_t groups, magic, shift, block0;
 };
 
-// dU = dH act(G), dG = dH U act'(G), of a square of 128 x 128 of H: both are computed from the same registers, one after the other.
+// dU = dH act(G), dG = dH U act'(G), of a square of 128 x 128 of H, in every form that is asked for from the same registers: 6 bytes a value are
+// read, 2 written for the codes of rows and 2 for those of columns.
 template <int SRC>
-__global__ __launch_bounds__(kThreads) void gated_grad(const GradParams p) {
-    __shared__ __align__(16) char tile[kPitch * 128];
-    __shared__ __align__(16) uint32_t most[16 * 128];
+__global__ __launch_bounds__(kSquare, 4) void gated_grad(const GradParams p) {
+    __shared__ __align__(16) char tile[16 * 1024];
+    __shared__ __align__(16) uint32_t most[8 * 128];
     const uint32_t j = threadIdx.x & 15u, team = threadIdx.x >> 4;
     const uint32_t id = p.block0 + (uint32_t)blockIdx.x, mb = (uint32_t)(((uint64_t)id * p.magic) >> p.shift), fb = id - mb * p.groups;
-    const int64_t row0 = (int64_t)mb * 128 + 8 * team, column = (int64_t)fb * 128 + 8 * j;
-    Eight<SRC> dh[8], g[8], u[8];
+    const int64_t row0 = (int64_t)mb * 128 + kEach * team, column = (int64_t)fb * 128 + 8 * j;
+    Eight<SRC> dh[kEach], g[kEach], u[kEach];
     load_block<SRC>(p.dh, row0, p.M, p.F, column, dh);
     load_block<SRC>(p.saved, row0, p.M, 2 * p.F, column, g);
     load_block<SRC>(p.saved, row0, p.M, 2 * p.F, p.F + column, u);
-#pragma unroll 1
-    for (int which = 0; which < 2; ++which) {
-        const int64_t at = which * p.F;                // of the 2 F columns
-        Block b;
+    Block dg, du;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            float a[8], x[8], y[8];
-            to_floats<SRC>(dh[r], a);
-            to_floats<SRC>(g[r], x);
-            to_floats<SRC>(u[r], y);
+    for (int r = 0; r < kEach; ++r) {                  // (rows that do not exist are zeros, and so are their gradients)
+        float a[8], x[8], y[8];
+        to_floats<SRC>(dh[r], a);
+        to_floats<SRC>(g[r], x);
+        to_floats<SRC>(u[r], y);
 #pragma unroll
-            for (int c = 0; c < 8; ++c) {
-                float f, slope;
-                activated(x[c], p.act, f, slope);
-                b.v[r][c] = row0 + r < p.M ? a[c] * (which == 0 ? y[c] * slope : f) : 0.0f;
-            }
-            if (p.dense && row0 + r < p.M) {
-                u32x4 out;
+        for (int c = 0; c < 8; ++c) {
+            float f, slope;
+            activated(x[c], p.act, f, slope);
+            dg.v[r][c] = a[c] * (y[c] * slope);
+            du.v[r][c] = a[c] * f;
+        }
+    }
+    auto out = [&](const Block& b, int64_t at) {       // `at`: of the 2 F columns the first of these
+        if (p.dense) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) out[c] = round_pair(b.v[r][2 * c], b.v[r][2 * c + 1], p.bf16);
-                *reinterpret_cast<u32x4*>(p.dense + ((row0 + r) * 2 * p.F + at + column) * 2) = out;
+            for (int r = 0; r < kEach; ++r) {
+                if (row0 + r >= p.M) continue;
+                u32x4 w;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) w[c] = round_pair(b.v[r][2 * c], b.v[r][2 * c + 1], p.bf16);
+                *reinterpret_cast<u32x4*>(p.dense + ((row0 + r) * 2 * p.F + at + column) * 2) = w;
             }
         }
         if (p.codes) rows_out(b, row0, p.M, p.codes + at + column, 2 * p.F, p.scales + (at / 128 + fb) * p.M);
         if (p.columns)
             columns_out(b, tile, most, p.columns + (at + (int64_t)fb * 128) * p.padded + (int64_t)mb * 128, p.padded,
                         p.column_scales + (int64_t)mb * 2 * p.F + at + (int64_t)fb * 128);
-    }
+    };
+    out(dg, 0);
+    out(du, p.F);
 }
 
 // ---------------------------------------------------------------------------------------------------- back
@@ -328,7 +351,7 @@ void division(uint32_t d, uint32_t* magic, uint32_t* shift) {
 
 // A launch has fewer than 2^32 threads, which the largest matrices reach.
 template <typename P, typename F> void in_launches(P p, int64_t blocks, F launch) {
-    constexpr int64_t kMost = (int64_t(1) << 32) / kThreads - 1;
+    constexpr int64_t kMost = (int64_t(1) << 32) / kSquare - 1;
     for (int64_t at = 0; at < blocks; at += kMost) {
         p.block0 = (uint32_t)at;
         launch(p, (uint32_t)(blocks - at < kMost ? blocks - at : kMost));
@@ -400,9 +423,9 @@ extern "C" lutq_status lutq_fp8_quantize_weights(const void* W, int w_is_f32, lu
     division(p.groups, &p.magic, &p.shift);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     in_launches(p, (N + 127) / 128 * p.groups, [&](const QuantizeParams& q, uint32_t grid) {
-        if (w_is_f32) quantize_weights<kF32><<<grid, kThreads, 0, s>>>(q);
-        else if (dtype == LUTQ_F16) quantize_weights<kF16><<<grid, kThreads, 0, s>>>(q);
-        else quantize_weights<kBF16><<<grid, kThreads, 0, s>>>(q);
+        if (w_is_f32) quantize_weights<kF32><<<grid, kSquare, 0, s>>>(q);
+        else if (dtype == LUTQ_F16) quantize_weights<kF16><<<grid, kSquare, 0, s>>>(q);
+        else quantize_weights<kBF16><<<grid, kSquare, 0, s>>>(q);
     });
     return launched();
 }
@@ -419,9 +442,9 @@ extern "C" lutq_status lutq_fp8_quantize_columns(const void* X, int x_is_f32, lu
     division(p.groups, &p.magic, &p.shift);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     in_launches(p, p.padded / 128 * p.groups, [&](const QuantizeParams& q, uint32_t grid) {
-        if (x_is_f32) quantize_columns<kF32><<<grid, kThreads, 0, s>>>(q);
-        else if (dtype == LUTQ_F16) quantize_columns<kF16><<<grid, kThreads, 0, s>>>(q);
-        else quantize_columns<kBF16><<<grid, kThreads, 0, s>>>(q);
+        if (x_is_f32) quantize_columns<kF32><<<grid, kSquare, 0, s>>>(q);
+        else if (dtype == LUTQ_F16) quantize_columns<kF16><<<grid, kSquare, 0, s>>>(q);
+        else quantize_columns<kBF16><<<grid, kSquare, 0, s>>>(q);
     });
     return launched();
 }
@@ -476,8 +499,8 @@ extern "C" lutq_status lutq_fp8_gated_grad(const void* dH, const void* saved, in
     division(p.groups, &p.magic, &p.shift);
     const hipStream_t s = static_cast<hipStream_t>(stream);
     in_launches(p, p.padded / 128 * p.groups, [&](const GradParams& q, uint32_t grid) {
-        if (dtype == LUTQ_F16) gated_grad<kF16><<<grid, kThreads, 0, s>>>(q);
-        else gated_grad<kBF16><<<grid, kThreads, 0, s>>>(q);
+        if (dtype == LUTQ_F16) gated_grad<kF16><<<grid, kSquare, 0, s>>>(q);
+        else gated_grad<kBF16><<<grid, kSquare, 0, s>>>(q);
     });
     return launched();
 }
