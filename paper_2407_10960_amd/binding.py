@@ -1114,13 +1114,26 @@ TRACE_STAMPS = ("start", "arguments arrived", "first loads issued", "table built
                 "K loop done", "waves reduced", "outputs stored")
 
 
-def calib_fp8_launch(M: int, N: int, K: int, experts: int = 0, form: str = "matmul", codes: bool = False, compute_units: int = 256) -> Mx4Launch:
+@dataclass(frozen=True)
+class Fp8Launch:
+    """How an 8-bit product is launched (include/lutq_calib.h)."""
+    quantised_first: bool
+    channels: int              # of both projections
+    rows: int
+    waves: int
+    room: int                  # steps of K in LDS
+    slices: int
+    streamed: int              # 0: tiles; 1: with X staged in LDS; 2, 3: with one or two pieces of eight rows of X at a time
+    past_caches: bool
+
+
+def calib_fp8_launch(M: int, N: int, K: int, experts: int = 0, form: str = "matmul", codes: bool = False, compute_units: int = 256) -> Fp8Launch:
     """How the library launches lutq_fp8_matmul (form "matmul"), lutq_fp8_gated ("gated", N is F, "gated_saved"; with experts the ones by expert), or
     lutq_fp8_weight_grad ("weight_grad"; its N, K, M as M, N, K)."""
     out = (ctypes.c_int * 8)()
     _check(load_library().lutq_calib_fp8_launch(M, N, K, experts, ("matmul", "gated", "weight_grad", "gated_saved").index(form), int(codes), compute_units, out),
            "lutq_calib_fp8_launch")
-    return Mx4Launch(bool(out[0]), *out[1:7], bool(out[7]))
+    return Fp8Launch(bool(out[0]), *out[1:7], bool(out[7]))
 
 
 def calib_matmul_trace(X, packed, scales, lut, bits: int, group_size: int, Y, workspace, trace, stream=None,

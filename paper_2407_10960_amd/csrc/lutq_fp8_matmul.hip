@@ -792,7 +792,6 @@ struct Choice {
 // `experts`: 0 without.
 Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool exact, bool codes, int cus) {
     Choice c{};
-    const int KQ = (int)((KT + 3) / 4);
     c.tiles = choose_tiles(M, NB, KT, experts, mode, exact, cus);
     const int64_t pieces = experts ? (M < experts ? M : experts) : (M + 15) / 16, mean = (M + pieces - 1) / pieces;
     const int64_t blocks = mode == kGated ? NB / 2 : NB, most_rows = M < 16 ? M : 16, staged = staged_bytes(most_rows, KT * 128);
