@@ -102,24 +102,27 @@ __device__ __forceinline__ f32x4 scaled_product(const i32x8& w, const i32x8& x, 
 // is cut off, 2^-18 of the sum of magnitudes on random codes.  The 16-bit instruction does not (2^-30), at half the rate: the same sums of
 // the codes as 16-bit numbers, which hold them exactly.
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-struct Wide { f16x8 v[4]; };
+struct Wide { u32x4 v[4]; };
+// Pair `n` of the sixteen that a lane's 32 codes make, into its place.
+__device__ __forceinline__ void widen_pair(Wide& to, const i32x8& c, int n) {
+    const uint32_t four = (uint32_t)c[n >> 1];
+    const f16x2 h = n & 1 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(four, 1.0f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(four, 1.0f, false);
+    to.v[n >> 2][n & 3] = __builtin_bit_cast(uint32_t, h);
+}
 __device__ __forceinline__ Wide widen(const i32x8& c) {
     Wide r;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        f16x2 h[4];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            h[2 * j] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)c[2 * q + j], 1.0f, false);
-            h[2 * j + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((uint32_t)c[2 * q + j], 1.0f, true);
-        }
-        r.v[q] = f16x8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
-    }
+    for (int n = 0; n < 16; ++n) widen_pair(r, c, n);
     return r;
+}
+// Quarter q of the product: 32 of the columns.
+__device__ __forceinline__ f32x4 product(const Wide& w, const Wide& x, const f32x4& acc, int q) {
+    const u32x4 a = w.v[q], b = x.v[q];
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), acc, 0, 0, 0);
 }
 __device__ __forceinline__ f32x4 product(const Wide& w, const Wide& x, f32x4 acc) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(w.v[q], x.v[q], acc, 0, 0, 0);
+    for (int q = 0; q < 4; ++q) acc = product(w, x, acc, q);
     return acc;
 }
 __device__ __forceinline__ i32x8 operand(u32x4 a, u32x4 b) {

@@ -318,7 +318,13 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
     constexpr int kLoads = kWLoads + kXLoads + kScaleLoads;
     constexpr int kRing = WN < 4 ? WN : 4;             // row blocks of weights in registers
     constexpr int kTurn = WN - kRing + 1;              // the row block at which the next step is looked at
+    // Row blocks of the next step between whose products the last copies are asked for.  With all copies asked for before that, closer together,
+    // they keep the reads of LDS waiting: 4096 x 4096 x 28672 takes 436 us instead of 395, 8192 x 8192 x 8192 522 instead of 510.  (Weight
+    // gradients, whose steps are shorter, take 400 instead of 411 so.)
+    constexpr int kLate = WN == 8 && MODE != kPowers ? 2 : WN == 4 && WM == 4 ? 1 : 0;
+    static_assert(kLate <= kTurn, "asked for before the next turn");
     constexpr int kXRing = EXACT && WM > 2 ? 2 : WM;   // of X (EXACT: until it is widened)
+    constexpr bool kSpread = EXACT && kRing == 4 && WM == 4;                   // widened between the instructions: 900 us instead of 935 (4096 x 28672 x 4096)
     constexpr int kDelay = EXACT ? 1 : kWaves * WN * WM >= 256 ? 1 : 2;
     static_assert(kWLoads * kWaves == 2 * kRB && kXLoads * kWaves == 2 * kMB && kMB % 4 == 0 && kRB % 4 == 0, "whole loads per wavefront");
     static_assert(MODE != kGated || kWLoads % 2 == 0, "as many of either projection");
@@ -490,7 +496,30 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         for (int j = 0; j < 4; ++j) sum[j] = __builtin_fmaf(pending[at][j], pending_scale[at], sum[j]);
         asm volatile("" : "+v"(sum)::"memory");
     };
-    Wide wide[EXACT ? WM : 1];
+    Wide wide[EXACT ? WM : 1], wide_w[kSpread ? 2 : 1];
+    // kSpread: one product, and between its four instructions the additions of the one before, a quarter of the next row block, and in turn the next
+    // step's X.
+    auto spread_product = [&](int r, int b) {
+        f32x4 sums = {0.f, 0.f, 0.f, 0.f};
+        f32x4& before = acc[(r * WM + b + kProducts - 1) % kProducts / WM][(r * WM + b + kProducts - 1) % WM];
+        const int wide_x = r == WN - 1 && b > 0 ? b - 1 : r == 0 && b == 0 ? WM - 1 : -1;       // of X, widened here
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            sums = product(wide_w[r & 1], wide[b], sums, q);
+            asm volatile("" : "+v"(sums)::"memory");
+            float sum = __builtin_fmaf(pending[0][q], pending_scale[0], before[q]);
+            asm volatile("" : "+v"(sum)::"memory");
+            before[q] = sum;
+            widen_pair(wide_w[(r + 1) & 1], w[(r + 1) % kRing], 4 * b + q);
+            asm volatile("" : "+v"(wide_w[(r + 1) & 1].v[b])::"memory");
+            if (wide_x >= 0) {
+#pragma unroll
+                for (int n = 0; n < 4; ++n) widen_pair(wide[wide_x], x[wide_x % kXRing], 4 * q + n);
+                asm volatile("" : "+v"(wide[wide_x].v[q])::"memory");
+            }
+        }
+        return sums;
+    };
     auto one_step = [&](bool stored) {
         float s[MODE == kGated ? 2 : 1][WM];
         uint32_t xe[WM];
@@ -509,7 +538,8 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
                 next();
                 here = (here + 1) % DEPTH;
                 // The next step is there, and nobody needs this one's place any more.
-                constexpr int kStores = MODE == kGated ? 0 : WN / 2 * WM;
+                // (A tile's stores may be under way as well, where the copies that are waited for were asked for before them.)
+                constexpr int kStores = MODE == kGated || (DEPTH == 2 && kLate > 0) ? 0 : WN / 2 * WM;
                 if (stored) arrive<(DEPTH - 2) * kLoads + kStores>();
                 else arrive<(DEPTH - 2) * kLoads>();
                 __builtin_amdgcn_sched_barrier(0);
@@ -521,24 +551,34 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
 #pragma unroll
                 for (int j = at * kLoads / places; j < (at + 1) * kLoads / places; ++j) load_part(j);
             };
-            Wide wide_w;
-            if constexpr (EXACT) wide_w = widen(w[r % kRing]);
+            if constexpr (EXACT && !kSpread) wide_w[0] = widen(w[r % kRing]);
+            if constexpr (kSpread) {
+                if (r == WN - 2) {
+                    read_x(here, 0);
+                    read_x(here, 1);
+                }
+            }
 #pragma unroll
             for (int b = 0; b < WM; ++b) {
                 const int n = r * WM + b;
                 if constexpr (MODE == kPowers) {
                     acc[r][b] = scaled_product(w[r % kRing], x[b], acc[r][b], we[r % kRing], xe[b]);
                     asm volatile("" : "+v"(acc[r][b])::"memory");
+                } else if constexpr (kSpread) {
+                    const f32x4 sums = spread_product(r, b);
+                    pending[0] = sums;
+                    pending_scale[0] = s[MODE == kGated && r >= WN / 2][b];
                 } else {
                     f32x4 sums = {0.f, 0.f, 0.f, 0.f};
-                    if constexpr (EXACT) sums = product(wide_w, wide[b], sums);
+                    if constexpr (EXACT) sums = product(wide_w[0], wide[b], sums);
                     else sums = product(w[r % kRing], x[b], sums);
                     asm volatile("" : "+v"(sums)::"memory");
                     retire(n - kDelay);
                     pending[n % kDelay] = sums;
                     pending_scale[n % kDelay] = s[MODE == kGated && r >= WN / 2][b];
                 }
-                if (r == WN - 1) {
+                if (kSpread && r == WN - 1 && (b == 1 || b == 2)) read_x(here, b + 1);
+                if (!kSpread && r == WN - 1) {
                     read_x(here, b);
                     if constexpr (EXACT) {
                         if (b > 0) wide[b - 1] = widen(x[(b - 1) % kXRing]);
@@ -546,7 +586,8 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
                     }
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if (r >= kTurn) copies(n - kTurn * WM, (WN - kTurn) * WM);
+                if (r >= kTurn) copies(n - kTurn * WM, (WN - kTurn + kLate) * WM);
+                else if (r < kLate) copies((WN - kTurn + r) * WM + b, (WN - kTurn + kLate) * WM);
             }
         }
     };
@@ -571,6 +612,7 @@ __global__ __launch_bounds__(GN * GM * 64, 2) void tile_kernel(const ProductPara
         read_x(0, b);
         if constexpr (EXACT) wide[b] = widen(x[b % kXRing]);
     }
+    if constexpr (kSpread) wide_w[0] = widen(w[0]);
     read_scales(0);
 
     bool stored = false;
