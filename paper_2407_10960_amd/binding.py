@@ -1123,7 +1123,7 @@ class Fp8Launch:
     waves: int
     room: int                  # steps of K in LDS
     slices: int
-    streamed: int              # 0: tiles; 1: with X staged in LDS; 2, 3: with one or two pieces of eight rows of X at a time
+    streamed: int              # 0: tiles; 1: with X quantised into LDS; 2, 3: with one or two pieces of eight rows of X at a time
     past_caches: bool
 
 

@@ -74,8 +74,8 @@ __device__ __forceinline__ void store_four(char* to, const f32x4& sum, int bf16)
 // its wavefronts have a part of K each, and their sums are added in LDS in the order of the wavefronts.  Bound by the reads of the weights: they
 // are copied from memory to LDS in whole cache lines, DEPTH blocks of 128 columns ahead, without passing through registers, and
 // from one row block to the next without a pause.
-// X is staged, all of it by all wavefronts before the first product (SRC 1, 2: quantised by sixteen lanes per block); or (XP > 0), where that would take
-// too much LDS, its codes come block by block with the weights, XP pieces of eight rows.
+// X of 16 bits (SRC 1, 2) is quantised into LDS by all wavefronts before the first product, sixteen lanes per block; codes come block by block with the
+// weights, XP pieces of eight rows.
 // The sums of the codes are exact (Wide): the 16-bit instruction's half rate is far above what the reads leave to do.
 constexpr int kAhead = 8;                              // blocks of X per sixteen lanes that are asked for at a time
 
@@ -99,7 +99,7 @@ template <int SRC, int XP, int MODE, bool GROUPED, bool ONCE>
 __global__ __launch_bounds__(1024) void stream_kernel(const ProductParams p) {
     constexpr int R = MODE == kGated ? 2 : 1, DEPTH = stream_depth(MODE);
     static_assert(DEPTH <= 4, "as wait_blocks knows");
-    static_assert(SRC == kF32 || XP == 0, "16-bit values are staged");
+    static_assert((SRC == kF32) == (XP > 0), "codes come in pieces");
     constexpr int kSlot = R * 2048 + XP * 1024 + (XP ? 256 : 0), kCopies = 2 * R + (XP ? XP + 1 : 0);
     extern __shared__ __align__(1024) char smem[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -127,41 +127,25 @@ __global__ __launch_bounds__(1024) void stream_kernel(const ProductParams p) {
     const int pitch = p.K + 16;                        // (rows sixteen bytes apart: no two in the same banks)
     float* const staged_scales = reinterpret_cast<float*>(staged + p.place_rows * pitch);              // [block][row]
 
-    // What is staged: unit u is block u / rows of row u % rows.
+    // Unit u of what is quantised is block u / rows of row u % rows.
     const int units = XP ? 0 : rows * p.KT, teams = (int)blockDim.x >> 4, team = (int)threadIdx.x >> 4;
-    Eight<SRC == kF32 ? kF16 : SRC> ahead[kAhead];
-    u32x2 ahead_codes[kAhead];
-    float ahead_scale[kAhead];
+    Eight<XP ? kF16 : SRC> ahead[XP ? 1 : kAhead];
     auto ask = [&](int u, int t) {
         if (u >= units) return;
         const int kb = quotient_of_lane(u, rows), row = m0 + u - kb * rows;
-        const int64_t at = (int64_t)row * p.K + kb * 128 + 8 * i;
-        if constexpr (SRC == kF32) {
-            ahead_codes[t] = *reinterpret_cast<const u32x2*>(p.x + at);
-            ahead_scale[t] = p.xs[(int64_t)kb * p.M + row];
-        } else {
-            ahead[t].v[0] = *reinterpret_cast<const u32x4*>(p.x + at * 2);
-        }
+        ahead[t].v[0] = *reinterpret_cast<const u32x4*>(p.x + ((int64_t)row * p.K + kb * 128 + 8 * i) * 2);
     };
     auto stage = [&](int u, int t) {
         if (u >= units) return;
         const int kb = quotient_of_lane(u, rows), row = u - kb * rows;
-        float scale;
-        u32x2 codes;
-        if constexpr (SRC == kF32) {
-            codes = ahead_codes[t];
-            scale = ahead_scale[t];
-        } else {
-            float v[8];
-            to_floats<SRC>(ahead[t], v);
-            const Scale s = scale_of(largest_of_sixteen(largest(v)));
-            codes = to_codes(v, s);
-            scale = s.scale;
-        }
+        float v[8];
+        to_floats<XP ? kF16 : SRC>(ahead[t], v);
+        const Scale s = scale_of(largest_of_sixteen(largest(v)));
+        const u32x2 codes = to_codes(v, s);
         // (written so, as the compiler would have every copy to LDS that is under way arrive before it lets anything else write there)
         const uint32_t to = lds_offset(staged + row * pitch + kb * 128 + 8 * i), scale_to = lds_offset(staged_scales + kb * rows + row);
         asm volatile("ds_write_b64 %0, %1" ::"v"(to), "v"(codes) : "memory");
-        if (i == 0) asm volatile("ds_write_b32 %0, %1" ::"v"(scale_to), "v"(scale) : "memory");
+        if (i == 0) asm volatile("ds_write_b32 %0, %1" ::"v"(scale_to), "v"(s.scale) : "memory");
     };
     if constexpr (XP == 0) {
 #pragma unroll
@@ -826,7 +810,7 @@ struct Choice {
     bool apart;                // X of 16 bits is quantised by a launch of its own
     bool once;                 // weights past the caches
     // streamed:
-    int pieces;                // of eight rows of X that come with them, 0: X is staged
+    int pieces;                // of eight rows of X that come with them, 0: X is quantised into LDS
     int waves;                 // per workgroup
     int runs;                  // of row blocks, one per workgroup
 };
@@ -837,13 +821,21 @@ Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool
     c.tiles = choose_tiles(M, NB, KT, experts, mode, exact, cus);
     const int64_t pieces = experts ? (M < experts ? M : experts) : (M + 15) / 16, mean = (M + pieces - 1) / pieces;
     const int64_t blocks = mode == kGated ? NB / 2 : NB, most_rows = M < 16 ? M : 16, staged = staged_bytes(most_rows, KT * 128);
-    constexpr int64_t kLds = 160 * 1024, kStagedMost = 72 * 1024;
-    const bool stage = staged <= kStagedMost;
-    c.apart = !codes && (c.tiles.shape >= 0 || mean > 4 || !stage);
-    c.once = c.tiles.shape < 0 && (experts ? mean <= 4 : M <= 16) && NB * (experts ? pieces : 1) * KT * 2048 > (int64_t(128) << 20);
-    c.pieces = stage ? 0 : most_rows > 8 ? 2 : 1;
+    constexpr int64_t kLds = 160 * 1024, kStagedMost = 72 * 1024, kStagedFew = 20 * 1024;
+    // Values of up to four rows, or of up to 20 KiB of codes, are quantised by every workgroup for itself, at the cost of LDS for fewer wavefronts; others
+    // once, by a launch of some 2 us.  (7 rows of 640, 336 channels: 0.77 of the time; 13 of 896, 10896 channels 0.92; against 13 of 8960: 1.2 times; by
+    // expert with up to four rows on average 0.75 .. 1.2.)  Codes come with the weights: 16 rows of 640, 752 channels 4.3 us, in LDS 5.2.
+    const bool into_lds = !codes && c.tiles.shape < 0 && (mean <= 4 || most_rows * KT * 128 <= kStagedFew) && staged <= kStagedMost;
+    c.apart = !codes && !into_lds;
+    // Past the caches from 40 MiB on, for matrices of which one follows the other: 2 rows, 20224 x 4352, 20.5 us, past them 17.7; below 30 MiB they do
+    // not gain (1536 channels of 9856: 12.0 us and 14.1).
+    c.once = c.tiles.shape < 0 && (experts ? mean <= 16 : M <= 16) && NB * (experts ? pieces : 1) * KT * 2048 > (int64_t(40) << 20);
+    c.pieces = into_lds ? 0 : most_rows > 8 ? 2 : 1;
     const int64_t per_wave = stream_place(mode, c.pieces) + stream_sums(mode), shared = c.pieces ? 0 : staged;
-    const int64_t most_waves = KT <= 32 && most_rows <= 8 ? 4 : 8;
+    // A row block's K is shared by as few wavefronts as leave all of them with work: each sum through LDS costs a barrier.  By expert, 14 rows of 18,
+    // 3200 x 7808: eight 51.9 us, four 37.9, two 39.0; two of 5, 9984 x 11264: 150, 127, 114; 768 channels of 9856 (48 row blocks): 11.8, 13.6, 20.3.
+    // Values of one row, 6144 x 4096: eight 7.5, four 6.9; 640 x 9984: 9.5, 12.0.
+    const int64_t all = blocks * pieces, most_waves = into_lds ? (KT <= (experts ? 16 : 32) && all >= cus ? 4 : 8) : all < cus ? 8 : experts && all >= 2 * cus ? 2 : 4;
     int64_t waves = KT < most_waves ? KT : most_waves;
     while (waves > 1 && waves * per_wave + shared > kLds) --waves;
     int64_t at_once = kLds / (waves * per_wave + shared);                      // workgroups per compute unit
@@ -857,9 +849,7 @@ Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool
 template <int MODE> hipError_t launch_stream_of(int src, const Choice& c, const ProductParams& p, hipStream_t s) {
     if (c.pieces == 1) return launch_stream<kF32, 1, MODE>(p, c.waves, c.runs, s);
     if (c.pieces == 2) return launch_stream<kF32, 2, MODE>(p, c.waves, c.runs, s);
-    return src == kF32   ? launch_stream<kF32, 0, MODE>(p, c.waves, c.runs, s)
-           : src == kF16 ? launch_stream<kF16, 0, MODE>(p, c.waves, c.runs, s)
-                         : launch_stream<kBF16, 0, MODE>(p, c.waves, c.runs, s);
+    return src == kF16 ? launch_stream<kF16, 0, MODE>(p, c.waves, c.runs, s) : launch_stream<kBF16, 0, MODE>(p, c.waves, c.runs, s);
 }
 
 template <int MODE, bool EXACT = false> hipError_t launch_of(const Choice& c, int src, const ProductParams& p, int cus, hipStream_t s) {
