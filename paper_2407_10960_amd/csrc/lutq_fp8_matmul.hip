@@ -755,8 +755,13 @@ hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
 }
 
 // Whether the weights are streamed past sixteen rows at a time, or which tile shape, and for the smaller ones how many slices of K: the least
-// of times estimated from the bytes of weights over the pieces of rows (B), or from the number of tiles on the busiest compute unit (n) and of
-// steps (S).  Microseconds.
+// of times that are estimated, in microseconds, from the bytes of weights over the pieces of rows (B), or from the rounds of tiles (n, for two small tiles
+// at once on a unit the number on the busiest) and of steps of 128 columns (S; 1.8 of them for each of the exact sums'):
+//   streamed    4.2 + B / 3 TB/s            256 x 256   4.8 + n (1.52 S + 5.6)         256 x 128   2.8 + n (0.88 S + 2.9)
+//   128 x 128   3.9 + n (0.57 S + 1.4)      128 x 64    3.25 + n (0.428 S + 0.7)       64 x 64     2.25 + n (0.374 S + 0.9), two at once 0.673 S + 0.9
+// and for z slices, each of S / z steps, 4.4 + 0.53 z, 3.6 + 0.75 z and 3.0 + 0.28 z more for storing and joining sums.  The constants are least squares
+// over 228 drawn calls of every shape; on others the best shape was faster by 1 .. 3 % on average, by expert 4 %.  Examples, us (weights from memory): 1594 rows, 288 x 13824: 64 x 64
+// in four slices 21.3, 128 x 128 in six (taken) 24.2, 256 x 128 82; 2048 rows gated, 27648 x 5120: 256 x 256 (taken) 296, 256 x 128 330.
 struct TileChoice { int shape, slices; };             // shape -1: streamed
 
 // `NB`: row blocks of weights, kGated: of both projections.
