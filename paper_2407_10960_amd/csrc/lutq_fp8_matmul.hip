@@ -757,11 +757,13 @@ hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
 // Whether the weights are streamed past sixteen rows at a time, or which tile shape, and for the smaller ones how many slices of K: the least
 // of times that are estimated, in microseconds, from the bytes of weights over the pieces of rows (B), or from the rounds of tiles (n, for two small tiles
 // at once on a unit the number on the busiest) and of steps of 128 columns (S; 1.8 of them for each of the exact sums'):
-//   streamed    4.2 + B / 3 TB/s            256 x 256   4.8 + n (1.52 S + 5.6)         256 x 128   2.8 + n (0.88 S + 2.9)
-//   128 x 128   3.9 + n (0.57 S + 1.4)      128 x 64    3.25 + n (0.428 S + 0.7)       64 x 64     2.25 + n (0.374 S + 0.9), two at once 0.673 S + 0.9
-// and for z slices, each of S / z steps, 4.4 + 0.53 z, 3.6 + 0.75 z and 3.0 + 0.28 z more for storing and joining sums.  The constants are least squares
-// over 228 drawn calls of every shape; on others the best shape was faster by 1 .. 3 % on average, by expert 4 %.  Examples, us (weights from memory): 1594 rows, 288 x 13824: 64 x 64
-// in four slices 21.3, 128 x 128 in six (taken) 24.2, 256 x 128 82; 2048 rows gated, 27648 x 5120: 256 x 256 (taken) 296, 256 x 128 330.
+//   streamed    4.1 + B / 5.8 TB/s (by expert 4, gated 10 from the caches)   256 x 256   4.8 + n (1.52 S + 5.6)         256 x 128   2.8 + n (0.88 S + 2.9)
+//   128 x 128   3.9 + n (0.57 S + 1.4)      128 x 64    3.25 + n (0.428 S + 0.7)       64 x 64     2.25 + n (0.374 S + 0.9), two at once 0.7 S + 0.9
+// and for z slices, each of S / z steps, 5.0 + 0.75 z, 3.6 + 0.75 z and 3.0 + 0.45 z more for storing and joining sums.  The constants are least squares
+// over 228 drawn calls of every shape, corrected on others; on those the best choice was 1 .. 3 % faster on average, by expert 6 %.  Examples, us (weights from
+// memory): 1594 rows, 288 x 13824: 64 x 64 in four slices 21.3, 128 x 128 in six (taken) 24.2, 256 x 128 82; 2048 rows gated, 27648 x 5120: 256 x 256
+// (taken) 296, 256 x 128 330; 33 rows gated, 2304 x 4224: streamed (taken) 7.2, 64 x 64 in three slices 10.8; 224 rows of 14 experts, 9008 x 1920: streamed 89,
+// tiles (taken) 52.
 struct TileChoice { int shape, slices; };             // shape -1: streamed
 
 // `NB`: row blocks of weights, kGated: of both projections.
@@ -774,8 +776,10 @@ TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int 
         const double some = (double)(M < experts ? M : experts), filled = (double)M / (double)rows + 0.5 * some;
         return (double)nx * (filled > some ? filled : some);
     };
-    if (mode != kPowers && M <= 16 * (experts ? experts : 1)) return best;
-    double least = mode == kPowers ? 1e30 : 4.2 + tiles(1, 16) * (double)KT * 2048.0 / 3.0e6;
+    if (mode != kPowers && M <= (experts ? 4 * experts : 16)) return best;
+    // (What is read again comes from the second caches where they hold it; of the gated call, whose X goes as far for twice the weights, twice as fast.)
+    const double rate = experts ? 4.0e6 : mode == kGated && NB * KT * 2048 <= (int64_t(32) << 20) ? 10.0e6 : 5.8e6;
+    double least = mode == kPowers ? 1e30 : 4.1 + tiles(1, 16) * (double)KT * 2048.0 / rate;
     auto consider = [&](int shape, int slices, double us) {
         if (us < least) { least = us; best = {shape, slices}; }
     };
@@ -794,11 +798,11 @@ TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int 
     for (int z = 1; z <= 8; ++z) {
         if (z > KT) break;
         const double steps = z > 1 ? (double)((int64_t)((S + z - 1) / z)) : S;
-        if (z == 1 || t1 * z <= most) consider(1, z, 3.9 + rounds(t1 * z) * (0.57 * steps + 1.4) + (z > 1 ? 4.4 + 0.53 * z : 0.0));
+        if (z == 1 || t1 * z <= most) consider(1, z, 3.9 + rounds(t1 * z) * (0.57 * steps + 1.4) + (z > 1 ? 5.0 + 0.75 * z : 0.0));
         if (z == 1 || t2 * z <= most) consider(2, z, 3.25 + rounds(t2 * z) * (0.428 * steps + 0.7) + (z > 1 ? 3.6 + 0.75 * z : 0.0));
         if (z == 1 || t3 * z <= 2 * most) {
             const double n = (double)(int64_t)((t3 * z + cus - 1) / cus);
-            consider(3, z, 2.25 + pairs(n, 0.374 * steps + 0.9, 0.673 * steps + 0.9) + (z > 1 ? 3.0 + 0.28 * z : 0.0));
+            consider(3, z, 2.25 + pairs(n, 0.374 * steps + 0.9, 0.7 * steps + 0.9) + (z > 1 ? 3.0 + 0.45 * z : 0.0));
         }
     }
     if (best.slices > 1) {                             // as many as the workspace has room for

@@ -18,67 +18,68 @@ from test_mx4_launches import uneven
 # channels and rows at a time, wavefronts, steps of room, slices of K, how it is streamed (0: tiles), past the caches
 CALLS = [
     ("gated", 598, 1664, 512, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)), ("gated", 322, 13824, 128, 0, 1, (0, 128, 128, 8, 4, 1, 0, 0)),
-    ("gated", 337, 1408, 4096, 0, 1, (0, 128, 128, 8, 4, 3, 0, 0)), ("gated", 480, 768, 4736, 0, 1, (0, 128, 128, 8, 4, 5, 0, 0)),
-    ("gated", 257, 1664, 512, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("gated", 132, 11136, 128, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
-    ("gated", 193, 1152, 4352, 0, 1, (0, 128, 64, 8, 4, 3, 0, 0)), ("gated", 328, 5504, 256, 0, 1, (0, 256, 128, 8, 3, 1, 0, 0)),
-    ("gated", 1104, 7424, 256, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)), ("gated", 2518, 1664, 256, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)),
-    ("gated", 2078, 9728, 384, 0, 0, (1, 256, 256, 8, 2, 1, 0, 0)), ("gated", 1, 128, 128, 0, 0, (0, 32, 16, 1, 2, 1, 1, 0)),
-    ("gated", 1, 128, 256, 0, 0, (0, 32, 16, 2, 2, 1, 1, 0)), ("gated", 1, 128, 1024, 0, 0, (0, 32, 16, 8, 2, 1, 1, 0)),
-    ("gated", 1, 7808, 2688, 0, 0, (0, 32, 16, 4, 2, 1, 1, 1)), ("gated", 2, 2688, 7808, 0, 0, (0, 32, 16, 8, 2, 1, 1, 1)),
-    ("gated", 1, 128, 128, 0, 1, (0, 32, 16, 1, 2, 1, 2, 0)), ("gated", 1, 128, 256, 0, 1, (0, 32, 16, 2, 2, 1, 2, 0)),
-    ("gated", 1, 128, 1024, 0, 1, (0, 32, 16, 8, 2, 1, 2, 0)), ("gated", 1, 12672, 1664, 0, 1, (0, 32, 16, 4, 2, 1, 2, 1)),
-    ("gated", 3, 3584, 5888, 0, 1, (0, 32, 16, 8, 2, 1, 2, 1)), ("gated", 9, 128, 128, 0, 1, (0, 32, 16, 1, 2, 1, 3, 0)),
-    ("gated", 9, 128, 256, 0, 1, (0, 32, 16, 2, 2, 1, 3, 0)), ("gated", 9, 128, 1024, 0, 1, (0, 32, 16, 8, 2, 1, 3, 0)),
-    ("gated", 9, 4224, 4992, 0, 1, (0, 32, 16, 4, 2, 1, 3, 1)), ("gated", 12, 2688, 7808, 0, 0, (1, 32, 16, 8, 2, 1, 3, 1)),
-    ("gated", 17, 128, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("gated", 217, 256, 1920, 0, 1, (0, 64, 64, 4, 4, 5, 0, 0)),
-    ("gated", 162, 256, 2688, 0, 1, (0, 64, 64, 4, 4, 7, 0, 0)), ("gated", 1211, 1408, 768, 1, 1, (0, 128, 128, 8, 4, 1, 0, 0)),
-    ("gated", 236, 1408, 6784, 1, 0, (1, 128, 128, 8, 4, 3, 0, 0)), ("gated", 632, 512, 5888, 1, 1, (0, 128, 128, 8, 4, 4, 0, 0)),
-    ("gated", 381, 1408, 512, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("gated", 213, 8576, 128, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
-    ("gated", 161, 1408, 4864, 1, 1, (0, 128, 64, 8, 4, 2, 0, 0)), ("gated", 1913, 1280, 256, 1, 1, (0, 256, 128, 8, 3, 1, 0, 0)),
-    ("gated", 1567, 5120, 128, 1, 1, (0, 256, 128, 8, 3, 1, 0, 0)), ("gated", 5740, 2688, 2304, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
-    ("gated", 5146, 4224, 1152, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)), ("gated", 1, 128, 128, 1, 0, (0, 32, 16, 1, 2, 1, 1, 0)),
-    ("gated", 1, 128, 256, 1, 0, (0, 32, 16, 2, 2, 1, 1, 0)), ("gated", 1, 128, 1024, 1, 0, (0, 32, 16, 8, 2, 1, 1, 0)),
-    ("gated", 43, 3840, 128, 43, 0, (0, 32, 16, 1, 2, 1, 1, 1)), ("gated", 9, 2944, 896, 8, 0, (0, 32, 16, 4, 2, 1, 1, 1)),
-    ("gated", 3, 896, 7808, 3, 0, (0, 32, 16, 8, 2, 1, 1, 1)), ("gated", 1, 128, 128, 1, 1, (0, 32, 16, 1, 2, 1, 2, 0)),
-    ("gated", 1, 128, 256, 1, 1, (0, 32, 16, 2, 2, 1, 2, 0)), ("gated", 1, 128, 1024, 1, 1, (0, 32, 16, 8, 2, 1, 2, 0)),
-    ("gated", 3, 1664, 4224, 3, 1, (0, 32, 16, 4, 2, 1, 2, 1)), ("gated", 6, 512, 13696, 3, 0, (1, 32, 16, 8, 2, 1, 2, 1)),
-    ("gated", 9, 128, 128, 1, 1, (0, 32, 16, 1, 2, 1, 3, 0)), ("gated", 10, 128, 256, 1, 1, (0, 32, 16, 2, 2, 1, 3, 0)),
-    ("gated", 9, 128, 1024, 1, 1, (0, 32, 16, 8, 2, 1, 3, 0)), ("gated", 15, 15104, 128, 11, 1, (0, 32, 16, 1, 2, 1, 3, 1)),
-    ("gated", 24, 1664, 1152, 11, 1, (0, 32, 16, 2, 2, 1, 3, 1)), ("gated", 11, 384, 5504, 10, 1, (0, 32, 16, 8, 2, 1, 3, 1)),
-    ("gated", 19, 128, 128, 1, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("gated", 131, 11648, 128, 1, 0, (1, 64, 64, 4, 4, 1, 0, 0)),
-    ("gated", 224, 256, 1920, 1, 1, (0, 64, 64, 4, 4, 5, 0, 0)), ("gated", 160, 256, 3328, 1, 1, (0, 64, 64, 4, 4, 7, 0, 0)),
-    ("gated_saved", 259, 3840, 256, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)), ("gated_saved", 1231, 3328, 256, 0, 1, (0, 128, 128, 8, 4, 1, 0, 0)),
-    ("gated_saved", 473, 1152, 2304, 0, 1, (0, 128, 128, 8, 4, 3, 0, 0)), ("gated_saved", 329, 1024, 2688, 0, 0, (1, 128, 128, 8, 4, 5, 0, 0)),
-    ("gated_saved", 268, 1664, 256, 0, 0, (1, 128, 64, 8, 4, 1, 0, 0)), ("gated_saved", 137, 16896, 128, 0, 0, (1, 128, 64, 8, 4, 1, 0, 0)),
-    ("gated_saved", 292, 896, 2432, 0, 0, (1, 128, 64, 8, 4, 3, 0, 0)), ("gated_saved", 159, 768, 9600, 0, 0, (1, 128, 64, 8, 4, 7, 0, 0)),
-    ("gated_saved", 75, 16640, 128, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)), ("gated_saved", 907, 8960, 128, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)),
-    ("gated_saved", 1, 128, 128, 0, 0, (0, 32, 16, 1, 2, 1, 1, 0)), ("gated_saved", 1, 128, 256, 0, 0, (0, 32, 16, 2, 2, 1, 1, 0)),
-    ("gated_saved", 1, 128, 1024, 0, 0, (0, 32, 16, 8, 2, 1, 1, 0)), ("gated_saved", 3, 7808, 2688, 0, 0, (0, 32, 16, 4, 2, 1, 1, 1)),
-    ("gated_saved", 2, 4992, 4224, 0, 0, (0, 32, 16, 8, 2, 1, 1, 1)), ("gated_saved", 1, 128, 128, 0, 1, (0, 32, 16, 1, 2, 1, 2, 0)),
-    ("gated_saved", 1, 128, 256, 0, 1, (0, 32, 16, 2, 2, 1, 2, 0)), ("gated_saved", 1, 128, 1024, 0, 1, (0, 32, 16, 8, 2, 1, 2, 0)),
-    ("gated_saved", 1, 18304, 1152, 0, 1, (0, 32, 16, 4, 2, 1, 2, 1)), ("gated_saved", 3, 2944, 7168, 0, 1, (0, 32, 16, 8, 2, 1, 2, 1)),
-    ("gated_saved", 9, 128, 128, 0, 1, (0, 32, 16, 1, 2, 1, 3, 0)), ("gated_saved", 9, 128, 256, 0, 1, (0, 32, 16, 2, 2, 1, 3, 0)),
-    ("gated_saved", 9, 128, 1024, 0, 1, (0, 32, 16, 8, 2, 1, 3, 0)), ("gated_saved", 9, 7168, 2944, 0, 0, (1, 32, 16, 4, 2, 1, 3, 1)),
-    ("gated_saved", 9, 2688, 7808, 0, 0, (1, 32, 16, 8, 2, 1, 3, 1)), ("gated_saved", 18, 128, 128, 0, 0, (1, 64, 64, 4, 4, 1, 0, 0)),
-    ("gated_saved", 158, 640, 1152, 0, 0, (1, 64, 64, 4, 4, 4, 0, 0)), ("gated_saved", 178, 384, 1920, 0, 0, (1, 64, 64, 4, 4, 7, 0, 0)),
-    ("gated_saved", 887, 2048, 384, 1, 1, (0, 128, 128, 8, 4, 1, 0, 0)), ("gated_saved", 211, 1664, 3712, 1, 1, (0, 128, 128, 8, 4, 3, 0, 0)),
-    ("gated_saved", 636, 384, 2816, 2, 1, (0, 128, 128, 8, 4, 5, 0, 0)), ("gated_saved", 583, 896, 256, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
-    ("gated_saved", 663, 3200, 128, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("gated_saved", 495, 512, 2688, 1, 0, (1, 128, 64, 8, 4, 2, 0, 0)),
-    ("gated_saved", 589, 3584, 256, 1, 1, (0, 256, 128, 8, 3, 1, 0, 0)), ("gated_saved", 964, 8704, 128, 1, 0, (1, 256, 128, 8, 3, 1, 0, 0)),
-    ("gated_saved", 1, 128, 128, 1, 0, (0, 32, 16, 1, 2, 1, 1, 0)), ("gated_saved", 1, 128, 256, 1, 0, (0, 32, 16, 2, 2, 1, 1, 0)),
-    ("gated_saved", 2, 128, 1024, 1, 0, (0, 32, 16, 8, 2, 1, 1, 0)), ("gated_saved", 29, 5760, 128, 29, 0, (0, 32, 16, 1, 2, 1, 1, 1)),
-    ("gated_saved", 8, 2944, 896, 8, 0, (0, 32, 16, 4, 2, 1, 1, 1)), ("gated_saved", 3, 4224, 4992, 1, 0, (0, 32, 16, 8, 2, 1, 1, 1)),
-    ("gated_saved", 1, 128, 128, 1, 1, (0, 32, 16, 1, 2, 1, 2, 0)), ("gated_saved", 1, 128, 256, 1, 1, (0, 32, 16, 2, 2, 1, 2, 0)),
-    ("gated_saved", 2, 128, 1024, 1, 1, (0, 32, 16, 8, 2, 1, 2, 0)), ("gated_saved", 3, 1408, 4992, 3, 1, (0, 32, 16, 4, 2, 1, 2, 1)),
-    ("gated_saved", 7, 384, 11008, 5, 0, (1, 32, 16, 8, 2, 1, 2, 1)), ("gated_saved", 9, 128, 128, 1, 1, (0, 32, 16, 1, 2, 1, 3, 0)),
-    ("gated_saved", 9, 128, 256, 1, 1, (0, 32, 16, 2, 2, 1, 3, 0)), ("gated_saved", 13, 128, 1024, 1, 1, (0, 32, 16, 8, 2, 1, 3, 0)),
-    ("gated_saved", 21, 7808, 128, 21, 1, (0, 32, 16, 1, 2, 1, 3, 1)), ("gated_saved", 20, 5504, 384, 10, 1, (0, 32, 16, 2, 2, 1, 3, 1)),
-    ("gated_saved", 16, 1920, 5504, 2, 1, (0, 32, 16, 8, 2, 1, 3, 1)), ("gated_saved", 23, 128, 128, 1, 0, (1, 64, 64, 4, 4, 1, 0, 0)),
-    ("gated_saved", 200, 512, 1280, 1, 0, (1, 64, 64, 4, 4, 4, 0, 0)), ("gated_saved", 247, 256, 2048, 1, 1, (0, 64, 64, 4, 4, 7, 0, 0)),
-    ("matmul", 777, 2640, 512, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)), ("matmul", 773, 10208, 384, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)),
-    ("matmul", 770, 1360, 4096, 0, 0, (1, 128, 128, 8, 4, 3, 0, 0)), ("matmul", 614, 1120, 5120, 0, 0, (1, 128, 128, 8, 4, 5, 0, 0)),
-    ("matmul", 589, 1680, 512, 0, 0, (1, 128, 64, 8, 4, 1, 0, 0)), ("matmul", 769, 5104, 128, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
-    ("matmul", 705, 672, 4736, 0, 0, (1, 128, 64, 8, 4, 3, 0, 0)), ("matmul", 1, 16, 128, 0, 0, (0, 16, 16, 1, 4, 1, 1, 0)),
+    ("gated", 451, 1152, 4864, 0, 1, (0, 128, 128, 8, 4, 3, 0, 0)), ("gated", 536, 640, 6784, 0, 0, (1, 128, 128, 8, 4, 5, 0, 0)),
+    ("gated", 275, 1664, 384, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("gated", 132, 11136, 128, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
+    ("gated", 386, 640, 3840, 0, 0, (1, 128, 64, 8, 4, 3, 0, 0)), ("gated", 132, 768, 11904, 0, 0, (1, 128, 64, 8, 4, 7, 0, 0)),
+    ("gated", 328, 5504, 256, 0, 1, (0, 256, 128, 8, 3, 1, 0, 0)), ("gated", 1104, 7424, 256, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)),
+    ("gated", 2518, 1664, 256, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)), ("gated", 2078, 9728, 384, 0, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
+    ("gated", 1, 128, 128, 0, 0, (0, 32, 16, 1, 2, 1, 1, 0)), ("gated", 1, 128, 256, 0, 0, (0, 32, 16, 2, 2, 1, 1, 0)),
+    ("gated", 1, 128, 1024, 0, 0, (0, 32, 16, 8, 2, 1, 1, 0)), ("gated", 1, 7808, 2688, 0, 0, (0, 32, 16, 4, 2, 1, 1, 1)),
+    ("gated", 2, 2688, 7808, 0, 0, (0, 32, 16, 8, 2, 1, 1, 1)), ("gated", 1, 128, 128, 0, 1, (0, 32, 16, 1, 2, 1, 2, 0)),
+    ("gated", 1, 128, 256, 0, 1, (0, 32, 16, 2, 2, 1, 2, 0)), ("gated", 1, 128, 1024, 0, 1, (0, 32, 16, 8, 2, 1, 2, 0)),
+    ("gated", 1, 12672, 1664, 0, 1, (0, 32, 16, 4, 2, 1, 2, 1)), ("gated", 3, 3584, 5888, 0, 1, (0, 32, 16, 8, 2, 1, 2, 1)),
+    ("gated", 9, 128, 128, 0, 1, (0, 32, 16, 1, 2, 1, 3, 0)), ("gated", 9, 128, 256, 0, 1, (0, 32, 16, 2, 2, 1, 3, 0)),
+    ("gated", 9, 128, 1024, 0, 1, (0, 32, 16, 8, 2, 1, 3, 0)), ("gated", 9, 4224, 4992, 0, 1, (0, 32, 16, 4, 2, 1, 3, 1)),
+    ("gated", 12, 2688, 7808, 0, 0, (1, 32, 16, 8, 2, 1, 3, 1)), ("gated", 17, 128, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)),
+    ("gated", 246, 640, 3328, 0, 1, (0, 64, 64, 4, 4, 3, 0, 0)), ("gated", 187, 384, 11264, 0, 1, (0, 64, 64, 4, 4, 7, 0, 0)),
+    ("gated", 1211, 1408, 768, 1, 1, (0, 128, 128, 8, 4, 1, 0, 0)), ("gated", 236, 1408, 6784, 1, 0, (1, 128, 128, 8, 4, 3, 0, 0)),
+    ("gated", 430, 640, 9088, 1, 0, (1, 128, 128, 8, 4, 4, 0, 0)), ("gated", 206, 2304, 384, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
+    ("gated", 213, 8576, 128, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("gated", 198, 768, 6912, 1, 1, (0, 128, 64, 8, 4, 4, 0, 0)),
+    ("gated", 1913, 1280, 256, 1, 1, (0, 256, 128, 8, 3, 1, 0, 0)), ("gated", 1567, 5120, 128, 1, 1, (0, 256, 128, 8, 3, 1, 0, 0)),
+    ("gated", 5740, 2688, 2304, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)), ("gated", 5146, 4224, 1152, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
+    ("gated", 1, 128, 128, 1, 0, (0, 32, 16, 1, 2, 1, 1, 0)), ("gated", 1, 128, 256, 1, 0, (0, 32, 16, 2, 2, 1, 1, 0)),
+    ("gated", 1, 128, 1024, 1, 0, (0, 32, 16, 8, 2, 1, 1, 0)), ("gated", 43, 3840, 128, 43, 0, (0, 32, 16, 1, 2, 1, 1, 1)),
+    ("gated", 9, 2944, 896, 8, 0, (0, 32, 16, 4, 2, 1, 1, 1)), ("gated", 3, 896, 7808, 3, 0, (0, 32, 16, 8, 2, 1, 1, 1)),
+    ("gated", 1, 128, 128, 1, 1, (0, 32, 16, 1, 2, 1, 2, 0)), ("gated", 1, 128, 256, 1, 1, (0, 32, 16, 2, 2, 1, 2, 0)),
+    ("gated", 1, 128, 1024, 1, 1, (0, 32, 16, 8, 2, 1, 2, 0)), ("gated", 3, 1664, 4224, 3, 1, (0, 32, 16, 4, 2, 1, 2, 1)),
+    ("gated", 6, 512, 13696, 3, 0, (1, 32, 16, 8, 2, 1, 2, 1)), ("gated", 9, 128, 128, 3, 1, (0, 32, 16, 1, 2, 1, 3, 0)),
+    ("gated", 9, 128, 384, 1, 1, (0, 32, 16, 3, 2, 1, 3, 0)), ("gated", 9, 128, 1024, 1, 1, (0, 32, 16, 8, 2, 1, 3, 0)),
+    ("gated", 15, 15104, 128, 11, 1, (0, 32, 16, 1, 2, 1, 3, 1)), ("gated", 24, 1664, 1152, 11, 1, (0, 32, 16, 2, 2, 1, 3, 1)),
+    ("gated", 11, 384, 5504, 10, 1, (0, 32, 16, 8, 2, 1, 3, 1)), ("gated", 5, 128, 128, 1, 0, (1, 64, 64, 4, 4, 1, 0, 0)),
+    ("gated", 131, 11648, 128, 1, 0, (1, 64, 64, 4, 4, 1, 0, 0)), ("gated", 285, 256, 2688, 1, 1, (0, 64, 64, 4, 4, 3, 0, 0)),
+    ("gated", 141, 384, 6272, 1, 1, (0, 64, 64, 4, 4, 7, 0, 0)), ("gated_saved", 259, 3840, 256, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)),
+    ("gated_saved", 1231, 3328, 256, 0, 1, (0, 128, 128, 8, 4, 1, 0, 0)), ("gated_saved", 657, 768, 2816, 0, 1, (0, 128, 128, 8, 4, 3, 0, 0)),
+    ("gated_saved", 459, 768, 3840, 0, 1, (0, 128, 128, 8, 4, 5, 0, 0)), ("gated_saved", 268, 1664, 256, 0, 0, (1, 128, 64, 8, 4, 1, 0, 0)),
+    ("gated_saved", 273, 11136, 128, 0, 0, (1, 128, 64, 8, 4, 1, 0, 0)), ("gated_saved", 310, 1024, 2944, 0, 1, (0, 128, 64, 8, 4, 3, 0, 0)),
+    ("gated_saved", 372, 384, 9344, 0, 0, (1, 128, 64, 8, 4, 7, 0, 0)), ("gated_saved", 788, 2560, 128, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)),
+    ("gated_saved", 907, 8960, 128, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)), ("gated_saved", 1, 128, 128, 0, 0, (0, 32, 16, 1, 2, 1, 1, 0)),
+    ("gated_saved", 1, 128, 256, 0, 0, (0, 32, 16, 2, 2, 1, 1, 0)), ("gated_saved", 1, 128, 1024, 0, 0, (0, 32, 16, 8, 2, 1, 1, 0)),
+    ("gated_saved", 3, 7808, 2688, 0, 0, (0, 32, 16, 4, 2, 1, 1, 1)), ("gated_saved", 2, 4992, 4224, 0, 0, (0, 32, 16, 8, 2, 1, 1, 1)),
+    ("gated_saved", 1, 128, 128, 0, 1, (0, 32, 16, 1, 2, 1, 2, 0)), ("gated_saved", 1, 128, 256, 0, 1, (0, 32, 16, 2, 2, 1, 2, 0)),
+    ("gated_saved", 1, 128, 1024, 0, 1, (0, 32, 16, 8, 2, 1, 2, 0)), ("gated_saved", 1, 18304, 1152, 0, 1, (0, 32, 16, 4, 2, 1, 2, 1)),
+    ("gated_saved", 3, 2944, 7168, 0, 1, (0, 32, 16, 8, 2, 1, 2, 1)), ("gated_saved", 9, 128, 128, 0, 1, (0, 32, 16, 1, 2, 1, 3, 0)),
+    ("gated_saved", 9, 128, 256, 0, 1, (0, 32, 16, 2, 2, 1, 3, 0)), ("gated_saved", 9, 128, 1024, 0, 1, (0, 32, 16, 8, 2, 1, 3, 0)),
+    ("gated_saved", 9, 7168, 2944, 0, 0, (1, 32, 16, 4, 2, 1, 3, 1)), ("gated_saved", 9, 2688, 7808, 0, 0, (1, 32, 16, 8, 2, 1, 3, 1)),
+    ("gated_saved", 18, 128, 128, 0, 0, (1, 64, 64, 4, 4, 1, 0, 0)), ("gated_saved", 35, 1920, 9088, 0, 1, (0, 64, 64, 4, 4, 4, 0, 0)),
+    ("gated_saved", 33, 1152, 15872, 0, 1, (0, 64, 64, 4, 4, 7, 0, 0)), ("gated_saved", 887, 2048, 384, 1, 1, (0, 128, 128, 8, 4, 1, 0, 0)),
+    ("gated_saved", 363, 896, 3968, 2, 0, (1, 128, 128, 8, 4, 3, 0, 0)), ("gated_saved", 291, 1024, 5760, 1, 0, (1, 128, 128, 8, 4, 4, 0, 0)),
+    ("gated_saved", 583, 896, 256, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("gated_saved", 663, 3200, 128, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
+    ("gated_saved", 495, 512, 2688, 1, 0, (1, 128, 64, 8, 4, 2, 0, 0)), ("gated_saved", 589, 3584, 256, 1, 1, (0, 256, 128, 8, 3, 1, 0, 0)),
+    ("gated_saved", 964, 8704, 128, 1, 0, (1, 256, 128, 8, 3, 1, 0, 0)), ("gated_saved", 1, 128, 128, 1, 0, (0, 32, 16, 1, 2, 1, 1, 0)),
+    ("gated_saved", 1, 128, 256, 1, 0, (0, 32, 16, 2, 2, 1, 1, 0)), ("gated_saved", 2, 128, 1024, 1, 0, (0, 32, 16, 8, 2, 1, 1, 0)),
+    ("gated_saved", 29, 5760, 128, 29, 0, (0, 32, 16, 1, 2, 1, 1, 1)), ("gated_saved", 8, 2944, 896, 8, 0, (0, 32, 16, 4, 2, 1, 1, 1)),
+    ("gated_saved", 3, 4224, 4992, 1, 0, (0, 32, 16, 8, 2, 1, 1, 1)), ("gated_saved", 1, 128, 128, 1, 1, (0, 32, 16, 1, 2, 1, 2, 0)),
+    ("gated_saved", 1, 128, 256, 1, 1, (0, 32, 16, 2, 2, 1, 2, 0)), ("gated_saved", 2, 128, 1024, 1, 1, (0, 32, 16, 8, 2, 1, 2, 0)),
+    ("gated_saved", 3, 1408, 4992, 3, 1, (0, 32, 16, 4, 2, 1, 2, 1)), ("gated_saved", 7, 384, 11008, 5, 0, (1, 32, 16, 8, 2, 1, 2, 1)),
+    ("gated_saved", 9, 128, 128, 3, 1, (0, 32, 16, 1, 2, 1, 3, 0)), ("gated_saved", 9, 128, 256, 1, 1, (0, 32, 16, 2, 2, 1, 3, 0)),
+    ("gated_saved", 13, 128, 1024, 1, 1, (0, 32, 16, 8, 2, 1, 3, 0)), ("gated_saved", 21, 7808, 128, 21, 1, (0, 32, 16, 1, 2, 1, 3, 1)),
+    ("gated_saved", 20, 5504, 384, 10, 1, (0, 32, 16, 2, 2, 1, 3, 1)), ("gated_saved", 16, 1920, 5504, 2, 1, (0, 32, 16, 8, 2, 1, 3, 1)),
+    ("gated_saved", 5, 128, 128, 1, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("gated_saved", 390, 384, 1280, 1, 1, (0, 64, 64, 4, 4, 3, 0, 0)),
+    ("gated_saved", 231, 256, 4992, 1, 1, (0, 64, 64, 4, 4, 7, 0, 0)), ("matmul", 777, 2640, 512, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)),
+    ("matmul", 773, 10208, 384, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)), ("matmul", 493, 2064, 4992, 0, 0, (1, 128, 128, 8, 4, 3, 0, 0)),
+    ("matmul", 658, 992, 6912, 0, 0, (1, 128, 128, 8, 4, 5, 0, 0)), ("matmul", 716, 1360, 384, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
+    ("matmul", 769, 5104, 128, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("matmul", 451, 1168, 3840, 0, 1, (0, 128, 64, 8, 4, 3, 0, 0)),
+    ("matmul", 322, 672, 11392, 0, 0, (1, 128, 64, 8, 4, 7, 0, 0)), ("matmul", 1, 16, 128, 0, 0, (0, 16, 16, 1, 4, 1, 1, 0)),
     ("matmul", 1, 16, 256, 0, 0, (0, 16, 16, 2, 4, 1, 1, 0)), ("matmul", 1, 16, 1024, 0, 0, (0, 16, 16, 8, 4, 1, 1, 0)),
     ("matmul", 1, 32896, 1280, 0, 0, (0, 16, 16, 4, 4, 1, 1, 1)), ("matmul", 3, 6304, 6656, 0, 0, (0, 16, 16, 8, 4, 1, 1, 1)),
     ("matmul", 1, 16, 128, 0, 1, (0, 16, 16, 1, 4, 1, 2, 0)), ("matmul", 1, 16, 256, 0, 1, (0, 16, 16, 2, 4, 1, 2, 0)),
@@ -89,31 +90,31 @@ CALLS = [
     ("matmul", 1690, 2416, 256, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)), ("matmul", 3715, 4384, 256, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)),
     ("matmul", 1514, 5392, 256, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)), ("matmul", 4225, 9584, 384, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)),
     ("matmul", 17, 16, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("matmul", 16491, 304, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)),
-    ("matmul", 202, 544, 1920, 0, 0, (1, 64, 64, 4, 4, 5, 0, 0)), ("matmul", 265, 352, 2688, 0, 1, (0, 64, 64, 4, 4, 7, 0, 0)),
+    ("matmul", 372, 576, 2432, 0, 1, (0, 64, 64, 4, 4, 4, 0, 0)), ("matmul", 155, 752, 6272, 0, 0, (1, 64, 64, 4, 4, 7, 0, 0)),
     ("matmul", 1704, 1808, 768, 1, 0, (1, 128, 128, 8, 4, 1, 0, 0)), ("matmul", 10012, 800, 256, 1, 1, (0, 128, 128, 8, 4, 1, 0, 0)),
-    ("matmul", 788, 832, 6400, 1, 0, (1, 128, 128, 8, 4, 3, 0, 0)), ("matmul", 996, 512, 4992, 1, 1, (0, 128, 128, 8, 4, 5, 0, 0)),
-    ("matmul", 617, 1680, 512, 1, 0, (1, 128, 64, 8, 4, 1, 0, 0)), ("matmul", 772, 5264, 128, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
+    ("matmul", 576, 1296, 6912, 1, 0, (1, 128, 128, 8, 4, 3, 0, 0)), ("matmul", 1049, 464, 8704, 1, 1, (0, 128, 128, 8, 4, 5, 0, 0)),
+    ("matmul", 581, 1760, 384, 1, 0, (1, 128, 64, 8, 4, 1, 0, 0)), ("matmul", 772, 5264, 128, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
     ("matmul", 373, 1456, 5120, 1, 1, (0, 128, 64, 8, 4, 2, 0, 0)), ("matmul", 1, 16, 128, 1, 0, (0, 16, 16, 1, 4, 1, 1, 0)),
     ("matmul", 1, 16, 256, 1, 0, (0, 16, 16, 2, 4, 1, 1, 0)), ("matmul", 1, 16, 1024, 1, 0, (0, 16, 16, 8, 4, 1, 1, 0)),
     ("matmul", 48, 11712, 128, 29, 0, (0, 16, 16, 1, 4, 1, 1, 1)), ("matmul", 8, 4256, 1408, 7, 0, (0, 16, 16, 4, 4, 1, 1, 1)),
     ("matmul", 3, 944, 14848, 3, 0, (0, 16, 16, 8, 4, 1, 1, 1)), ("matmul", 1, 16, 128, 1, 1, (0, 16, 16, 1, 4, 1, 2, 0)),
     ("matmul", 1, 16, 256, 1, 1, (0, 16, 16, 2, 4, 1, 2, 0)), ("matmul", 1, 16, 1024, 1, 1, (0, 16, 16, 8, 4, 1, 2, 0)),
     ("matmul", 2, 3152, 6656, 2, 1, (0, 16, 16, 4, 4, 1, 2, 1)), ("matmul", 6, 1072, 13056, 3, 1, (0, 16, 16, 8, 4, 1, 2, 1)),
-    ("matmul", 9, 16, 128, 1, 1, (0, 16, 16, 1, 4, 1, 3, 0)), ("matmul", 9, 16, 256, 1, 1, (0, 16, 16, 2, 4, 1, 3, 0)),
+    ("matmul", 12, 16, 128, 3, 1, (0, 16, 16, 1, 4, 1, 3, 0)), ("matmul", 9, 16, 384, 1, 1, (0, 16, 16, 3, 4, 1, 3, 0)),
     ("matmul", 11, 16, 1152, 1, 1, (0, 16, 16, 8, 4, 1, 3, 0)), ("matmul", 46, 14352, 128, 23, 1, (0, 16, 16, 1, 4, 1, 3, 1)),
     ("matmul", 14, 1808, 1792, 13, 1, (0, 16, 16, 2, 4, 1, 3, 1)), ("matmul", 10, 2688, 15616, 1, 0, (1, 16, 16, 8, 4, 1, 3, 1)),
     ("matmul", 2755, 1696, 256, 1, 0, (1, 256, 128, 8, 3, 1, 0, 0)), ("matmul", 789, 19504, 128, 1, 0, (1, 256, 128, 8, 3, 1, 0, 0)),
     ("matmul", 10739, 2768, 2304, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)), ("matmul", 6387, 5280, 1920, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
-    ("matmul", 24, 16, 128, 1, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("matmul", 130, 23728, 128, 1, 1, (0, 64, 64, 4, 4, 1, 0, 0)),
-    ("matmul", 254, 416, 2176, 1, 0, (1, 64, 64, 4, 4, 6, 0, 0)), ("matmul", 208, 464, 3584, 1, 1, (0, 64, 64, 4, 4, 7, 0, 0)),
+    ("matmul", 5, 16, 128, 1, 0, (1, 64, 64, 4, 4, 1, 0, 0)), ("matmul", 130, 23728, 128, 1, 1, (0, 64, 64, 4, 4, 1, 0, 0)),
+    ("matmul", 195, 880, 2304, 1, 1, (0, 64, 64, 4, 4, 3, 0, 0)), ("matmul", 99, 736, 7168, 1, 0, (1, 64, 64, 4, 4, 7, 0, 0)),
     ("weight_grad", 800, 2544, 512, 0, 1, (0, 128, 128, 8, 4, 1, 0, 0)), ("weight_grad", 784, 12624, 128, 0, 1, (0, 128, 128, 8, 4, 1, 0, 0)),
-    ("weight_grad", 880, 1168, 4352, 0, 1, (0, 128, 128, 8, 4, 3, 0, 0)), ("weight_grad", 576, 1216, 4864, 0, 1, (0, 128, 128, 8, 4, 5, 0, 0)),
-    ("weight_grad", 800, 1248, 512, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("weight_grad", 784, 5104, 128, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
-    ("weight_grad", 720, 656, 4352, 0, 1, (0, 128, 64, 8, 4, 3, 0, 0)), ("weight_grad", 1680, 2416, 256, 0, 1, (0, 256, 128, 8, 3, 1, 0, 0)),
-    ("weight_grad", 4816, 3360, 256, 0, 1, (0, 256, 128, 8, 3, 1, 0, 0)), ("weight_grad", 5456, 1424, 256, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)),
-    ("weight_grad", 4320, 9568, 384, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)), ("weight_grad", 16, 16, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)),
-    ("weight_grad", 18384, 272, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("weight_grad", 16, 16, 1920, 0, 1, (0, 64, 64, 4, 4, 5, 0, 0)),
-    ("weight_grad", 16, 16, 2688, 0, 1, (0, 64, 64, 4, 4, 7, 0, 0)),
+    ("weight_grad", 928, 1120, 4864, 0, 1, (0, 128, 128, 8, 4, 3, 0, 0)), ("weight_grad", 464, 1424, 7040, 0, 1, (0, 128, 128, 8, 4, 5, 0, 0)),
+    ("weight_grad", 784, 1232, 384, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("weight_grad", 784, 5104, 128, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
+    ("weight_grad", 464, 1152, 3840, 0, 1, (0, 128, 64, 8, 4, 3, 0, 0)), ("weight_grad", 304, 800, 11392, 0, 1, (0, 128, 64, 8, 4, 7, 0, 0)),
+    ("weight_grad", 1680, 2416, 256, 0, 1, (0, 256, 128, 8, 3, 1, 0, 0)), ("weight_grad", 4816, 3360, 256, 0, 1, (0, 256, 128, 8, 3, 1, 0, 0)),
+    ("weight_grad", 5456, 1424, 256, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)), ("weight_grad", 4320, 9568, 384, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)),
+    ("weight_grad", 16, 16, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("weight_grad", 18384, 272, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)),
+    ("weight_grad", 16, 16, 2304, 0, 1, (0, 64, 64, 4, 4, 3, 0, 0)), ("weight_grad", 16, 16, 6272, 0, 1, (0, 64, 64, 4, 4, 7, 0, 0)),
 ]
 
 
