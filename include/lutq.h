@@ -552,9 +552,10 @@ typedef enum {
  *   H                    device, [M, F], dtype, or NULL
  *   h_codes, h_scales    device, or NULL: ROWS [M, F], what lutq_fp8_quantize makes of H of `dtype`, ready for the down projection's product.
  *                        H, these, or all of them
- *   saved                device, [M, 2 F], dtype, or NULL: G and U side by side, for lutq_fp8_gated_grad.  The codes' products are then summed by the
- *                        16-bit instruction, which cuts nothing off: a last bit of G or U that differs becomes a whole step of a code where
- *                        their gradients are quantised.  It has half the rate; H may differ in its last bits from a call without.
+ *   saved                device, [M, 2 F], dtype, or NULL: G and U side by side, for lutq_fp8_gated_grad
+ * With h_codes or saved the codes' products are summed by the 16-bit instruction, which cuts nothing off: a last bit of G or U that differs becomes a
+ * whole step of a code where H or the gradients are quantised.  With many rows it takes 1.9 times as long; H may differ in its last bits from that of a
+ * call without either.
  *   workspace            >= lutq_fp8_gated_workspace_bytes(M, F, K, 1), as for lutq_fp8_matmul
  * Errors: those of lutq_fp8_matmul; DTYPE also for an activation that there is not.
  * By expert (lutq_fp8_gated_grouped; W: `experts` of them) as for lutq_fp8_matmul_grouped: rows outside stay in every output. */

@@ -67,7 +67,7 @@ int lutq_calib_plan(int bits, int group_size, int64_t M, int64_t N, int64_t K, i
  * Return values: 0, 1 (launch NULL) or 4 (shape, M < 1 or compute units out of range). */
 int lutq_calib_mx4_launch(int64_t M, int64_t N, int64_t K, int64_t experts, int x_is_codes, int compute_units, int launch[8]);
 
-/* The same for the 8-bit products: form 0 lutq_fp8_matmul (_grouped), 1 lutq_fp8_gated (_grouped; N is F), 3 the same with `saved`, 2 lutq_fp8_weight_grad (its N, K,
+/* The same for the 8-bit products: form 0 lutq_fp8_matmul (_grouped), 1 lutq_fp8_gated (_grouped; N is F), 3 the same with `saved` or `h_codes`, 2 lutq_fp8_weight_grad (its N, K,
  * M as M, N, K; experts 0, codes).  launch[1] counts the channels of both projections; launch[6] = 0: tiles, 1: streamed
  * with X quantised into LDS, 2, 3: with one or two pieces of eight rows of X at a time; launch[4] is the steps there is room for in every case.  Return values as above. */
 int lutq_calib_fp8_launch(int64_t M, int64_t N, int64_t K, int64_t experts, int form, int x_is_codes, int compute_units, int launch[8]);

@@ -993,7 +993,8 @@ def _fp8_gated(name, X, W, w_scales, offsets, H, workspace, x_scales, activation
 def lutq_fp8_gated(X, W, w_scales, H, workspace, x_scales=None, activation="silu", h_scales=None, saved=None, dtype=None, stream=None):
     """H [M, F] = act(X G^T) * (X U^T), W [2 F, K] = G over U, X as for lutq_fp8_matmul; activation "silu" or "gelu" (tanh form).
     H: float16 or bfloat16; or, with h_scales [F / 128, M], codes, quantised from H rounded to `dtype` (that of X where it is no
-    codes).  saved [M, 2 F]: takes the two projections side by side, for lutq_fp8_gated_grad."""
+    codes).  saved [M, 2 F]: takes the two projections side by side, for lutq_fp8_gated_grad.  With h_scales or saved the sums of codes
+    are exact, at 1.9 times the time where rows are many."""
     return _fp8_gated("lutq_fp8_gated", X, W, w_scales, None, H, workspace, x_scales, activation, h_scales, saved, dtype, stream)
 
 
@@ -1128,7 +1129,7 @@ class Fp8Launch:
 
 
 def calib_fp8_launch(M: int, N: int, K: int, experts: int = 0, form: str = "matmul", codes: bool = False, compute_units: int = 256) -> Fp8Launch:
-    """How the library launches lutq_fp8_matmul (form "matmul"), lutq_fp8_gated ("gated", N is F, "gated_saved"; with experts the ones by expert), or
+    """How the library launches lutq_fp8_matmul (form "matmul"), lutq_fp8_gated ("gated", N is F; "gated_saved" with saved or codes of H; with experts the ones by expert), or
     lutq_fp8_weight_grad ("weight_grad"; its N, K, M as M, N, K)."""
     out = (ctypes.c_int * 8)()
     _check(load_library().lutq_calib_fp8_launch(M, N, K, experts, ("matmul", "gated", "weight_grad", "gated_saved").index(form), int(codes), compute_units, out),

@@ -913,7 +913,9 @@ lutq_status product_on(const Call& a, hipStream_t s) {
     int src = a.xs ? kF32 : a.dtype == LUTQ_F16 ? kF16 : kBF16;
     const int cus = compute_units();
     if (cus < 1) return LUTQ_ERR_DEVICE;
-    const Choice c = choose(a.M, w_rows / 16, p.KT, p.offsets ? a.experts : 0, a.mode, a.saved != nullptr, a.xs != nullptr, cus);
+    // What is kept for gradients or quantised is summed exactly: a last bit there becomes a whole step of a code in what is made of it.
+    const bool exact = a.saved || a.h_codes;
+    const Choice c = choose(a.M, w_rows / 16, p.KT, p.offsets ? a.experts : 0, a.mode, exact, a.xs != nullptr, cus);
     if (c.apart) {
         const lutq_status st = quantize_rows_on(a.x, src, a.M, nullptr, nullptr, 0, a.M, a.K, codes, scales, s);
         if (st != LUTQ_OK) return st;
@@ -922,8 +924,10 @@ lutq_status product_on(const Call& a, hipStream_t s) {
     }
     p.once = c.once;
     p.slices = c.tiles.slices;
-    const hipError_t e = a.mode == kGated ? (a.saved ? launch_of<kGated, true>(c, src, p, cus, s) : launch_of<kGated>(c, src, p, cus, s)) : a.mode == kPowers ? launch_of<kPowers>(c, src, p, cus, s)
-                                                                                                   : launch_of<kPlain>(c, src, p, cus, s);
+    const hipError_t e = a.mode == kPowers  ? launch_of<kPowers>(c, src, p, cus, s)
+                         : a.mode == kPlain ? launch_of<kPlain>(c, src, p, cus, s)
+                         : exact            ? launch_of<kGated, true>(c, src, p, cus, s)
+                                            : launch_of<kGated>(c, src, p, cus, s);
     if (e != hipSuccess) return LUTQ_ERR_DEVICE;
     if (!a.h_codes) return LUTQ_OK;
     return quantize_rows_on(p.y, a.dtype == LUTQ_F16 ? kF16 : kBF16, a.M, nullptr, p.offsets, a.experts, a.M, a.N, a.h_codes, a.h_scales, s);
@@ -985,12 +989,12 @@ extern "C" lutq_status lutq_fp8_weight_grad(const void* dY, const float* dy_scal
 
 extern "C" int lutq_calib_fp8_launch(int64_t M, int64_t N, int64_t K, int64_t experts, int form, int x_is_codes, int compute_units, int* launch) {
     if (!launch) return LUTQ_ERR_NULL;
-    constexpr int kSaved = 3;
-    const bool gate = form == kGated || form == kSaved;
+    constexpr int kExact = 3;
+    const bool gate = form == kGated || form == kExact;
     if (form < 0 || form > 3 || experts < 0 || M < 1 || compute_units < 1 || compute_units > 4096 || (form == kPowers && (experts || !x_is_codes)) ||
         (gate ? lutq_fp8_gated_workspace_bytes(M, N, K, experts ? experts : 1) : lutq_fp8_workspace_bytes(M, N, K, experts ? experts : 1)) == 0)
         return LUTQ_ERR_SHAPE;
-    const Choice c = choose(M, N / 16 * (gate ? 2 : 1), K / 128, experts, form == kSaved ? kGated : form, form == kSaved, x_is_codes != 0, compute_units);
+    const Choice c = choose(M, N / 16 * (gate ? 2 : 1), K / 128, experts, form == kExact ? kGated : form, form == kExact, x_is_codes != 0, compute_units);
     const bool streamed = c.tiles.shape < 0;
     const TileSize t = streamed ? TileSize{gate ? 32 : 16, 16, c.waves, stream_depth(gate ? kGated : kPlain)} : kTiles[c.tiles.shape];
     const int out[8] = {c.apart, t.channels, t.rows, t.waves, t.room, c.tiles.slices, streamed ? 1 + c.pieces : 0, c.once};

@@ -541,7 +541,7 @@ def test_gated(lutq, M, F, K, act, dtype, dense):
         assert worst_of(as_f64(saved[:, at:at + F]), sums[0], off_by_at_most(sums, K, dtype)) <= 1.0
     codes, hs = p.out("u8"), empty(F // 128, M, dtype="f32")
     lutq.lutq_fp8_gated(x, p.W, p.sw, codes, p.ws, x_scales=s, activation=act, h_scales=hs, dtype=torch_dtype(dtype))
-    assert check_h_codes(codes, hs, h) and p.guards_hold() and p.clean()
+    assert check_h_codes(codes, hs, again) and p.guards_hold() and p.clean()
     codes, was = p.out("u8"), saved.clone()
     saved.fill_(0)
     lutq.lutq_fp8_gated(x, p.W, p.sw, codes, p.ws, x_scales=s, activation=act, h_scales=hs, saved=saved, dtype=torch_dtype(dtype))
@@ -572,7 +572,7 @@ def test_gated_by_expert(lutq, name, F, K, act, dtype, dense):
     plain = p.out()
     lutq.lutq_fp8_gated_grouped(x, p.W, p.sw, to_gpu(off), plain, p.ws, x_scales=s, activation=act)
     assert worst_of(as_f64(plain), want, bound) <= 1.0 and p.guards_hold()
-    codes, hs, h = p.out("u8"), empty(F // 128, p.M, dtype="f32"), plain
+    codes, hs = p.out("u8"), empty(F // 128, p.M, dtype="f32")
     lutq.lutq_fp8_gated_grouped(x, p.W, p.sw, to_gpu(off), codes, p.ws, x_scales=s, activation=act, h_scales=hs, dtype=torch_dtype(dtype))
     inside = slice(int(off[0]), int(off[-1]))
     assert check_h_codes(codes[inside], hs[:, inside], h[inside]) and p.guards_hold()
