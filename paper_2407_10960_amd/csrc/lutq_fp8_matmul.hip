@@ -730,7 +730,7 @@ hipError_t launch_stream(ProductParams p, int waves, int runs, hipStream_t s) {
 
 // Output channels (kGated: of both projections) and rows of a tile, wavefronts, and steps of room, by shape.
 struct TileSize { int channels, rows, waves, room; };
-constexpr TileSize kTiles[] = {{256, 256, 8, 2}, {128, 128, 8, 4}, {128, 64, 8, 4}, {64, 64, 4, 4}, {256, 128, 8, 3}};
+constexpr TileSize kTiles[] = {{256, 256, 8, 2}, {128, 128, 8, 4}, {128, 64, 8, 4}, {64, 64, 4, 4}, {256, 128, 8, 3}, {256, 192, 8, 2}};
 
 template <int SHAPE, int WN, int WM, int GN, int GM, int DEPTH, int MODE, bool EXACT>
 hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
@@ -758,11 +758,11 @@ hipError_t launch_tiles(ProductParams p, int cus, hipStream_t s) {
 // of times that are estimated, in microseconds, from the bytes of weights over the pieces of rows (B), or from the rounds of tiles (n, for two small tiles
 // at once on a unit the number on the busiest) and of steps of 128 columns (S; 1.8 of them for each of the exact sums'):
 //   streamed    4.1 + B / 5.8 TB/s (by expert 4, gated 10 from the caches)   256 x 256   4.8 + n (1.52 S + 5.6)         256 x 128   2.8 + n (0.88 S + 2.9)
-//   128 x 128   3.9 + n (0.57 S + 1.4)      128 x 64    3.25 + n (0.428 S + 0.7)       64 x 64     2.25 + n (0.374 S + 0.9), two at once 0.7 S + 0.9
+//   256 x 192   4.8 + n (1.19 S + 4.5)      128 x 128   3.9 + n (0.57 S + 1.4)      128 x 64    3.25 + n (0.428 S + 0.7)       64 x 64     2.25 + n (0.374 S + 0.9), two at once 0.7 S + 0.9
 // and for z slices, each of S / z steps, 5.0 + 0.75 z, 3.6 + 0.75 z and 3.0 + 0.45 z more for storing and joining sums.  The constants are least squares
 // over 228 drawn calls of every shape, corrected on others; on those the best choice was 1 .. 3 % faster on average, by expert 6 %.  Examples, us (weights from
 // memory): 1594 rows, 288 x 13824: 64 x 64 in four slices 21.3, 128 x 128 in six (taken) 24.2, 256 x 128 82; 2048 rows gated, 27648 x 5120: 256 x 256
-// (taken) 296, 256 x 128 330; 33 rows gated, 2304 x 4224: streamed (taken) 7.2, 64 x 64 in three slices 10.8; 224 rows of 14 experts, 9008 x 1920: streamed 89,
+// (taken) 296, 256 x 128 330; 1751 rows, 5120 x 2944, where tiles of 256 x 256 are 140 for 256 units: 256 x 192 (taken) 32.8, 256 x 256 37.5, 256 x 128 45; 33 rows gated, 2304 x 4224: streamed (taken) 7.2, 64 x 64 in three slices 10.8; 224 rows of 14 experts, 9008 x 1920: streamed 89,
 // tiles (taken) 52.
 struct TileChoice { int shape, slices; };             // shape -1: streamed
 
@@ -791,8 +791,9 @@ TileChoice choose_tiles(int64_t M, int64_t NB, int64_t KT, int64_t experts, int 
         return up < 2.0 ? up : 0.8 * up + 0.2 * exact_rounds;
     };
     auto pairs = [&](double n, double one, double two) { return two * (double)(int64_t)(n / 2) + ((int64_t)n % 2 ? one : 0.0); };
-    const double t0 = tiles(16, 256), t1 = tiles(8, 128), t2 = tiles(8, 64), t3 = tiles(4, 64), t4 = tiles(16, 128);
+    const double t0 = tiles(16, 256), t1 = tiles(8, 128), t2 = tiles(8, 64), t3 = tiles(4, 64), t4 = tiles(16, 128), t5 = tiles(16, 192);
     if (!exact) consider(0, 1, 4.8 + rounds(t0) * (1.52 * S + 5.6 * (t0 < cus ? t0 / cus : 1.0)));
+    if (!exact) consider(5, 1, 4.8 + rounds(t5) * (1.19 * S + 4.5 * (t5 < cus ? t5 / cus : 1.0)));
     consider(4, 1, 2.8 + rounds(t4) * (0.88 * S + 2.9));
     const double most = (experts ? 0.7 : 1.0) * cus;   // slices that run at once
     for (int z = 1; z <= 8; ++z) {
@@ -870,6 +871,9 @@ template <int MODE, bool EXACT = false> hipError_t launch_of(const Choice& c, in
         case 2: return launch_tiles<2, 2, 2, 4, 2, 4, MODE, EXACT>(p, cus, s);
         case 3: return launch_tiles<3, 2, 2, 2, 2, 4, MODE, EXACT>(p, cus, s);
         case 4: return launch_tiles<4, 4, 4, 4, 2, 3, MODE, EXACT>(p, cus, s);
+        case 5:
+            if constexpr (!EXACT) return launch_tiles<5, 8, 3, 2, 4, 2, MODE, EXACT>(p, cus, s);
+            return hipErrorInvalidValue;
     }
     if constexpr (MODE != kPowers) return launch_stream_of<MODE>(src, c, p, s);
     return hipErrorInvalidValue;

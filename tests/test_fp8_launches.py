@@ -22,7 +22,8 @@ CALLS = [
     ("gated", 275, 1664, 384, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("gated", 132, 11136, 128, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
     ("gated", 386, 640, 3840, 0, 0, (1, 128, 64, 8, 4, 3, 0, 0)), ("gated", 132, 768, 11904, 0, 0, (1, 128, 64, 8, 4, 7, 0, 0)),
     ("gated", 328, 5504, 256, 0, 1, (0, 256, 128, 8, 3, 1, 0, 0)), ("gated", 1104, 7424, 256, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)),
-    ("gated", 2518, 1664, 256, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)), ("gated", 2078, 9728, 384, 0, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
+    ("gated", 1669, 2432, 256, 0, 0, (1, 256, 192, 8, 2, 1, 0, 0)), ("gated", 1432, 11008, 256, 0, 1, (0, 256, 192, 8, 2, 1, 0, 0)),
+    ("gated", 252, 16640, 256, 0, 0, (1, 256, 256, 8, 2, 1, 0, 0)), ("gated", 2078, 9728, 384, 0, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
     ("gated", 1, 128, 128, 0, 0, (0, 32, 16, 1, 2, 1, 1, 0)), ("gated", 1, 128, 256, 0, 0, (0, 32, 16, 2, 2, 1, 1, 0)),
     ("gated", 1, 128, 1024, 0, 0, (0, 32, 16, 8, 2, 1, 1, 0)), ("gated", 1, 7808, 2688, 0, 0, (0, 32, 16, 4, 2, 1, 1, 1)),
     ("gated", 2, 2688, 7808, 0, 0, (0, 32, 16, 8, 2, 1, 1, 1)), ("gated", 1, 128, 128, 0, 1, (0, 32, 16, 1, 2, 1, 2, 0)),
@@ -36,7 +37,8 @@ CALLS = [
     ("gated", 430, 640, 9088, 1, 0, (1, 128, 128, 8, 4, 4, 0, 0)), ("gated", 206, 2304, 384, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
     ("gated", 213, 8576, 128, 1, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("gated", 198, 768, 6912, 1, 1, (0, 128, 64, 8, 4, 4, 0, 0)),
     ("gated", 1913, 1280, 256, 1, 1, (0, 256, 128, 8, 3, 1, 0, 0)), ("gated", 1567, 5120, 128, 1, 1, (0, 256, 128, 8, 3, 1, 0, 0)),
-    ("gated", 5740, 2688, 2304, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)), ("gated", 5146, 4224, 1152, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
+    ("gated", 4914, 2432, 3456, 1, 0, (1, 256, 192, 8, 2, 1, 0, 0)), ("gated", 5740, 2688, 2304, 1, 0, (1, 256, 192, 8, 2, 1, 0, 0)),
+    ("gated", 12947, 1280, 1792, 1, 1, (0, 256, 256, 8, 2, 1, 0, 0)), ("gated", 5146, 4224, 1152, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
     ("gated", 1, 128, 128, 1, 0, (0, 32, 16, 1, 2, 1, 1, 0)), ("gated", 1, 128, 256, 1, 0, (0, 32, 16, 2, 2, 1, 1, 0)),
     ("gated", 1, 128, 1024, 1, 0, (0, 32, 16, 8, 2, 1, 1, 0)), ("gated", 43, 3840, 128, 43, 0, (0, 32, 16, 1, 2, 1, 1, 1)),
     ("gated", 9, 2944, 896, 8, 0, (0, 32, 16, 4, 2, 1, 1, 1)), ("gated", 3, 896, 7808, 3, 0, (0, 32, 16, 8, 2, 1, 1, 1)),
@@ -76,7 +78,7 @@ CALLS = [
     ("gated_saved", 20, 5504, 384, 10, 1, (0, 32, 16, 2, 2, 1, 3, 1)), ("gated_saved", 16, 1920, 5504, 2, 1, (0, 32, 16, 8, 2, 1, 3, 1)),
     ("gated_saved", 5, 128, 128, 1, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("gated_saved", 390, 384, 1280, 1, 1, (0, 64, 64, 4, 4, 3, 0, 0)),
     ("gated_saved", 231, 256, 4992, 1, 1, (0, 64, 64, 4, 4, 7, 0, 0)), ("matmul", 777, 2640, 512, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)),
-    ("matmul", 773, 10208, 384, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)), ("matmul", 493, 2064, 4992, 0, 0, (1, 128, 128, 8, 4, 3, 0, 0)),
+    ("matmul", 1285, 7792, 128, 0, 0, (1, 128, 128, 8, 4, 1, 0, 0)), ("matmul", 493, 2064, 4992, 0, 0, (1, 128, 128, 8, 4, 3, 0, 0)),
     ("matmul", 658, 992, 6912, 0, 0, (1, 128, 128, 8, 4, 5, 0, 0)), ("matmul", 716, 1360, 384, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
     ("matmul", 769, 5104, 128, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("matmul", 451, 1168, 3840, 0, 1, (0, 128, 64, 8, 4, 3, 0, 0)),
     ("matmul", 322, 672, 11392, 0, 0, (1, 128, 64, 8, 4, 7, 0, 0)), ("matmul", 1, 16, 128, 0, 0, (0, 16, 16, 1, 4, 1, 1, 0)),
@@ -88,7 +90,8 @@ CALLS = [
     ("matmul", 9, 16, 256, 0, 1, (0, 16, 16, 2, 4, 1, 3, 0)), ("matmul", 9, 16, 1024, 0, 1, (0, 16, 16, 8, 4, 1, 3, 0)),
     ("matmul", 9, 6192, 6784, 0, 1, (0, 16, 16, 4, 4, 1, 3, 1)), ("matmul", 9, 4048, 10368, 0, 0, (1, 16, 16, 8, 4, 1, 3, 1)),
     ("matmul", 1690, 2416, 256, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)), ("matmul", 3715, 4384, 256, 0, 0, (1, 256, 128, 8, 3, 1, 0, 0)),
-    ("matmul", 1514, 5392, 256, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)), ("matmul", 4225, 9584, 384, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)),
+    ("matmul", 1514, 5392, 256, 0, 1, (0, 256, 192, 8, 2, 1, 0, 0)), ("matmul", 1051, 29312, 256, 0, 0, (1, 256, 192, 8, 2, 1, 0, 0)),
+    ("matmul", 200, 33520, 256, 0, 0, (1, 256, 256, 8, 2, 1, 0, 0)), ("matmul", 4225, 9584, 384, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)),
     ("matmul", 17, 16, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("matmul", 16491, 304, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)),
     ("matmul", 372, 576, 2432, 0, 1, (0, 64, 64, 4, 4, 4, 0, 0)), ("matmul", 155, 752, 6272, 0, 0, (1, 64, 64, 4, 4, 7, 0, 0)),
     ("matmul", 1704, 1808, 768, 1, 0, (1, 128, 128, 8, 4, 1, 0, 0)), ("matmul", 10012, 800, 256, 1, 1, (0, 128, 128, 8, 4, 1, 0, 0)),
@@ -104,7 +107,8 @@ CALLS = [
     ("matmul", 11, 16, 1152, 1, 1, (0, 16, 16, 8, 4, 1, 3, 0)), ("matmul", 46, 14352, 128, 23, 1, (0, 16, 16, 1, 4, 1, 3, 1)),
     ("matmul", 14, 1808, 1792, 13, 1, (0, 16, 16, 2, 4, 1, 3, 1)), ("matmul", 10, 2688, 15616, 1, 0, (1, 16, 16, 8, 4, 1, 3, 1)),
     ("matmul", 2755, 1696, 256, 1, 0, (1, 256, 128, 8, 3, 1, 0, 0)), ("matmul", 789, 19504, 128, 1, 0, (1, 256, 128, 8, 3, 1, 0, 0)),
-    ("matmul", 10739, 2768, 2304, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)), ("matmul", 6387, 5280, 1920, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
+    ("matmul", 4473, 4800, 4480, 1, 0, (1, 256, 192, 8, 2, 1, 0, 0)), ("matmul", 2916, 9232, 2944, 1, 1, (0, 256, 192, 8, 2, 1, 0, 0)),
+    ("matmul", 17289, 1664, 2176, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)), ("matmul", 6387, 5280, 1920, 1, 0, (1, 256, 256, 8, 2, 1, 0, 0)),
     ("matmul", 5, 16, 128, 1, 0, (1, 64, 64, 4, 4, 1, 0, 0)), ("matmul", 130, 23728, 128, 1, 1, (0, 64, 64, 4, 4, 1, 0, 0)),
     ("matmul", 195, 880, 2304, 1, 1, (0, 64, 64, 4, 4, 3, 0, 0)), ("matmul", 99, 736, 7168, 1, 0, (1, 64, 64, 4, 4, 7, 0, 0)),
     ("weight_grad", 800, 2544, 512, 0, 1, (0, 128, 128, 8, 4, 1, 0, 0)), ("weight_grad", 784, 12624, 128, 0, 1, (0, 128, 128, 8, 4, 1, 0, 0)),
@@ -112,7 +116,8 @@ CALLS = [
     ("weight_grad", 784, 1232, 384, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)), ("weight_grad", 784, 5104, 128, 0, 1, (0, 128, 64, 8, 4, 1, 0, 0)),
     ("weight_grad", 464, 1152, 3840, 0, 1, (0, 128, 64, 8, 4, 3, 0, 0)), ("weight_grad", 304, 800, 11392, 0, 1, (0, 128, 64, 8, 4, 7, 0, 0)),
     ("weight_grad", 1680, 2416, 256, 0, 1, (0, 256, 128, 8, 3, 1, 0, 0)), ("weight_grad", 4816, 3360, 256, 0, 1, (0, 256, 128, 8, 3, 1, 0, 0)),
-    ("weight_grad", 5456, 1424, 256, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)), ("weight_grad", 4320, 9568, 384, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)),
+    ("weight_grad", 5456, 1424, 256, 0, 1, (0, 256, 192, 8, 2, 1, 0, 0)), ("weight_grad", 2208, 14576, 256, 0, 1, (0, 256, 192, 8, 2, 1, 0, 0)),
+    ("weight_grad", 208, 33968, 256, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)), ("weight_grad", 4320, 9568, 384, 0, 1, (0, 256, 256, 8, 2, 1, 0, 0)),
     ("weight_grad", 16, 16, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)), ("weight_grad", 18384, 272, 128, 0, 1, (0, 64, 64, 4, 4, 1, 0, 0)),
     ("weight_grad", 16, 16, 2304, 0, 1, (0, 64, 64, 4, 4, 3, 0, 0)), ("weight_grad", 16, 16, 6272, 0, 1, (0, 64, 64, 4, 4, 7, 0, 0)),
 ]
