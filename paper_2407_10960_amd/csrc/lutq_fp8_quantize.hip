@@ -3,6 +3,8 @@
 // All are bound by memory traffic.  Sixteen lanes ("team") hold 128 columns, eight values each, so every load is 16 (fp32: 32)
 // consecutive bytes per lane and whole cache lines per wavefront.  Where a square of 128 x 128 is looked at as one (weights, columns,
 // gradients), a workgroup holds it in registers, a 4 x 8 block per lane: its rows' and columns' codes both leave from there.
+// Measured, us and what they read and write a second: rows of 8192 x 8192 bf16 33 (6.1 TB/s), 1003 picked rows of 2176 fp16 3.7; weights 28672 x 4096
+// fp32 104 (5.6 TB/s), bf16 with those of the transposed as well 72 (6.5 TB/s); columns of 4096 x 4096 bf16 11; weights back to bf16 50 (7.0 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -256,7 +258,8 @@ struct GradParams {
 };
 
 // dU = dH act(G), dG = dH U act'(G), of a square of 128 x 128 of H, in every form that is asked for from the same registers: 6 bytes a value are
-// read, 2 written for the codes of rows and 2 for those of columns.
+// read, 2 written for the codes of rows and 2 for those of columns.  4096 x 14336 bf16: 145 .. 155 us, 3.9 TB/s, vector instructions
+// issued for 73 % of the cycles; with registers for one workgroup a unit instead of two (a few values in scratch memory) 177, computed once for either layout 231.
 template <int SRC>
 __global__ __launch_bounds__(kSquare, 4) void gated_grad(const GradParams p) {
     __shared__ __align__(16) char tile[16 * 1024];
