@@ -138,7 +138,10 @@ __device__ __forceinline__ float activated(float g, int act) { return g * sigma(
 __device__ __forceinline__ void activated(float g, int act, float& f, float& slope) {
     const float s = sigma(argument(g, act)), rest = 1.0f - s;
     f = g * s;
-    slope = act == kSilu ? s + f * rest : s + f * rest * (1.5957691216057308f * (1.0f + 0.134145f * g * g));
+    // (Beyond the ends f rest is 0 and stays it, whatever g is: z' by itself passes fp32's largest number from |g| = 5e19 on, and 0 times that would be no
+    // number.  Holding g at +-64 for it instead takes one instruction more, 159 us for 147 at 4096 x 14336.)
+    const float t = f * rest;
+    slope = act == kSilu ? s + t : s + 1.5957691216057308f * (t + 0.134145f * (t * g * g));
 }
 
 }  // namespace fp8

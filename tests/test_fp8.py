@@ -651,6 +651,36 @@ def test_gated_gradient(lutq, M, F, act, dtype):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_gated_gradient_far_beyond_the_activation(lutq, act, dtype):
+    """G from 128 to the type's largest number, of either sign: sigma is 1 or 0 there, to far less than 2^-24 (sigma(-128) < 2^-184), and so is the slope.
+    dG = dH U and dU = dH G are products of two 16-bit numbers, which fp32 holds; three roundings of 2^-24 are allowed all the same.  Every block and column
+    of the quantised forms has a scale."""
+    import torch
+    M, F = 130, 256
+    rng = np.random.default_rng(5)
+    t = lambda a: torch.from_numpy(a).to(torch_dtype(dtype)).cuda()
+    g = np.exp2(rng.uniform(7, {"f16": 15.9, "bf16": 127.9}[dtype], (M, F))) * rng.choice([-1, 1], (M, F))
+    g[0, :8], g[1, :8] = BIG[dtype], -BIG[dtype]
+    if dtype == "bf16":
+        g[2, :6] = [1e19, -1e19, 3.7e19, -3.7e19, 6e19, -6e19]      # (about where 0.134 G^2 passes fp32's largest number)
+    gu = t(np.concatenate([g, rng.standard_normal((M, F)) * 4], 1))
+    dh = t(rng.standard_normal((M, F)) * 2.0 ** -5)
+    d, g, u = as_f64(dh), as_f64(gu[:, :F]), as_f64(gu[:, F:])
+    ref = np.concatenate([np.where(g > 0, d * u, 0.0), np.where(g > 0, d * g, 0.0)], 1)
+    up = -(-M // 128)
+    dense, (rc, rs), (cc, cs) = empty(M, 2 * F, dtype=dtype), (empty(M, 2 * F), empty(2 * F // 128, M, dtype="f32")), (empty(2 * F, up * 128), empty(up, 2 * F, dtype="f32"))
+    lutq.lutq_fp8_gated_grad(dh, gu, activation=act, dense=dense, rows=(rc, rs), columns=(cc, cs))
+    assert worst_of(as_f64(dense), ref, half_step(ref, dtype) + 3 * 2.0 ** -24 * np.abs(ref)) <= 1.0 and (as_f64(dense)[ref == 0] == 0).all()
+    assert rs.isfinite().all().item() and cs.isfinite().all().item()
+    off = 3 * 2.0 ** -24 * np.abs(ref)
+    near = lambda values, scales: (np.abs(values - ref) <= np.maximum(np.abs(ref) * 2.0 ** -4, scales * 2.0 ** -10) * (1 + 2.0 ** -20) + off).all()
+    assert near(fx.row_values(as_u8(rc), rs.cpu().numpy()), np.repeat(rs.cpu().numpy().astype(np.float64).T, 128, 1))
+    assert near(fx.row_values(as_u8(cc), cs.cpu().numpy()).T[:M], np.repeat(cs.cpu().numpy().astype(np.float64), 128, 0)[:M])
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("N,K,M", [(16, 16, 1), (48, 128, 128), (64, 80, 300), (272, 144, 129), (304, 528, 1000), (1040, 272, 640), (2816, 1152, 300), (144, 96, 9000)])
 def test_weight_gradient(lutq, N, K, M, dtype):
