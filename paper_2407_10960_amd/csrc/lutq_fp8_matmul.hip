@@ -79,6 +79,7 @@ __device__ __forceinline__ void store_four(char* to, const f32x4& sum, int bf16)
 // The sums of the codes are exact (Wide): the 16-bit instruction's half rate is far above what the reads leave to do.
 // Measured (weights as a program finds them, partly in the caches): one row, 6144 x 4096, 6.0 us; gated 28672 x 4096 16.4 (7.2 TB/s); 250 rows of 64 experts, 2816 x
 // 2048, 59 (5.8 TB/s).  A first form with the weights loaded into operand registers took 14 and 28 us a call from Python for the first two, this one 6.9 and 19.4.
+constexpr int kStreamWaves = 8;                        // per workgroup at most; registers for two such workgroups a compute unit
 constexpr int kAhead = 8;                              // blocks of X per sixteen lanes that are asked for at a time
 
 // Waits until at most BLOCKS times N of this wavefront's global loads are under way.
@@ -98,7 +99,7 @@ constexpr int stream_sums(int mode) { return 2 * (mode == kGated ? 2 : 1) * 1024
 __device__ __forceinline__ float scalar_at(const float* p) { return *(const __attribute__((address_space(4))) float*)(uintptr_t)p; }
 
 template <int SRC, int XP, int MODE, bool GROUPED, bool ONCE>
-__global__ __launch_bounds__(1024) void stream_kernel(const ProductParams p) {
+__global__ __launch_bounds__(64 * kStreamWaves, 4) void stream_kernel(const ProductParams p) {
     constexpr int R = MODE == kGated ? 2 : 1, DEPTH = stream_depth(MODE);
     static_assert(DEPTH <= 4, "as wait_blocks knows");
     static_assert((SRC == kF32) == (XP > 0), "codes come in pieces");
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(1024) void stream_kernel(const ProductParams p) {
         m1 = min(in.end, m0 + 16);
     }
     const int rows = m1 - m0;
-    // This workgroup's row blocks and this wavefront's part of K (up to 2^15 blocks over sixteen wavefronts: the products fit).
+    // This workgroup's row blocks and this wavefront's part of K (up to 2^15 blocks over eight wavefronts: the products fit).
     const int run = (int)blockIdx.x, each = quotient(p.NB, (int)gridDim.x), more = p.NB - each * (int)gridDim.x;
     const int rb0 = run * each + min(run, more), rb1 = rb0 + each + (run < more ? 1 : 0);
     const int kb0 = quotient(wave * p.KT, waves), kb1 = quotient((wave + 1) * p.KT, waves);
@@ -850,7 +851,7 @@ Choice choose(int64_t M, int64_t NB, int64_t KT, int64_t experts, int mode, bool
     // A row block's K is shared by as few wavefronts as leave all of them with work: each sum through LDS costs a barrier.  By expert, 14 rows of 18,
     // 3200 x 7808: eight 51.9 us, four 37.9, two 39.0; two of 5, 9984 x 11264: 150, 127, 114; 768 channels of 9856 (48 row blocks): 11.8, 13.6, 20.3.
     // Values of one row, 6144 x 4096: eight 7.5, four 6.9; 640 x 9984: 9.5, 12.0.
-    const int64_t all = blocks * pieces, most_waves = into_lds ? (KT <= (experts ? 16 : 32) && all >= cus ? 4 : 8) : all < cus ? 8 : experts && all >= 2 * cus ? 2 : 4;
+    const int64_t all = blocks * pieces, most_waves = into_lds ? (KT <= (experts ? 16 : 32) && all >= cus ? 4 : kStreamWaves) : all < cus ? kStreamWaves : experts && all >= 2 * cus ? 2 : 4;
     int64_t waves = KT < most_waves ? KT : most_waves;
     while (waves > 1 && waves * per_wave + shared > kLds) --waves;
     int64_t at_once = kLds / (waves * per_wave + shared);                      // workgroups per compute unit

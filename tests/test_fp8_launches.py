@@ -156,6 +156,18 @@ def test_no_kind_of_launch_is_missing(lutq):
             assert kind(form, M, N, experts, codes, lutq.calib_fp8_launch(M, N, K, experts, form, codes)) in have, (form, M, N, K, experts, codes)
 
 
+def test_no_launch_has_more_wavefronts_than_its_kernel_is_built_for(lutq):
+    """Eight, of a workgroup that streams as of one of tiles."""
+    rng = random.Random(13)
+    some = lambda a, b: round(math.exp(rng.uniform(math.log(a), math.log(b))))
+    seen = set()
+    for _ in range(10000):
+        form, experts = rng.choice(("matmul", "gated", "gated_saved")), rng.choice((0, some(1, 1000)))
+        r = lutq.calib_fp8_launch(some(1, 60), 128 * some(1, 1000), 128 * some(1, 4000), experts, form, rng.random() < 0.5, some(1, 4096))
+        seen.add((r.streamed > 0, r.waves))
+    assert {w for _, w in seen} <= set(range(1, 9)) and (True, 8) in seen
+
+
 def test_refusals_of_the_question(lutq):
     import ctypes
     f = lutq.load_library().lutq_calib_fp8_launch
