@@ -130,7 +130,8 @@ __device__ __forceinline__ i32x8 operand(u32x4 a, u32x4 b) {
 }
 
 // The gate's activation g sigma(z), z = g, or 2 sqrt(2 / pi) (g + 0.044715 g^3) (gelu in its tanh form), and its derivative
-// sigma + g sigma (1 - sigma) z'.  exp and the reciprocal are the hardware's, off by an ulp or two of 32 bits; beyond the ends sigma is 0 or 1.
+// sigma + g sigma (1 - sigma) z'.  exp and the reciprocal are the hardware's: sigma is off by some steps of 2^-24 relative to it, and by about |z| as
+// many, since z log2 e is rounded before the power of two is taken ((16 + 8 |z|) 2^-24 holds everywhere); beyond the ends it is 0 or 1.
 enum Activation { kSilu = 0, kGelu = 1 };
 __device__ __forceinline__ float sigma(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 __device__ __forceinline__ float argument(float g, int act) { return act == kSilu ? g : 1.5957691216057308f * (g + 0.044715f * g * g * g); }
