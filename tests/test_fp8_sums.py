@@ -9,6 +9,7 @@ that their products, 4 to 14.1, lie below 2^-13 2^17 = 16 and are the whole of t
 Bounds as in test_fp8.py: (K / 128 + 22) 2^-22 of the magnitudes, which here are at most 16 448^2 + 112 14.1 a block of 128 columns, 3470 times the mean sum:
 a sum may be off by (K / 128 + 22) / 1209 of the mean, where cutting takes all of it; K is at most 124 blocks, so that is 0.13."""
 import math
+import random
 
 import numpy as np
 import pytest
@@ -63,6 +64,20 @@ def test_every_launch_with_exact_sums_is_among_them():
         assert {s[2:] for s in shapes if s[1] == experts} >= {(256, 128, False), *(t + (z,) for t in ((128, 128), (128, 64), (64, 64)) for z in (False, True))}
         for form in ("matmul", "gated", "gated_saved"):
             assert {c[6][6] for c in EXACT if c[0] == form and bool(c[4]) == experts and c[6][6]} == {1, 2, 3}
+
+
+def test_few_rows_are_streamed_whatever_the_sizes(lutq):
+    """Up to 16 rows, by expert up to 4 for each, which are promised exact sums; 17 and more are not all."""
+    rng = random.Random(3)
+    some = lambda a, b: round(math.exp(rng.uniform(math.log(a), math.log(b))))
+    tiles = 0
+    for _ in range(20000):
+        form, experts = rng.choice(("matmul", "gated", "gated_saved")), rng.choice((0, some(1, 65536)))
+        M = 4 * experts + 1 if experts else 17
+        N, K, codes, units = 128 * some(1, min(8000, 2 ** 28 // M)), 128 * some(1, min(8000, 2 ** 28 // M)), rng.random() < 0.5, some(1, 4096)
+        assert lutq.calib_fp8_launch(rng.randint(1, M - 1), N, K, experts, form, codes, units).streamed
+        tiles += not lutq.calib_fp8_launch(M, N, K, experts, form, codes, units).streamed
+    assert tiles
 
 
 class Made(Factors):
