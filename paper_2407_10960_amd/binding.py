@@ -994,7 +994,8 @@ def lutq_fp8_gated(X, W, w_scales, H, workspace, x_scales=None, activation="silu
     """H [M, F] = act(X G^T) * (X U^T), W [2 F, K] = G over U, X as for lutq_fp8_matmul; activation "silu" or "gelu" (tanh form).
     H: float16 or bfloat16; or, with h_scales [F / 128, M], codes, quantised from H rounded to `dtype` (that of X where it is no
     codes).  saved [M, 2 F]: takes the two projections side by side, for lutq_fp8_gated_grad.  With h_scales or saved the sums of codes
-    are exact, at 1.9 times the time where rows are many."""
+    are exact, at 1.4 to 2.1 times the time where rows are many; H at 16 bits without saved, and then lutq_fp8_quantize, is the faster way to
+    codes of an H whose last bits may differ."""
     return _fp8_gated("lutq_fp8_gated", X, W, w_scales, None, H, workspace, x_scales, activation, h_scales, saved, dtype, stream)
 
 
