@@ -552,18 +552,20 @@ typedef enum {
     LUTQ_GELU = 1              /* g / 2 (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) */
 } lutq_activation;
 
-/* The gated block's projections, activation and product in one kernel: with G and U the two halves of the rows of X W^T,
+/* The gated block's projections, activation and product, fused: with G and U the two halves of the rows of X W^T,
  *        H[m, f] = act(G[m, f]) * U[m, f],  G = X W[0 .. F - 1]^T,  U = X W[F .. 2 F - 1]^T
  *   X, x_scales          as for lutq_fp8_matmul;  W, w_scales  WEIGHTS [2 F, K], the gate's rows first
  *   H                    device, [M, F], dtype, or NULL
  *   h_codes, h_scales    device, or NULL: ROWS [M, F], what lutq_fp8_quantize makes of H of `dtype`, ready for the down projection's product.
  *                        H, these, or all of them
  *   saved                device, [M, 2 F], dtype, or NULL: G and U side by side, for lutq_fp8_gated_grad
+ *   workspace            >= lutq_fp8_gated_workspace_bytes(M, F, K, 1), as for lutq_fp8_matmul
+ * The projections and H are one launch; G and U go through memory only as `saved`, and as partial sums where a small H has K cut into slices.  X of 16 bits
+ * and many rows is quantised by a launch before it, and H by one behind it, from H (where H is not asked for, from the workspace).
  * With h_codes or saved the sums are exact at any number of rows (above): a last bit of G or U that differs becomes a whole step of a code where H or the
  * gradients are quantised.  With few rows that costs nothing, with many up to twice the time and a little more (2 F x K, rows: 2816 x 1152, 300: 1.4 times;
  * 27648 x 5120, 2048: 1.75; 28672 x 4096, 512 to 8192: 1.9 to 2.1).  H may differ in its last bits from that of a call without either, and whoever would
  * rather have the codes of that H sooner takes it at 16 bits and gives it to lutq_fp8_quantize.
- *   workspace            >= lutq_fp8_gated_workspace_bytes(M, F, K, 1), as for lutq_fp8_matmul
  * Errors: those of lutq_fp8_matmul; DTYPE also for an activation that there is not.
  * By expert (lutq_fp8_gated_grouped; W: `experts` of them) as for lutq_fp8_matmul_grouped: rows outside stay in every output. */
 lutq_status lutq_fp8_gated(const void* X, const float* x_scales, const void* W, const float* w_scales, int64_t M, int64_t F, int64_t K,
