@@ -590,10 +590,11 @@ lutq_status lutq_fp8_gated_grad(const void* dH, const void* saved, int64_t M, in
 /* Second part, the gradient of any product's weights: dW[n, k] = sum_m dY[m, n] * X[m, k], rounded once to `dtype`.
  *   dY, dy_scales   device, COLUMNS of the gradient of Y: codes [N, M], scales [M / 128, N]
  *   X, x_scales     device, COLUMNS of X: codes [K, M], scales [M / 128, K]
- *   M               rows, with those that fill them up: a multiple of 128, at least 128
+ *   M               rows, with those that fill them up: a multiple of 128, from 128 to 2^22 (they are the product's K; gradients of more are added up by
+ *                   the caller)
  *   dW              device, [N, K], dtype; fully overwritten
  *   workspace       >= lutq_fp8_workspace_bytes(N, K, M, 1), as for lutq_fp8_matmul
- * N and K multiples of 16.  The scales have to be powers of two from 2^-126 on (or not a number), as the quantiser of columns makes them: the matrix
+ * N and K multiples of 16, K up to 2^24, N * M / 128 < 2^30.  The scales have to be powers of two from 2^-126 on (or not a number), as the quantiser of columns makes them: the matrix
  * instruction takes their exponents.  Errors: those of lutq_fp8_matmul; SHAPE for M = 0, too. */
 lutq_status lutq_fp8_weight_grad(const void* dY, const float* dy_scales, const void* X, const float* x_scales, int64_t N, int64_t K, int64_t M,
                                  lutq_dtype dtype, void* dW, void* workspace, size_t workspace_bytes, void* stream);

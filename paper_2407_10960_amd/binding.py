@@ -1035,7 +1035,7 @@ def lutq_fp8_gated_grad(dH, saved, activation="silu", dense=None, rows=None, col
 
 def lutq_fp8_weight_grad(dY, dy_scales, X, x_scales, dW, workspace, stream=None):
     """dW [N, K] (float16 or bfloat16) = the sum over rows of dY times X, both by columns: codes [N, M'] with scales [M' / 128, N], codes
-    [K, M'] with scales [M' / 128, K].  workspace: new_fp8_workspace(N, K, M')."""
+    [K, M'] with scales [M' / 128, K], M' up to 2^22.  workspace: new_fp8_workspace(N, K, M')."""
     name = "lutq_fp8_weight_grad"
     if stream is None and _done(_native().fp8_weight_grad(dY, dy_scales, X, x_scales, dW, workspace), name):
         return dW
