@@ -810,11 +810,11 @@ extern "C" const char* lutq_status_string(lutq_status s) {
         case LUTQ_ERR_NULL: return "null pointer";
         case LUTQ_ERR_BITS: return "bits must be 2, 3 or 4";
         case LUTQ_ERR_GROUP: return "group_size must be 32, 64, 128 or 256 and divide K";
-        case LUTQ_ERR_SHAPE: return "unsupported shape (N % 16 == 0; table-quantised: 1 <= M <= 128, K % K-tile == 0; microscaled: K % 128 == 0)";
-        case LUTQ_ERR_ALIGN: return "device pointer not 16-byte aligned";
+        case LUTQ_ERR_SHAPE: return "unsupported shape (N % 16 == 0; table-quantised: 1 <= M <= 128, K % K-tile == 0; microscaled and 8-bit: K % 128 == 0; gated: F % 128 == 0)";
+        case LUTQ_ERR_ALIGN: return "device pointer not aligned (to 16 bytes; row numbers, offsets and 32-bit scales to 4)";
         case LUTQ_ERR_INDEX_RANGE: return "index out of range for the bit width";
         case LUTQ_ERR_WORKSPACE: return "workspace missing or too small";
-        case LUTQ_ERR_DTYPE: return "dtype must be LUTQ_F16 or LUTQ_BF16";
+        case LUTQ_ERR_DTYPE: return "dtype must be LUTQ_F16 or LUTQ_BF16, activation LUTQ_SILU or LUTQ_GELU";
         case LUTQ_ERR_DEVICE: return "HIP runtime error";
         case LUTQ_ERR_PLAN: return "invalid plan";
         case LUTQ_ERR_SCRATCH: return "the work decomposition needs more partial-sum scratch than lutq_matmul_static's built-in LUTQ_STATIC_SCRATCH_BYTES";

@@ -207,6 +207,13 @@ def test_refusals_before_any_launch(lutq):
     assert w(dY=a + 8) == w(ds=a + 2) == w(X=a + 1) == w(dW=a + 8) == ALIGN and w(wk=None) == w(wb=need - 1) == WORKSPACE
 
 
+def test_what_an_error_says_is_so_of_8_bit_calls(lutq):
+    """Each status's text names the limit that the call was refused for."""
+    text = lambda status: lutq.load_library().lutq_status_string(status).decode()
+    assert "8-bit: K % 128" in text(4) and "F % 128" in text(4) and "N % 16" in text(4)
+    assert "to 4" in text(5) and "LUTQ_GELU" in text(8)
+
+
 def test_binding_refuses_host_tensors(lutq):
     import torch
     x, u = torch.zeros((16, 128), dtype=torch.float16), torch.zeros((16, 128), dtype=torch.uint8)
