@@ -979,8 +979,12 @@ def _fp8_activation(name, activation):
     return _FP8_ACTIVATIONS[activation]
 
 
-def _fp8_gated(name, X, W, w_scales, offsets, H, workspace, x_scales, activation, h_scales, saved, dtype, stream):
+def _fp8_gated(name, X, W, w_scales, offsets, H, workspace, x_scales, activation, h_scales, saved, dtype, stream, h_codes):
     act = _fp8_activation(name, activation)
+    if h_codes is not None:
+        if h_scales is None:
+            raise TypeError(f"{name}: h_codes needs h_scales")
+        return _fp8_product(name, X, x_scales, W, w_scales, offsets, H, workspace, stream, (act, H.dtype, h_codes, h_scales, saved))
     if h_scales is None:
         return _fp8_product(name, X, x_scales, W, w_scales, offsets, H, workspace, stream, (act, H.dtype, None, None, saved))
     if dtype is None:
@@ -990,21 +994,22 @@ def _fp8_gated(name, X, W, w_scales, offsets, H, workspace, x_scales, activation
     return _fp8_product(name, X, x_scales, W, w_scales, offsets, None, workspace, stream, (act, dtype, H, h_scales, saved))
 
 
-def lutq_fp8_gated(X, W, w_scales, H, workspace, x_scales=None, activation="silu", h_scales=None, saved=None, dtype=None, stream=None):
+def lutq_fp8_gated(X, W, w_scales, H, workspace, x_scales=None, activation="silu", h_scales=None, saved=None, dtype=None, stream=None, h_codes=None):
     """H [M, F] = act(X G^T) * (X U^T), W [2 F, K] = G over U, X as for lutq_fp8_matmul; activation "silu" or "gelu" (tanh form).
     H: float16 or bfloat16; or, with h_scales [F / 128, M], codes, quantised from H rounded to `dtype` (that of X where it is no
-    codes).  saved [M, 2 F]: takes the two projections side by side, for lutq_fp8_gated_grad.  With h_scales or saved the sums of codes
+    codes); or, with h_codes [M, F] and h_scales, both: H at 16 bits (for its columns, in training), and the codes quantised from it.
+    saved [M, 2 F]: takes the two projections side by side, for lutq_fp8_gated_grad.  With h_scales or saved the sums of codes
     are exact, at 1.4 to 2.1 times the time where rows are many; H at 16 bits without saved, and then lutq_fp8_quantize, is the faster way to
     codes of an H whose last bits may differ."""
-    return _fp8_gated("lutq_fp8_gated", X, W, w_scales, None, H, workspace, x_scales, activation, h_scales, saved, dtype, stream)
+    return _fp8_gated("lutq_fp8_gated", X, W, w_scales, None, H, workspace, x_scales, activation, h_scales, saved, dtype, stream, h_codes)
 
 
 def lutq_fp8_gated_grouped(X, W, w_scales, offsets, H, workspace, x_scales=None, activation="silu", h_scales=None, saved=None, dtype=None,
-                           stream=None):
+                           stream=None, h_codes=None):
     """The same by expert, as lutq_fp8_matmul_grouped: W [experts, 2 F, K].  Rows outside stay as they were in every output."""
     if offsets is None:
         raise TypeError("lutq_fp8_gated_grouped: offsets must be int32, [experts + 1]")
-    return _fp8_gated("lutq_fp8_gated_grouped", X, W, w_scales, offsets, H, workspace, x_scales, activation, h_scales, saved, dtype, stream)
+    return _fp8_gated("lutq_fp8_gated_grouped", X, W, w_scales, offsets, H, workspace, x_scales, activation, h_scales, saved, dtype, stream, h_codes)
 
 
 def lutq_fp8_gated_grad(dH, saved, activation="silu", dense=None, rows=None, columns=None, stream=None):

@@ -574,3 +574,47 @@ def test_the_binding_refuses(lutq):
     with pytest.raises(TypeError):
         grad(dw=empty(256, 48, dtype="f32"))
     torch.cuda.synchronize()
+
+
+def test_codes_of_h_beside_h_need_their_scales(lutq):
+    import torch
+    x, u, s = torch.zeros((16, 128), dtype=torch.float16), torch.zeros((16, 128), dtype=torch.uint8), torch.zeros((1, 16))
+    for call in (lambda **k: lutq.lutq_fp8_gated(x, u, s, x, u, **k), lambda **k: lutq.lutq_fp8_gated_grouped(x, u, s, torch.zeros(3, dtype=torch.int32), x, u, **k)):
+        with pytest.raises(TypeError, match="h_scales"):
+            call(h_codes=u)
+        with pytest.raises(ValueError, match="CUDA"):
+            call(h_codes=u, h_scales=s)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("dense", [False, True])
+@pytest.mark.parametrize("M", [1, 12, 130, 700])
+def test_h_and_its_codes_by_the_binding(lutq, monkeypatch, M, dense, native):
+    """H at 16 bits and the codes that the quantiser makes of it, the bits of the calls that give either; by expert too, rows outside untouched; refusals."""
+    import torch
+    F, K = 256, 384
+    if not native:
+        monkeypatch.setattr(lutq.binding, "_NATIVE", lutq.binding._NoNative)
+    p, e = Problem(lutq, M, F, K, "bf16", gated=True), Problem(lutq, M, F, K, "bf16", experts=2, gated=True)
+    off = np.array([min(1, M - 1), M // 2, M - M // 10], np.int32)
+    for q, call, inside in ((p, lambda *a, **k: lutq.lutq_fp8_gated(q.args(dense)[0], q.W, q.sw, *a, x_scales=q.args(dense)[1], **k), slice(0, M)),
+                            (e, lambda *a, **k: lutq.lutq_fp8_gated_grouped(q.args(dense)[0], q.W, q.sw, to_gpu(off), *a, x_scales=q.args(dense)[1], **k),
+                             slice(int(off[0]), int(off[-1])))):
+        h, codes, hs, saved = q.out(), empty(M + 32, F), empty(F // 128, M, dtype="f32"), empty(M, 2 * F, dtype="bf16")
+        assert call(h, q.ws, h_codes=codes[16:16 + M], h_scales=hs, saved=saved) is h
+        assert check_h_codes(codes[16:16 + M][inside], hs[:, inside], h[inside]) and q.guards_hold() and q.clean()
+        assert (codes[:16] == 0x7f).all().item() and (codes[16 + M:] == 0x7f).all().item()
+        outside = torch.ones(M, dtype=torch.bool, device="cuda")
+        outside[inside] = False
+        assert (h[outside] == -7.0).all().item() and (codes[16:16 + M][outside] == 0x7f).all().item() and (hs[:, outside] == -7.0).all().item()
+        alone, its_scales, h16, kept = empty(M, F), empty(F // 128, M, dtype="f32"), empty(M, F, dtype="bf16"), empty(M, 2 * F, dtype="bf16")
+        call(alone, q.ws, h_scales=its_scales, dtype=torch.bfloat16)
+        call(h16, q.ws, saved=kept)
+        assert torch.equal(alone, codes[16:16 + M]) and torch.equal(its_scales, hs) and torch.equal(h16, h) and torch.equal(kept, saved)
+        with pytest.raises(ValueError, match="shapes"):
+            call(h, q.ws, h_codes=empty(M, 2 * F), h_scales=hs)
+        with pytest.raises(TypeError):
+            call(h, q.ws, h_codes=empty(M, F, dtype="bf16"), h_scales=hs)
+        with pytest.raises(TypeError):
+            call(codes[16:16 + M], q.ws, h_codes=codes[16:16 + M], h_scales=hs)
