@@ -29,7 +29,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t unbounded(const char* base) {
 // Sixteen bytes per lane that workgroups on other dies read, or wrote, in the same launch.
 // Stores of sixteen bytes have their whole offset in the vector register and the instruction, none in a scalar register: the data are read over
 // several cycles, and only without a scalar offset does the compiler keep the next instruction from overwriting the first of them (seen to be
-// stored overwritten: the address of the next store, in the last lanes of a row).
+// stored overwritten: the address of the next store, in the last lanes of a row).  The additions cost nothing that shows: 28 microscaled calls, listed and drawn
+// ones, took 0.986 to 1.012 of the time without them, in turn (8192 x 8192 x 8192 266.9 us and 266.4; 1024 x 4096 x 14336 45.6 and 45.6).
 __device__ __forceinline__ void store16_shared(__amdgpu_buffer_rsrc_t to, uint32_t lane_at, int at, f32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), to, lane_at + at, 0, kSc1);
 }
