@@ -259,7 +259,7 @@ struct GradParams {
 
 // dU = dH act(G), dG = dH U act'(G), of a square of 128 x 128 of H, in every form that is asked for from the same registers: 6 bytes a value are
 // read, 2 written for the codes of rows and 2 for those of columns.  4096 x 14336 bf16: 145 .. 155 us, 3.9 TB/s, vector instructions
-// issued for 73 % of the cycles; with registers for one workgroup a unit instead of two (a few values in scratch memory) 177, computed once for either layout 231.
+// issued for 70 % of the cycles; with registers for one workgroup a unit instead of two (a few values in scratch memory) 177, computed once for either layout 231.
 template <int SRC>
 __global__ __launch_bounds__(kSquare, 4) void gated_grad(const GradParams p) {
     __shared__ __align__(16) char tile[16 * 1024];
